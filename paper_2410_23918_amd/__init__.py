@@ -31,3 +31,14 @@ from .binding import (  # noqa: F401
     strerror,
     unpack_image_host,
 )
+
+_F8 = ("F8Rows", "Routing", "combine", "f8_workspace_bytes", "grouped_linear_f8", "linear_f8", "quantise_f8", "quantise_weight_f8", "route")
+
+
+def __getattr__(name):
+    """The 8-bit products and the routing (f8.py) need PyTorch: loaded at their first use."""
+    if name not in _F8:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import f8
+    globals().update({n: getattr(f8, n) for n in _F8})
+    return globals()[name]

@@ -1,0 +1,345 @@
+// Around the products grouped by expert (f8_product.hip): which experts a token goes to and where its rows lie, the list of tiles that
+// the grouped product works through, and the weighted sums of a token's rows.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "f8.h"
+
+namespace bitstack {
+
+// inclusive scan of v[0 .. n) in LDS by the whole workgroup (n <= blockDim.x), OP associative
+template <class OP>
+__device__ __forceinline__ void scan_lds(int* v, int n, OP op) {
+    const int i = threadIdx.x;
+    for (int d = 1; d < n; d <<= 1) {
+        const int mine = i < n ? (i >= d ? op(v[i - d], v[i]) : v[i]) : 0;
+        __syncthreads();
+        if (i < n) v[i] = mine;
+        __syncthreads();
+    }
+}
+
+// The tiles of the groups: group e has the rows [end[e - 1], end[e]), cut into pieces of tile_rows; the rows past the last group are one
+// more group, of zeros.
+__global__ __launch_bounds__(1024) void k_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles) {
+    __shared__ int end[kMaxExperts + 1], upto[kMaxExperts + 1];
+    const int i = threadIdx.x;
+    if (i < experts) end[i] = min(max(offsets[i + 1], 0), rows);
+    __syncthreads();
+    scan_lds(end, experts, [](int a, int b) { return max(a, b); });
+    if (i == 0) end[experts] = rows;
+    __syncthreads();
+    for (int e = i; e <= experts; e += 1024) upto[e] = (end[e] - (e ? end[e - 1] : 0) + tile_rows - 1) / tile_rows;
+    __syncthreads();
+    scan_lds(upto, experts, [](int a, int b) { return a + b; });
+    if (i == 0) upto[experts] += upto[experts - 1];
+    __syncthreads();
+    for (int t = i; t < n_tiles; t += 1024) {
+        int lo = 0, hi = experts + 1;   // the first group with upto > t
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (upto[mid] > t) hi = mid;
+            else lo = mid + 1;
+        }
+        F8Tile tile = {-1, 0, 0, 0};
+        if (lo <= experts) {
+            const int first = (lo ? end[lo - 1] : 0) + (t - (lo ? upto[lo - 1] : 0)) * tile_rows;
+            tile = {lo < experts ? lo : -1, first, min(tile_rows, end[lo] - first), 0};
+        }
+        tiles[t] = tile;
+    }
+}
+
+hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st) {
+    hipLaunchKernelGGL(k_f8_worklist, dim3(1), dim3(1024), 0, st, offsets, experts, rows, tile_rows, tiles, n_tiles);
+    return hipGetLastError();
+}
+
+// ---- routing.  Tokens are cut into chunks, one workgroup each, worked through 64 tokens at a time.  k_route_choose takes the top_k of every
+// token, a wavefront a token, and counts a chunk's rows by expert; k_route_place adds up the counts before its own chunk and ranks its
+// rows.  Ranks are counted with ballots, in order, so the places do not depend on the order in which anything runs.  One chunk: one launch.
+constexpr int kRouteStep = 64, kRouteChunks = 256;
+
+// Orders like the logit; 0: not to be taken (NaN, -infinity)
+__device__ __forceinline__ unsigned route_key(float l) {
+    if (!(l > -INFINITY)) return 0;
+    l = fminf(l, 3.402823466e38f) + 0.0f;   // -0 -> 0
+    const unsigned b = __float_as_uint(l);
+    return b ^ (unsigned(int(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float route_value(unsigned key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// NL: experts per lane.  The j-th lane ends with the j-th choice (-1: none) and its weight.
+template <int T, int NL>
+__device__ __forceinline__ void choose(const RouteParams& p, int token, int lane, int& expert, float& weight) {
+    const typename Elem<T>::type* const l = static_cast<const typename Elem<T>::type*>(p.logits) + size_t(token) * p.ld;
+    unsigned key[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        const int e = i * 64 + lane;
+        key[i] = e < p.experts ? route_key(float(l[e])) : 0;
+    }
+    unsigned taken[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) taken[i] = key[i];
+    unsigned mine = 0;
+    expert = -1;
+    for (int j = 0; j < p.top_k; ++j) {
+        unsigned long long best = 0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {   // the larger key, of equal ones the lower index
+            const unsigned long long c = (unsigned long long)(taken[i]) << 32 | (0xffffffffu - unsigned(i * 64 + lane));
+            best = c > best ? c : best;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const unsigned long long o = __shfl_xor(best, d);
+            best = o > best ? o : best;
+        }
+        const unsigned k = unsigned(best >> 32);
+        if (k == 0) break;
+        const int e = int(0xffffffffu - unsigned(best));
+        if (lane == j) {
+            mine = k;
+            expert = e;
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+            if (i * 64 + lane == e) taken[i] = 0;
+    }
+    const float most = route_value(unsigned(__shfl(int(mine), 0)));
+    const float share = mine ? expf(route_value(mine) - most) : 0.0f;
+    float total;
+    if (p.renormalise) {
+        total = wave_sum(share);
+    } else {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) sum += key[i] ? expf(route_value(key[i]) - most) : 0.0f;
+        total = wave_sum(sum);
+    }
+    weight = mine ? share / total : 0.0f;
+}
+
+struct RouteLds {
+    int base[kMaxExperts];                     // where an expert's rows of this step begin
+    int count[kMaxExperts];
+    short chosen[kRouteStep * kMaxTopK];
+    unsigned short before[];                   // [top_k][experts]: an expert's rows in the 64-entry groups before
+};
+
+template <int T, int NL>
+__device__ __forceinline__ void choose_step(const RouteParams& p, RouteLds& s, int token0) {
+    const int lane = threadIdx.x & 63;
+    for (int t = threadIdx.x >> 6; t < kRouteStep && token0 + t < p.tokens; t += 16) {
+        int expert;
+        float weight;
+        choose<T, NL>(p, token0 + t, lane, expert, weight);
+        if (lane < p.top_k) {
+            const size_t at = size_t(token0 + t) * p.top_k + lane;
+            p.chosen[at] = expert;
+            p.weights[at] = weight;
+            s.chosen[t * p.top_k + lane] = short(expert);
+        }
+    }
+}
+
+// Ranks the step's entries (s.chosen, n of them in the order of (token, j)) within their experts and writes their places; s.base moves on.
+__device__ __forceinline__ void place_step(const RouteParams& p, RouteLds& s, int token0, int n) {
+    const int lane = threadIdx.x & 63;
+    for (int i = threadIdx.x; i < p.top_k * p.experts; i += 1024) s.before[i] = 0;
+    __syncthreads();
+    int rank[kMaxTopK / 16];
+#pragma unroll
+    for (int r = 0; r < kMaxTopK / 16; ++r) {
+        const int g = (threadIdx.x >> 6) + 16 * r, i = g * 64 + lane;
+        if (g >= p.top_k) break;
+        const int e = i < n ? s.chosen[i] : -1;
+        unsigned long long same = __ballot(e >= 0);
+#pragma unroll
+        for (int b = 0; b < 10; ++b) {   // the lanes with the same expert
+            const unsigned long long set = __ballot(e >> b & 1);
+            same &= e >> b & 1 ? set : ~set;
+        }
+        rank[r] = __popcll(same & ((1ull << lane) - 1));
+        if (e >= 0 && rank[r] == 0) s.before[g * p.experts + e] = (unsigned short)__popcll(same);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.experts; e += 1024) {
+        int sum = 0;
+        for (int g = 0; g < p.top_k; ++g) {
+            const int c = s.before[g * p.experts + e];
+            s.before[g * p.experts + e] = (unsigned short)sum;
+            sum += c;
+        }
+        s.count[e] = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kMaxTopK / 16; ++r) {
+        const int g = (threadIdx.x >> 6) + 16 * r, i = g * 64 + lane;
+        if (g >= p.top_k) break;
+        if (i >= n) continue;
+        const int e = s.chosen[i];
+        int slot = -1;
+        if (e >= 0) {
+            slot = s.base[e] + s.before[g * p.experts + e] + rank[r];
+            p.index[slot] = token0 + i / p.top_k;
+        }
+        p.slots[size_t(token0) * p.top_k + i] = slot;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.experts; e += 1024) s.base[e] += s.count[e];
+    __syncthreads();
+}
+
+// s.count[e]: all rows of expert e; s.base[e]: its rows in earlier chunks.  Afterwards s.base[e] is where its next row goes.  The first
+// workgroup writes the offsets; all of them share the entries past the last row.
+__device__ __forceinline__ void bases(const RouteParams& p, RouteLds& s) {
+    scan_lds(s.count, p.experts, [](int a, int b) { return a + b; });
+    const int e = threadIdx.x;
+    if (e < p.experts) {
+        s.base[e] += e ? s.count[e - 1] : 0;
+        if (blockIdx.x == 0) {
+            p.offsets[e + 1] = s.count[e];
+            if (e == 0) p.offsets[0] = 0;
+        }
+    }
+    const int rows = s.count[p.experts - 1];
+    for (size_t i = size_t(rows) + blockIdx.x * 1024 + threadIdx.x; i < size_t(p.tokens) * p.top_k; i += size_t(gridDim.x) * 1024) p.index[i] = -1;
+    __syncthreads();
+}
+
+template <int T, int NL, bool ALONE>
+__global__ __launch_bounds__(1024) void k_route_choose(RouteParams p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    RouteLds& s = *reinterpret_cast<RouteLds*>(smem);
+    for (int e = threadIdx.x; e < p.experts; e += 1024) s.count[e] = s.base[e] = 0;
+    const int steps = (p.tokens + kRouteStep - 1) / kRouteStep, per_chunk = (steps + p.chunks - 1) / p.chunks;
+    for (int step = blockIdx.x * per_chunk; step < min(steps, int(blockIdx.x + 1) * per_chunk); ++step) {
+        __syncthreads();
+        choose_step<T, NL>(p, s, step * kRouteStep);
+        __syncthreads();
+        const int n = min(kRouteStep, p.tokens - step * kRouteStep) * p.top_k;
+        for (int i = threadIdx.x; i < n; i += 1024)
+            if (s.chosen[i] >= 0) atomicAdd(&s.count[s.chosen[i]], 1);   // whole numbers: the order does not matter
+    }
+    __syncthreads();
+    if constexpr (ALONE) {   // one step
+        bases(p, s);
+        place_step(p, s, 0, p.tokens * p.top_k);
+    } else {
+        for (int e = threadIdx.x; e < p.experts; e += 1024) p.counts[size_t(blockIdx.x) * p.experts + e] = s.count[e];
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_route_place(RouteParams p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    RouteLds& s = *reinterpret_cast<RouteLds*>(smem);
+    for (int e = threadIdx.x; e < p.experts; e += 1024) s.count[e] = s.base[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.chunks * p.experts; i += 1024) {
+        const int chunk = i / p.experts, e = i - chunk * p.experts, c = p.counts[i];
+        atomicAdd(&s.count[e], c);
+        if (chunk < int(blockIdx.x)) atomicAdd(&s.base[e], c);
+    }
+    __syncthreads();
+    bases(p, s);
+    const int steps = (p.tokens + kRouteStep - 1) / kRouteStep, per_chunk = (steps + p.chunks - 1) / p.chunks;
+    for (int step = blockIdx.x * per_chunk; step < min(steps, int(blockIdx.x + 1) * per_chunk); ++step) {
+        const int token0 = step * kRouteStep, n = min(kRouteStep, p.tokens - token0) * p.top_k;
+        for (int i = threadIdx.x; i < n; i += 1024) s.chosen[i] = short(p.chosen[size_t(token0) * p.top_k + i]);
+        __syncthreads();
+        place_step(p, s, token0, n);
+    }
+}
+
+size_t route_workspace_bytes(int tokens, int experts, int top_k) {
+    (void)tokens, (void)top_k;
+    return size_t(kRouteChunks) * experts * 4;
+}
+
+template <int T, int NL>
+static hipError_t route(const RouteParams& p, hipStream_t st) {
+    const unsigned lds = unsigned(sizeof(RouteLds)) + unsigned(p.top_k * p.experts * 2);
+    const bool alone = p.tokens <= kRouteStep;
+    const void* const kernels[] = {reinterpret_cast<const void*>(&k_route_choose<T, NL, true>), reinterpret_cast<const void*>(&k_route_choose<T, NL, false>),
+                                   reinterpret_cast<const void*>(&k_route_place)};
+    if (lds > 65536)
+        for (const void* k : kernels) {
+            const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+            if (e != hipSuccess) return e;
+        }
+    if (alone) {
+        hipLaunchKernelGGL((k_route_choose<T, NL, true>), dim3(1), dim3(1024), lds, st, p);
+    } else {
+        hipLaunchKernelGGL((k_route_choose<T, NL, false>), dim3(unsigned(p.chunks)), dim3(1024), lds, st, p);
+        hipLaunchKernelGGL(k_route_place, dim3(unsigned(p.chunks)), dim3(1024), lds, st, p);
+    }
+    return hipGetLastError();
+}
+
+template <int T>
+static hipError_t route_of(const RouteParams& p, hipStream_t st) {
+    if (p.experts <= 64) return route<T, 1>(p, st);
+    if (p.experts <= 128) return route<T, 2>(p, st);
+    if (p.experts <= 256) return route<T, 4>(p, st);
+    return route<T, 16>(p, st);
+}
+
+hipError_t launch_route(RouteParams p, int dtype, void* workspace, hipStream_t st) {
+    p.counts = static_cast<int*>(workspace);
+    const int steps = (p.tokens + kRouteStep - 1) / kRouteStep;
+    p.chunks = std::max(1, std::min(steps, kRouteChunks));
+    if (dtype == BITSTACK_T_F16) return route_of<BITSTACK_T_F16>(p, st);
+    if (dtype == BITSTACK_T_BF16) return route_of<BITSTACK_T_BF16>(p, st);
+    return route_of<BITSTACK_T_F32>(p, st);
+}
+
+// ---- y[t] = sum_j weights[t][j] h[slots[t][j]]: eight columns a thread, 16 bytes a load, bound by memory
+template <int T>
+__global__ __launch_bounds__(256) void k_combine(CombineParams p) {
+    typedef typename Elem<T>::type E;
+    const int token = blockIdx.x, col = (blockIdx.y * 256 + threadIdx.x) * 8;
+    if (col >= p.width) return;
+    float sum[8] = {};
+    for (int j = 0; j < p.top_k; ++j) {
+        const int slot = p.slots[size_t(token) * p.top_k + j];
+        if (unsigned(slot) >= unsigned(p.h_rows)) continue;
+        const float w = p.weights[size_t(token) * p.top_k + j];
+        float v[8];
+        load_elems<T, 8>(static_cast<const E*>(p.h) + size_t(slot) * p.ld_h + col, p.width - col, p.vec, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+    }
+    E* const y = static_cast<E*>(p.y) + size_t(token) * p.ld_y + col;
+    if (p.vec && p.width - col >= 8) {
+        typedef E piece __attribute__((ext_vector_type(Elem<T>::kPer16)));
+#pragma unroll
+        for (int i = 0; i < 8 / Elem<T>::kPer16; ++i) {
+            piece u;
+#pragma unroll
+            for (int e = 0; e < Elem<T>::kPer16; ++e) u[e] = E(sum[i * Elem<T>::kPer16 + e]);
+            reinterpret_cast<piece*>(y)[i] = u;
+        }
+    } else {
+        for (int i = 0; i < 8 && col + i < p.width; ++i) y[i] = E(sum[i]);
+    }
+}
+
+hipError_t launch_combine(const CombineParams& p, int dtype, hipStream_t st) {
+    const dim3 grid(unsigned(p.tokens), unsigned((p.width + 2047) / 2048));
+    if (dtype == BITSTACK_T_F16) hipLaunchKernelGGL((k_combine<BITSTACK_T_F16>), grid, dim3(256), 0, st, p);
+    else if (dtype == BITSTACK_T_BF16) hipLaunchKernelGGL((k_combine<BITSTACK_T_BF16>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_combine<BITSTACK_T_F32>), grid, dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace bitstack

@@ -1,0 +1,119 @@
+// Shared by the 8-bit kernels (f8_rows.hip, f8_product.hip), the routing (experts.hip) and their host code (f8_host.cpp).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/bitstack_f8.h"
+#include "rebuild.h"
+
+namespace bitstack {
+
+constexpr int kF8Block = 128;      // columns (and weight rows) that share a scale
+constexpr float kF8Max = 448.0f;   // largest e4m3 value
+constexpr int kMaxExperts = 1024, kMaxTopK = 32;
+
+// one piece of a product: rows [row0, row0 + rows) of y with expert's weight; expert < 0: rows of zeros; rows 0: nothing
+struct F8Tile {
+    int expert, row0, rows, pad;
+};
+
+struct F8Params {
+    const unsigned char* x;    // [x_rows][kp], e4m3, zero past `in`
+    const unsigned char* xs;   // [x_rows][ks] biased exponents
+    const unsigned char* w;    // [experts][out] rows of e4m3, ldw bytes apart
+    const void* ws;            // [experts][ceil(out / 128)][kb]
+    void* y;
+    const int* index;          // [rows] or null
+    const F8Tile* tiles;       // null: one group
+    size_t ldw, ldy;
+    int out, in, kb, kp, ks;   // kb: blocks of columns, kp = 128 kb, ks = kb rounded up to 4
+    int x_rows, rows;          // rows of x, of y
+    int n_tiles;               // tiles of rows (an upper bound where they are grouped)
+    int y_dtype, ws_f32;       // ws_f32: fp32 scales
+    int y_vec;                 // four consecutive outputs may be stored at once
+};
+
+// float of an element, and back
+template <int T>
+struct Elem;
+template <>
+struct Elem<BITSTACK_T_F16> {
+    typedef _Float16 type;
+    static constexpr int kPer16 = 8;
+};
+template <>
+struct Elem<BITSTACK_T_BF16> {
+    typedef __bf16 type;
+    static constexpr int kPer16 = 8;
+};
+template <>
+struct Elem<BITSTACK_T_F32> {
+    typedef float type;
+    static constexpr int kPer16 = 4;
+};
+
+// N consecutive elements as floats; `vec`: 16-byte loads are allowed, and all N are there; else those at or past `n` are zero
+template <int T, int N>
+__device__ __forceinline__ void load_elems(const typename Elem<T>::type* p, int n, bool vec, float (&v)[N]) {
+    typedef typename Elem<T>::type E;
+    constexpr int K = Elem<T>::kPer16;
+    static_assert(N % K == 0, "whole 16-byte pieces");
+    if (vec && n >= N) {
+        typedef E piece __attribute__((ext_vector_type(K)));
+#pragma unroll
+        for (int i = 0; i < N / K; ++i) {
+            const piece u = reinterpret_cast<const piece*>(p)[i];
+#pragma unroll
+            for (int e = 0; e < K; ++e) v[i * K + e] = float(u[e]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = i < n ? float(p[i]) : 0.0f;
+    }
+}
+
+// The least e with amax <= 448 * 2^e, at least -126, biased by 127 (448 = 1.75 * 2^8; amax = 1.f * 2^q): exact, and so is the division by
+// 2^e.  amax finite.
+__device__ __forceinline__ int f8_exponent(float amax) {
+    const unsigned bits = __float_as_uint(amax);
+    const int e = int(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return e < 1 ? 1 : e;
+}
+__device__ __forceinline__ float f8_inverse(int biased) { return __uint_as_float(unsigned(254 - biased) << 23); }   // 2^-e; biased <= 247
+
+hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,
+                              hipStream_t st);
+hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int out, int in, unsigned char* q, size_t ld_q,
+                                     unsigned char* s, hipStream_t st);
+hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st);
+hipError_t launch_f8_product(const F8Params& p, int experts, F8Tile* list, const int* offsets, hipStream_t st);
+// an upper bound on the work list's length, whatever tile the product takes
+size_t f8_worklist_entries(int rows, int experts);
+
+size_t route_workspace_bytes(int tokens, int experts, int top_k);
+struct RouteParams {
+    const void* logits;
+    size_t ld;
+    int tokens, experts, top_k, renormalise;
+    int* chosen;
+    float* weights;
+    int* slots;
+    int* index;
+    int* offsets;
+    int* counts;   // [chunks][experts]
+    int chunks;
+};
+hipError_t launch_route(RouteParams p, int dtype, void* workspace, hipStream_t st);
+struct CombineParams {
+    const void* h;
+    void* y;
+    const int* slots;
+    const float* weights;
+    size_t ld_h, ld_y;
+    int h_rows, width, tokens, top_k, vec;
+};
+hipError_t launch_combine(const CombineParams& p, int dtype, hipStream_t st);
+
+int hip_error(hipError_t e);   // host.cpp: remembers e for bitstack_last_hip_error, BITSTACK_E_HIP
+
+}  // namespace bitstack

@@ -1,0 +1,195 @@
+// Host side of include/bitstack_f8.h: argument checks, the layout of the workspace, dispatch.
+#include <hip/hip_runtime.h>
+
+#include "../../include/bitstack_f8.h"
+#include "f8.h"
+#include "layout.h"
+
+using namespace bitstack;
+
+namespace {
+
+constexpr int kMaxIn = 1 << 20, kMaxOut = 1 << 24;
+constexpr size_t kMaxLd = size_t(1) << 22;               // bytes between two rows of a weight: a tile of 256 is reached by 31-bit offsets
+constexpr size_t kMaxRowBytes = (size_t(1) << 31) - 1;   // 8-bit activations: reached by 31-bit offsets
+
+bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
+bool real_type(int t) { return t == BITSTACK_T_F16 || t == BITSTACK_T_F32 || t == BITSTACK_T_BF16; }
+size_t type_size(int t) { return t == BITSTACK_T_F32 ? 4 : 2; }
+bool columns_ok(int in) { return in >= 1 && in <= kMaxIn; }
+
+struct Workspace {
+    size_t q, scales, list, total;
+};
+Workspace workspace_of(int x_rows, int in, int y_rows, int experts, bool quantised) {
+    Workspace w;
+    w.q = 0;
+    w.scales = quantised ? 0 : align256(size_t(x_rows) * bitstack_f8_row_bytes(in));
+    w.list = quantised ? 0 : w.scales + align256(size_t(x_rows) * bitstack_f8_row_scales(in));
+    w.total = w.list + align256(f8_worklist_entries(y_rows, experts) * sizeof(F8Tile));
+    return w;
+}
+
+int check_rows(const bitstack_f8_rows_t& x, int in) {
+    if (x.rows < 0) return BITSTACK_E_RANGE;
+    if (size_t(x.rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return BITSTACK_E_RANGE;
+    if (x.dtype == BITSTACK_T_F8) {
+        if (x.rows && (!x.x || !x.scales)) return BITSTACK_E_NULL;
+        if (misaligned(x.x, 16)) return BITSTACK_E_ALIGN;
+        return BITSTACK_OK;
+    }
+    if (!real_type(x.dtype) || (x.gated != 0 && x.gated != 1)) return BITSTACK_E_ARG;
+    if (x.rows && !x.x) return BITSTACK_E_NULL;
+    if (misaligned(x.x, type_size(x.dtype))) return BITSTACK_E_ALIGN;
+    if (x.rows > 1 && x.ld < size_t(in) << x.gated) return BITSTACK_E_SHAPE;
+    return BITSTACK_OK;
+}
+
+int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, void* y,
+            int y_dtype, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+    if (y_rows < 0) return BITSTACK_E_RANGE;
+    if (!columns_ok(w->in) || w->out < 1 || w->out > kMaxOut || w->experts < 1 || w->experts > kMaxExperts) return BITSTACK_E_SHAPE;
+    if (w->scale_type != BITSTACK_S_E8M0 && w->scale_type != BITSTACK_S_F32) return BITSTACK_E_ARG;
+    if (!real_type(y_dtype)) return BITSTACK_E_ARG;
+    int rc = check_rows(*x, w->in);
+    if (rc) return rc;
+    if (y_rows == 0) return BITSTACK_OK;
+    if (!w->q || !w->scales || !y) return BITSTACK_E_NULL;
+    if (misaligned(w->q, 16) || w->ld % 16 || (w->scale_type == BITSTACK_S_F32 && misaligned(w->scales, 4))) return BITSTACK_E_ALIGN;
+    if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
+    if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
+    const bool quantised = x->dtype == BITSTACK_T_F8;
+    const Workspace at = workspace_of(x->rows, w->in, y_rows, w->experts, quantised);
+    if (!quantised || offsets) {
+        if (!workspace) return BITSTACK_E_NULL;
+        if (misaligned(workspace, 256)) return BITSTACK_E_ALIGN;
+        if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    F8Params p{};
+    if (quantised) {
+        p.x = static_cast<const unsigned char*>(x->x);
+        p.xs = static_cast<const unsigned char*>(x->scales);
+    } else {
+        if (x->rows) {
+            const hipError_t e = launch_f8_quantise(x->x, x->dtype, x->ld, x->rows, w->in, x->gated != 0, ws + at.q, ws + at.scales, st);
+            if (e != hipSuccess) return hip_error(e);
+        }
+        p.x = ws + at.q;
+        p.xs = ws + at.scales;
+    }
+    p.w = static_cast<const unsigned char*>(w->q);
+    p.ws = w->scales;
+    p.y = y;
+    p.index = index;
+    p.ldw = w->ld;
+    p.ldy = ld_y;
+    p.out = w->out;
+    p.in = w->in;
+    p.kb = (w->in + kF8Block - 1) / kF8Block;
+    p.kp = p.kb * kF8Block;
+    p.ks = int(bitstack_f8_row_scales(w->in));
+    p.x_rows = x->rows;
+    p.rows = y_rows;
+    p.y_dtype = y_dtype;
+    p.ws_f32 = w->scale_type == BITSTACK_S_F32;
+    p.y_vec = ld_y % 4 == 0 && !misaligned(y, 4 * type_size(y_dtype));
+    const hipError_t e = launch_f8_product(p, w->experts, reinterpret_cast<F8Tile*>(ws + at.list), offsets, st);
+    return e == hipSuccess ? BITSTACK_OK : hip_error(e);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t bitstack_f8_row_bytes(int in) { return columns_ok(in) ? (size_t(in) + 127) / 128 * 128 : 0; }
+size_t bitstack_f8_row_scales(int in) { return columns_ok(in) ? ((size_t(in) + 127) / 128 + 3) / 4 * 4 : 0; }
+
+int bitstack_f8_quantise(const void* x, int x_dtype, size_t ld, int rows, int in, int gated, void* q, void* scales,
+                         bitstack_stream_t stream) {
+    if (!columns_ok(in)) return BITSTACK_E_SHAPE;
+    if (x_dtype == BITSTACK_T_F8) return BITSTACK_E_ARG;
+    const bitstack_f8_rows_t r = {x, nullptr, ld, x_dtype, rows, gated};
+    const int rc = check_rows(r, in);
+    if (rc) return rc;
+    if (rows == 0) return BITSTACK_OK;
+    if (!q || !scales) return BITSTACK_E_NULL;
+    if (misaligned(q, 16)) return BITSTACK_E_ALIGN;
+    const hipError_t e = launch_f8_quantise(x, x_dtype, ld, rows, in, gated != 0, static_cast<unsigned char*>(q),
+                                            static_cast<unsigned char*>(scales), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? BITSTACK_OK : hip_error(e);
+}
+
+int bitstack_f8_quantise_weight(const void* w, int w_dtype, size_t ld, int out, int in, void* q, size_t ld_q, void* scales,
+                                bitstack_stream_t stream) {
+    if (!columns_ok(in) || out < 1 || out > kMaxOut) return BITSTACK_E_SHAPE;
+    if (!real_type(w_dtype)) return BITSTACK_E_ARG;
+    if (!w || !q || !scales) return BITSTACK_E_NULL;
+    if (misaligned(w, type_size(w_dtype)) || misaligned(q, 16) || ld_q % 16) return BITSTACK_E_ALIGN;
+    if ((out > 1 && ld < size_t(in)) || ld_q < size_t(in) || ld_q > kMaxLd) return BITSTACK_E_SHAPE;
+    const hipError_t e = launch_f8_quantise_weight(w, w_dtype, ld, out, in, static_cast<unsigned char*>(q), ld_q,
+                                                   static_cast<unsigned char*>(scales), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? BITSTACK_OK : hip_error(e);
+}
+
+size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int experts) {
+    if (x_rows < 0 || y_rows < 0 || !columns_ok(in) || out < 1 || out > kMaxOut || experts < 1 || experts > kMaxExperts) return 0;
+    if (size_t(x_rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return 0;
+    return workspace_of(x_rows, in, y_rows, experts, false).total;
+}
+
+int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, void* y, int y_dtype, size_t ld_y,
+                       void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+    if (!x || !w) return BITSTACK_E_NULL;
+    if (w->experts != 1) return BITSTACK_E_SHAPE;
+    return product(x, w, nullptr, nullptr, x->rows, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
+}
+
+int bitstack_f8_grouped_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets,
+                               const int32_t* index, int y_rows, void* y, int y_dtype, size_t ld_y, void* workspace,
+                               size_t workspace_bytes, bitstack_stream_t stream) {
+    if (!x || !w || !offsets || (!index && y_rows > 0 && y_rows > x->rows)) return !x || !w || !offsets ? BITSTACK_E_NULL : BITSTACK_E_RANGE;
+    if (misaligned(offsets, 4) || misaligned(index, 4)) return BITSTACK_E_ALIGN;
+    return product(x, w, offsets, index, y_rows, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
+}
+
+size_t bitstack_route_workspace_bytes(int tokens, int experts, int top_k) {
+    if (tokens < 0 || experts < 1 || experts > kMaxExperts || top_k < 1 || top_k > kMaxTopK || top_k > experts) return 0;
+    return align256(route_workspace_bytes(tokens, experts, top_k));
+}
+
+int bitstack_route(const void* logits, int dtype, size_t ld, int tokens, int experts, int top_k, int renormalise,
+                   int32_t* chosen, float* weights, int32_t* slots, int32_t* index, int32_t* offsets, void* workspace,
+                   size_t workspace_bytes, bitstack_stream_t stream) {
+    if (tokens < 0 || size_t(tokens) * size_t(top_k > 0 ? top_k : 0) > 0x7fffffffu) return BITSTACK_E_RANGE;
+    if (experts < 1 || experts > kMaxExperts || top_k < 1 || top_k > kMaxTopK || top_k > experts) return BITSTACK_E_SHAPE;
+    if (!real_type(dtype) || (renormalise != 0 && renormalise != 1)) return BITSTACK_E_ARG;
+    if (!offsets || !workspace || (tokens && (!logits || !chosen || !weights || !slots || !index))) return BITSTACK_E_NULL;
+    if (misaligned(logits, type_size(dtype)) || misaligned(chosen, 4) || misaligned(weights, 4) || misaligned(slots, 4) || misaligned(index, 4) ||
+        misaligned(offsets, 4) || misaligned(workspace, 256))
+        return BITSTACK_E_ALIGN;
+    if (tokens > 1 && ld < size_t(experts)) return BITSTACK_E_SHAPE;
+    if (workspace_bytes < bitstack_route_workspace_bytes(tokens, experts, top_k)) return BITSTACK_E_BUFSIZE;
+    RouteParams p{logits, ld, tokens, experts, top_k, renormalise, chosen, weights, slots, index, offsets, nullptr, 0};
+    const hipError_t e = launch_route(p, dtype, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? BITSTACK_OK : hip_error(e);
+}
+
+int bitstack_combine(const void* h, int dtype, size_t ld_h, int h_rows, int width, const int32_t* slots,
+                     const float* weights, int tokens, int top_k, void* y, size_t ld_y, bitstack_stream_t stream) {
+    if (h_rows < 0 || tokens < 0) return BITSTACK_E_RANGE;
+    if (width < 1 || width > kMaxOut || top_k < 1 || top_k > kMaxTopK) return BITSTACK_E_SHAPE;
+    if (!real_type(dtype)) return BITSTACK_E_ARG;
+    if (tokens == 0) return BITSTACK_OK;
+    if ((h_rows && !h) || !slots || !weights || !y) return BITSTACK_E_NULL;
+    const size_t size = type_size(dtype);
+    if (misaligned(h, size) || misaligned(y, size) || misaligned(slots, 4) || misaligned(weights, 4)) return BITSTACK_E_ALIGN;
+    if ((h_rows > 1 && ld_h < size_t(width)) || (tokens > 1 && ld_y < size_t(width))) return BITSTACK_E_SHAPE;
+    const int vec = !misaligned(h, 16) && !misaligned(y, 16) && ld_h * size % 16 == 0 && ld_y * size % 16 == 0;
+    const CombineParams p{h, y, slots, weights, ld_h, ld_y, h_rows, width, tokens, top_k, vec};
+    const hipError_t e = launch_combine(p, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? BITSTACK_OK : hip_error(e);
+}
+
+}  // extern "C"

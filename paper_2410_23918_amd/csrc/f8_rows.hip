@@ -1,0 +1,142 @@
+// Activations and weights into 8-bit floating point (e4m3), one power-of-two scale for each 128 columns of a row, or for each
+// block of 128 x 128:
+//
+//     s = 2^e, e = the least with max |v| <= 448 * 2^e, at least -126;   q = v / s rounded to nearest even
+//
+// With a power of two the quotient is exact, so that the rounding to e4m3 is the only one.
+#include <hip/hip_runtime.h>
+
+#include "f8.h"
+
+namespace bitstack {
+
+// Four floats, at most 448 in magnitude, to e4m3 (round to nearest even)
+__device__ __forceinline__ unsigned to_f8x4(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return unsigned(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
+}
+
+// |v| as an integer that orders like it, NaN and infinity above all others
+__device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row.  Bound by memory: x is read
+// once and q written once, 16 and 8 bytes a lane.
+template <int T, bool GATED>
+__global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, int vec, unsigned char* q,
+                                                     unsigned char* s, int kp, int ks) {
+    const int lane16 = threadIdx.x & 15;
+    const int per_row = (kp + 511) / 512;   // wavefronts
+    const size_t wave = (size_t(blockIdx.x) * 256 + threadIdx.x) >> 6;
+    const int row = int(wave / per_row);
+    if (row >= rows) return;
+    const int block = int(wave % per_row) * 4 + ((threadIdx.x & 63) >> 4);
+    if (block >= ks) return;
+    if (block * kF8Block >= kp) {
+        if (lane16 == 0) s[size_t(row) * ks + block] = 127;   // the scales' padding
+        return;
+    }
+    const int col = block * kF8Block + lane16 * 8;
+    float v[8];
+    const typename Elem<T>::type* const from = x + size_t(row) * ld + col;
+    load_elems<T, 8>(from, in - col, vec, v);
+    if constexpr (GATED) {
+        float u[8];
+        load_elems<T, 8>(from + in, in - col, vec, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(__fdiv_rn(v[i], __fadd_rn(1.0f, expf(-v[i]))), u[i]);
+    }
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, magnitude_bits(v[i]));
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) m = max(m, unsigned(__shfl_xor(int(m), d, 16)));
+    uint2 bytes;
+    int e = 127;
+    if (m >= 0x7f800000u) {
+        bytes = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);   // a NaN or an infinity in the block: NaN
+    } else {
+        e = f8_exponent(__uint_as_float(m));
+        const float r = f8_inverse(e);
+        bytes = make_uint2(to_f8x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), to_f8x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
+    }
+    *reinterpret_cast<uint2*>(q + size_t(row) * kp + col) = bytes;
+    if (lane16 == 0) s[size_t(row) * ks + block] = (unsigned char)e;
+}
+
+// A workgroup brings a block of 128 rows x 128 columns to 8 bits: sixteen lanes a row, sixteen rows a pass, the values in registers between
+// the maximum and the rounding.
+template <int T>
+__global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<T>::type* w, size_t ld, int out, int in, int vec,
+                                                            unsigned char* q, size_t ld_q, int q_cols, unsigned char* s, int kb) {
+    __shared__ unsigned most[4];
+    const int kblock = blockIdx.x % kb, nblock = blockIdx.x / kb;
+    const int col = kblock * kF8Block + (threadIdx.x & 15) * 8;
+    float v[8][8];
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = nblock * kF8Block + i * 16 + (threadIdx.x >> 4);
+        load_elems<T, 8>(w + size_t(row) * ld + col, row < out ? in - col : 0, vec, v[i]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = max(m, magnitude_bits(v[i][k]));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = max(m, unsigned(__shfl_xor(int(m), d)));
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = max(max(most[0], most[1]), max(most[2], most[3]));
+    const bool bad = m >= 0x7f800000u;
+    const int e = bad ? 127 : f8_exponent(__uint_as_float(m));
+    const float r = f8_inverse(e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = nblock * kF8Block + i * 16 + (threadIdx.x >> 4);
+        if (row >= out || col >= q_cols) continue;
+        const uint2 bytes = bad ? make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu)
+                                : make_uint2(to_f8x4(v[i][0] * r, v[i][1] * r, v[i][2] * r, v[i][3] * r),
+                                             to_f8x4(v[i][4] * r, v[i][5] * r, v[i][6] * r, v[i][7] * r));
+        *reinterpret_cast<uint2*>(q + size_t(row) * ld_q + col) = bytes;
+    }
+    if (threadIdx.x == 0) s[size_t(nblock) * kb + kblock] = (unsigned char)e;
+}
+
+static bool vector_rows(const void* p, size_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0; }
+
+template <int T>
+static void quantise(const void* x, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s, hipStream_t st) {
+    typedef typename Elem<T>::type E;
+    const int kp = (in + 127) / 128 * 128, ks = (kp / 128 + 3) / 4 * 4;
+    // the halves of a gated row begin `in` elements apart
+    const int vec = vector_rows(x, ld, sizeof(E)) && (!gated || size_t(in) * sizeof(E) % 16 == 0);
+    const size_t waves = size_t(rows) * ((kp + 511) / 512);
+    const unsigned grid = unsigned((waves + 3) / 4);
+    if (gated) hipLaunchKernelGGL((k_f8_quantise<T, true>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, s, kp, ks);
+    else hipLaunchKernelGGL((k_f8_quantise<T, false>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, s, kp, ks);
+}
+
+hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,
+                              hipStream_t st) {
+    if (dtype == BITSTACK_T_F16) quantise<BITSTACK_T_F16>(x, ld, rows, in, gated, q, s, st);
+    else if (dtype == BITSTACK_T_BF16) quantise<BITSTACK_T_BF16>(x, ld, rows, in, gated, q, s, st);
+    else quantise<BITSTACK_T_F32>(x, ld, rows, in, gated, q, s, st);
+    return hipGetLastError();
+}
+
+template <int T>
+static void quantise_weight(const void* w, size_t ld, int out, int in, unsigned char* q, size_t ld_q, unsigned char* s, hipStream_t st) {
+    typedef typename Elem<T>::type E;
+    const int kb = (in + 127) / 128, nb = (out + 127) / 128;
+    const int q_cols = int(ld_q < size_t(kb) * 128 ? ld_q : size_t(kb) * 128);   // written: what lies past `in` as zero
+    hipLaunchKernelGGL((k_f8_quantise_weight<T>), dim3(unsigned(size_t(kb) * nb)), dim3(256), 0, st, static_cast<const E*>(w), ld, out, in,
+                       int(vector_rows(w, ld, sizeof(E))), q, ld_q, q_cols, s, kb);
+}
+
+hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int out, int in, unsigned char* q, size_t ld_q,
+                                     unsigned char* s, hipStream_t st) {
+    if (dtype == BITSTACK_T_F16) quantise_weight<BITSTACK_T_F16>(w, ld, out, in, q, ld_q, s, st);
+    else if (dtype == BITSTACK_T_BF16) quantise_weight<BITSTACK_T_BF16>(w, ld, out, in, q, ld_q, s, st);
+    else quantise_weight<BITSTACK_T_F32>(w, ld, out, in, q, ld_q, s, st);
+    return hipGetLastError();
+}
+
+}  // namespace bitstack

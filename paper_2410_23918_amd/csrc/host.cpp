@@ -10,6 +10,7 @@
 
 #include "../../include/bitstack.h"
 #include "../../include/bitstack_bench.h"
+#include "f8.h"
 #include "kernels.h"
 #include "kparams.h"
 #include "layout.h"
@@ -29,6 +30,9 @@ static int hip_fail(hipError_t e) {
     g_last_hip = static_cast<int>(e);
     return BITSTACK_E_HIP;
 }
+namespace bitstack {
+int hip_error(hipError_t e) { return hip_fail(e); }
+}  // namespace bitstack
 #define BS_HIP(call)                                   \
     do {                                               \
         hipError_t e__ = (call);                       \

@@ -1,0 +1,301 @@
+"""ctypes binding of include/bitstack_f8.h (argument marshalling only): products in 8-bit floating point with a scale for each block
+of 128, the same grouped by expert, and the routing around them.
+
+8-bit values are torch.float8_e4m3fn; power-of-two scales are torch.float8_e8m0fnu, others torch.float32.  A weight is a pair (q, scales) of
+tensors, [out, in] and [ceil(out / 128), ceil(in / 128)], with a leading dimension for the weights of a layer of experts; the rows of q lie
+a multiple of 16 bytes apart.  Without `stream` everything runs on the current stream of the tensors' device; with it, what a call allocates belongs
+to that stream, and the caller orders it with the streams that made the inputs and use the outputs."""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+import threading
+from typing import NamedTuple
+
+import torch
+
+from . import binding
+from .binding import BitStackError, _check
+
+T_F16, T_F32, T_BF16, T_F8 = 0, 1, 2, 3
+S_E8M0, S_F32 = 0, 1
+_TYPES = {torch.float16: T_F16, torch.float32: T_F32, torch.bfloat16: T_BF16}
+_SCALES = {torch.float8_e8m0fnu: S_E8M0, torch.float32: S_F32}
+_lib = None
+
+
+class _Weight(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld", C.c_size_t), ("scales", C.c_void_p), ("scale_type", C.c_int), ("out", C.c_int),
+                ("inn", C.c_int), ("experts", C.c_int)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_size_t), ("dtype", C.c_int), ("rows", C.c_int), ("gated", C.c_int)]
+
+
+class _Args(threading.local):
+    """argument blocks of one thread, filled anew for every call"""
+
+    def __init__(self):
+        self.w, self.x = _Weight(), _Rows()
+        self.wp, self.xp = C.byref(self.w), C.byref(self.x)
+
+
+_args = _Args()
+
+
+def _f8_lib():
+    global _lib
+    if _lib is None:
+        L = binding.lib()
+        vp, i32, sz = C.c_void_p, C.c_int, C.c_size_t
+        for name, res, args in (
+            ("bitstack_f8_row_bytes", sz, [i32]),
+            ("bitstack_f8_row_scales", sz, [i32]),
+            ("bitstack_f8_quantise", i32, [vp, i32, sz, i32, i32, i32, vp, vp, vp]),
+            ("bitstack_f8_quantise_weight", i32, [vp, i32, sz, i32, i32, vp, sz, vp, vp]),
+            ("bitstack_f8_workspace_bytes", sz, [i32] * 5),
+            ("bitstack_f8_linear", i32, [vp, vp, vp, i32, sz, vp, sz, vp]),
+            ("bitstack_f8_grouped_linear", i32, [vp, vp, vp, vp, i32, vp, i32, sz, vp, sz, vp]),
+            ("bitstack_route_workspace_bytes", sz, [i32] * 3),
+            ("bitstack_route", i32, [vp, i32, sz, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+            ("bitstack_combine", i32, [vp, i32, sz, i32, i32, vp, vp, i32, i32, vp, sz, vp]),
+        ):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
+        _lib = L
+    return _lib
+
+
+class F8Rows(NamedTuple):
+    """Activations in 8 bits, as quantise_f8 makes them: several products may read them.  q [rows, in rounded up to 128], scales
+    [rows, ceil(in / 128) rounded up to 4], `width` = in."""
+    q: torch.Tensor
+    scales: torch.Tensor
+    width: int
+
+    def values(self) -> torch.Tensor:
+        """the numbers they stand for, fp32 [rows, width]"""
+        n, kb = self.q.shape[0], self.q.shape[1] // 128
+        s = self.scales[:, :kb].view(torch.float8_e8m0fnu).float()
+        return (self.q.float().view(n, kb, 128) * s[:, :, None]).view(n, -1)[:, : self.width]
+
+
+class Routing(NamedTuple):
+    """What `route` returns; see bitstack_route."""
+    experts: torch.Tensor   # int32 [tokens, top_k], -1 where there is none
+    weights: torch.Tensor   # fp32 [tokens, top_k]
+    slots: torch.Tensor     # int32 [tokens, top_k]: the row of (token, j), -1 where there is none
+    rows: torch.Tensor      # int32 [tokens * top_k]: the token of a row, -1 past the last one
+    offsets: torch.Tensor   # int32 [experts + 1]
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: float16, bfloat16 or float32, not {t.dtype}")
+    return code
+
+
+class _On:
+    """The stream of a call: its handle, and the context in which the call allocates (so that what it allocates belongs to that
+    stream).  Inputs used on another stream than the current one are kept from reuse until that stream has passed the call."""
+
+    def __init__(self, device, stream, inputs):
+        if device.type != "cuda":
+            raise ValueError(f"tensors on a GPU are needed, not on {device}")
+        self._ctx = None
+        if stream is None:
+            if device.index == torch.cuda.current_device():
+                self.handle = torch._C._cuda_getCurrentRawStream(device.index)
+                return
+            stream = torch.cuda.current_stream(device)
+        else:
+            _need(stream.device == device, "the stream is another device's")
+            if stream != torch.cuda.current_stream(device):
+                for t in inputs:
+                    if t is not None:
+                        t.record_stream(stream)
+        self.handle = stream.cuda_stream
+        self._ctx = contextlib.ExitStack()
+        self._ctx.enter_context(torch.cuda.stream(stream))   # its device too
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        if self._ctx is not None:
+            self._ctx.close()
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"all tensors have to be on {device}: one is on {t.device}")
+
+
+def _matrix(t: torch.Tensor, what: str):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: a matrix whose rows are contiguous is needed")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _fill_weight(q, scales, grouped):
+    if q.dtype is not torch.float8_e4m3fn:
+        raise ValueError(f"q: float8_e4m3fn, not {q.dtype}")
+    kind = _SCALES.get(scales.dtype)
+    if kind is None:
+        raise ValueError(f"scales: float8_e8m0fnu or float32, not {scales.dtype}")
+    w = _args.w
+    shape = q.shape
+    _need(len(shape) == (3 if grouped else 2) and (q.stride(-1) == 1 or shape[-1] == 1), "q: rows of e4m3, [out, in] or [experts, out, in]")
+    e, out, inn = (shape[0] if grouped else 1), shape[-2], shape[-1]
+    ld = q.stride(-2) if out > 1 else -(-inn // 16) * 16
+    _need(not grouped or e == 1 or q.stride(0) == out * ld, "q: the experts' weights have to follow one another")
+    want = (-(-out // 128), -(-inn // 128))
+    _need(tuple(scales.shape) == ((e, *want) if grouped else want) and scales.is_contiguous(), f"scales: one for each 128 x 128 block of q, {want}, contiguous")
+    w.q, w.ld, w.scales, w.scale_type, w.out, w.inn, w.experts = q.data_ptr(), ld, scales.data_ptr(), kind, out, inn, e
+    return out, inn, e
+
+
+def _fill_rows(x, inn, gated):
+    a = _args.x
+    if isinstance(x, F8Rows):
+        _need(not gated, "gated: apply it in quantise_f8")
+        L = _f8_lib()
+        _need(x.width == inn, f"x has {x.width} columns, the weight {inn}")
+        _need(x.q.dtype is torch.float8_e4m3fn and x.q.is_contiguous() and x.scales.is_contiguous() and x.scales.element_size() == 1
+              and tuple(x.q.shape[1:]) == (L.bitstack_f8_row_bytes(inn),) and tuple(x.scales.shape) == (x.q.shape[0], L.bitstack_f8_row_scales(inn)),
+              "x: as quantise_f8 makes it")
+        _same_device(x.q.device, x.scales)
+        a.x, a.scales, a.ld, a.dtype, a.rows, a.gated = x.q.data_ptr(), x.scales.data_ptr(), 0, T_F8, x.q.shape[0], 0
+        return x.q.shape[0], x.q.device, torch.float16, (x.q, x.scales)
+    t = _type(x, "x")
+    ld = _matrix(x, "x")
+    _need(x.shape[1] == (2 * inn if gated else inn), f"x has {x.shape[1]} columns, the weight {inn}{' (gated: twice as many are needed)' if gated else ''}")
+    a.x, a.scales, a.ld, a.dtype, a.rows, a.gated = x.data_ptr(), None, ld, t, x.shape[0], int(gated)
+    return x.shape[0], x.device, x.dtype, (x,)
+
+
+def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, stream, grouped):
+    L = _f8_lib()
+    out, inn, experts = _fill_weight(q, scales, grouped)
+    x_rows, device, dtype, held = _fill_rows(x, inn, gated)
+    _same_device(device, q, scales, offsets, index, y, workspace)
+    rows = x_rows
+    if grouped:
+        _need(offsets.dtype is torch.int32 and offsets.is_contiguous() and tuple(offsets.shape) == (experts + 1,), "offsets: int32 [experts + 1]")
+        if index is not None:
+            _need(index.dtype is torch.int32 and index.is_contiguous() and index.dim() == 1, "rows: int32 [rows of y]")
+            rows = index.shape[0]
+    with _On(device, stream, (*held, q, scales, offsets, index, y, workspace)) as on:
+        if y is None:
+            y = torch.empty((rows, out), dtype=out_dtype or dtype, device=device)
+        else:
+            _need(tuple(y.shape) == (rows, out) and (out_dtype is None or y.dtype is out_dtype), f"y: [{rows}, {out}] is needed")
+        ld_y = _matrix(y, "y")
+        if workspace is None:
+            nbytes = L.bitstack_f8_workspace_bytes(x_rows, inn, rows, out, experts)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        else:
+            _need(workspace.is_contiguous(), "workspace: contiguous")
+            nbytes = workspace.numel() * workspace.element_size()
+        if grouped:
+            _check(L.bitstack_f8_grouped_linear(_args.xp, _args.wp, offsets.data_ptr(), None if index is None else index.data_ptr(), rows, y.data_ptr(),
+                                                _type(y, "y"), ld_y, workspace.data_ptr(), nbytes, on.handle), "bitstack_f8_grouped_linear")
+        else:
+            _check(L.bitstack_f8_linear(_args.xp, _args.wp, y.data_ptr(), _type(y, "y"), ld_y, workspace.data_ptr(), nbytes, on.handle),
+                   "bitstack_f8_linear")
+    return y
+
+
+def f8_workspace_bytes(x_rows: int, inn: int, y_rows: int, out: int, experts: int = 1) -> int:
+    n = int(_f8_lib().bitstack_f8_workspace_bytes(x_rows, inn, y_rows, out, experts))
+    if n == 0:
+        raise BitStackError(-2, "bitstack_f8_workspace_bytes")
+    return n
+
+
+def linear_f8(x, q, scales, *, gated: bool = False, y=None, out_dtype=None, workspace=None, stream=None):
+    """bitstack_f8_linear: y = x8 w^T.  x [tokens, in] (gated: [tokens, 2 in], gate and value side by side) or an F8Rows; q [out, in] and its
+    scales.  y has the type of x (fp16 for F8Rows) unless given.  workspace: a uint8 tensor of f8_workspace_bytes, else one is allocated."""
+    return _product(x, q, scales, None, None, gated, y, out_dtype, workspace, stream, False)
+
+
+def grouped_linear_f8(x, q, scales, offsets, rows=None, *, gated: bool = False, y=None, out_dtype=None, workspace=None, stream=None):
+    """bitstack_f8_grouped_linear: the rows [offsets[e], offsets[e + 1]) of y are products with expert e's weight, of x's rows of the same
+    number, or of x[rows] where `rows` is given (Routing.rows).  q [experts, out, in].  Rows past the last group are zero."""
+    return _product(x, q, scales, offsets, rows, gated, y, out_dtype, workspace, stream, True)
+
+
+def quantise_f8(x, *, gated: bool = False, stream=None) -> F8Rows:
+    """bitstack_f8_quantise: x [rows, in] (gated: [rows, 2 in]) -> F8Rows."""
+    L = _f8_lib()
+    t, ld = _type(x, "x"), _matrix(x, "x")
+    _need(not gated or x.shape[1] % 2 == 0, "gated: gate and value side by side are needed")
+    n, inn = x.shape[0], x.shape[1] // (2 if gated else 1)
+    with _On(x.device, stream, (x,)) as on:
+        q = torch.empty((n, L.bitstack_f8_row_bytes(inn)), dtype=torch.float8_e4m3fn, device=x.device)
+        s = torch.empty((n, L.bitstack_f8_row_scales(inn)), dtype=torch.uint8, device=x.device)
+        _check(L.bitstack_f8_quantise(x.data_ptr(), t, ld, n, inn, int(gated), q.data_ptr(), s.data_ptr(), on.handle), "bitstack_f8_quantise")
+    return F8Rows(q, s, inn)
+
+
+def quantise_weight_f8(w, *, stream=None):
+    """bitstack_f8_quantise_weight for w [out, in] or [experts, out, in] -> (q, scales), q's rows a multiple of 128 bytes apart and zero
+    past `in`."""
+    L = _f8_lib()
+    _need(w.dim() in (2, 3), "w: [out, in] or [experts, out, in]")
+    t = _type(w, "w")
+    each = w if w.dim() == 3 else w[None]
+    e, out, inn = each.shape
+    ld_q = int(L.bitstack_f8_row_bytes(inn))
+    with _On(w.device, stream, (w,)) as on:
+        q = torch.empty((e, out, ld_q), dtype=torch.float8_e4m3fn, device=w.device)
+        s = torch.empty((e, -(-out // 128), -(-inn // 128)), dtype=torch.float8_e8m0fnu, device=w.device)
+        for i in range(e):
+            _check(L.bitstack_f8_quantise_weight(each[i].data_ptr(), t, _matrix(each[i], "w"), out, inn, q[i].data_ptr(), ld_q, s[i].data_ptr(),
+                                                 on.handle), "bitstack_f8_quantise_weight")
+    q = q[:, :, :inn]
+    return (q, s) if w.dim() == 3 else (q[0], s[0])
+
+
+def route(logits, top_k: int, *, renormalise: bool = True, stream=None) -> Routing:
+    """bitstack_route: logits [tokens, experts] -> Routing."""
+    L = _f8_lib()
+    t, ld = _type(logits, "logits"), _matrix(logits, "logits")
+    n, e = logits.shape
+    with _On(logits.device, stream, (logits,)) as on:
+        nbytes = L.bitstack_route_workspace_bytes(n, e, top_k)
+        if nbytes == 0:
+            raise BitStackError(-2, "bitstack_route_workspace_bytes")
+        i32 = dict(dtype=torch.int32, device=logits.device)
+        r = Routing(torch.empty((n, top_k), **i32), torch.empty((n, top_k), dtype=torch.float32, device=logits.device), torch.empty((n, top_k), **i32),
+                    torch.empty(n * top_k, **i32), torch.empty(e + 1, **i32))
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+        _check(L.bitstack_route(logits.data_ptr(), t, ld, n, e, top_k, int(renormalise), r.experts.data_ptr(), r.weights.data_ptr(), r.slots.data_ptr(),
+                                r.rows.data_ptr(), r.offsets.data_ptr(), ws.data_ptr(), nbytes, on.handle), "bitstack_route")
+    return r
+
+
+def combine(h, slots, weights, *, y=None, stream=None):
+    """bitstack_combine: y[t] = sum_j weights[t, j] h[slots[t, j]], a slot of -1 adds nothing.  h [rows, width]; y has its type."""
+    L = _f8_lib()
+    t, ld = _type(h, "h"), _matrix(h, "h")
+    _need(slots.dtype is torch.int32 and weights.dtype is torch.float32 and slots.dim() == 2 and slots.shape == weights.shape
+          and slots.is_contiguous() and weights.is_contiguous(), "slots: int32, weights: float32, both [tokens, top_k] and contiguous")
+    _same_device(h.device, slots, weights, y)
+    n, k = slots.shape
+    with _On(h.device, stream, (h, slots, weights, y)) as on:
+        if y is None:
+            y = torch.empty((n, h.shape[1]), dtype=h.dtype, device=h.device)
+        else:
+            _need(tuple(y.shape) == (n, h.shape[1]) and y.dtype is h.dtype, "y: [tokens, width] of h's type")
+        _check(L.bitstack_combine(h.data_ptr(), t, ld, h.shape[0], h.shape[1], slots.data_ptr(), weights.data_ptr(), n, k, y.data_ptr(), _matrix(y, "y"),
+                                  on.handle), "bitstack_combine")
+    return y

@@ -1,0 +1,288 @@
+"""The 8-bit products and their quantisers against the oracle in 64 bits, through the public entry points."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2410_23918_amd as B
+from oracle import f8_oracle as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+EPS = {F16: 2.0**-11, BF16: 2.0**-8, F32: 2.0**-24}   # half a step of the outputs' type, relative (bf16: 8 bits)
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def weight(gen, out, inn, scales, experts=None):
+    """e4m3 values of any size, rows with NaN behind them where they end inside 16 bytes, and scales far apart"""
+    e = experts or 1
+    ld = -(-inn // 16) * 16
+    q = (torch.randn((e, out, ld), generator=gen, device=DEV) * 60).clamp(-448, 448).to(torch.float8_e4m3fn)
+    q.view(torch.uint8)[:, :, inn:] = 0x7F
+    q = q[:, :, :inn]
+    shape = (e, -(-out // 128), -(-inn // 128))
+    if scales == "e8m0":
+        s = torch.randint(120, 126, shape, generator=gen, device=DEV, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    else:
+        s = torch.rand(shape, generator=gen, device=DEV) * 0.02 + 1e-3
+    return (q, s) if experts else (q[0], s[0])
+
+
+def acts(gen, n, width, dtype):
+    x = torch.randn((n, width), generator=gen, device=DEV)
+    x[:, :: max(1, width // 5)] *= 30
+    x[:, 1::7] *= 1e-3
+    return x.to(dtype)
+
+
+def rng(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def tolerance(x8, w, dtype, y):
+    """fp32 sums of `in` products: one rounding (2^-23, in case the matrix cores cut off) for each of the 128 terms of an instruction, for each
+    block and for the eight partial sums, relative to the sum of magnitudes; then the rounding to the output's type.  16-bit outputs: the 8-bit
+    instruction cuts seven products of each eight columns to a multiple of 2^-13 of the eighth."""
+    steps = 128 + -(-x8.shape[1] // 128) + 8
+    a, b = np.abs(x8), np.abs(w)
+    bound = steps * 2.0**-23 * (a @ b.T) + EPS[dtype] * np.abs(y) + (2.0**-25 if dtype is F16 else 0)
+    if dtype is not F32:
+        most = lambda v: np.pad(v, ((0, 0), (0, -v.shape[1] % 8))).reshape(len(v), -1, 8).max(axis=2)
+        bound += 7 * 2.0**-13 * (most(a) @ most(b).T)
+    return bound
+
+
+SHAPES = [  # tokens, out, in
+    (1, 1, 1), (1, 16, 128), (1, 512, 512), (1, 1056, 2001), (2, 130, 127), (3, 100, 129), (5, 33, 4096), (15, 257, 640), (16, 256, 256), (17, 96, 300),
+    (31, 1000, 1111), (57, 1056, 2001), (64, 512, 1024), (65, 129, 513), (127, 255, 1152), (128, 128, 128), (129, 384, 2048), (200, 1056, 1040), (255, 640, 777),
+    (257, 513, 1280), (300, 1024, 4096), (513, 300, 384),
+]
+
+
+@pytest.mark.parametrize("scales", ["e8m0", "f32"])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["f16", "bf16", "f32"])
+@pytest.mark.parametrize("tokens,out,inn", SHAPES)
+def test_linear(tokens, out, inn, dtype, scales):
+    g = rng(tokens * 7 + out + inn)
+    q, s = weight(g, out, inn, scales)
+    x = acts(g, tokens, inn, dtype)
+    y = B.linear_f8(x, q, s)
+    assert y.dtype is dtype and tuple(y.shape) == (tokens, out)
+    x8, _ = O.quantise_rows(np64(x))
+    w = O.weight_values(np64(q), np64(s))
+    want = x8 @ w.T
+    if dtype is F16:   # beyond fp16's range both are infinite
+        want = np.where(np.abs(want) >= 65520, np.sign(want) * np.inf, want)
+    fine = np.isfinite(want)
+    got = np64(y)
+    assert np.array_equal(got[~fine], want[~fine])
+    assert (np.abs(got - want)[fine] <= tolerance(x8, w, dtype, want)[fine]).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 9, 40, 300])
+def test_linear_of_whole_numbers_is_exact(tokens):
+    """Small whole numbers: every product and every sum is exact in fp32, so any order and any precision that is there gives the same bits.  Shows
+    a lane or a column that is out of place."""
+    g = rng(tokens)
+    out, inn = 777, 1300
+    q = torch.randint(-8, 9, (out, 1312), generator=g, device=DEV).float().to(torch.float8_e4m3fn)[:, :inn]
+    x = torch.randint(-8, 9, (tokens, inn), generator=g, device=DEV).to(F16)
+    x[:, ::128] = 8   # the block's largest: its scale is 2^-5, and 8 * 2^5 = 256 is an e4m3 number
+    s = torch.full((7, 11), 127, dtype=torch.uint8, device=DEV)
+    want = torch.from_numpy(np64(x) @ np64(q).T)
+    for scales in (s.view(torch.float8_e8m0fnu), torch.ones((7, 11), device=DEV)):
+        y = B.linear_f8(x, q, scales, out_dtype=F32)
+        assert torch.equal(y.double().cpu(), want)
+    # few enough for 16 bits: sums below 2048
+    q = torch.randint(-1, 2, (out, 1312), generator=g, device=DEV).float().to(torch.float8_e4m3fn)[:, :inn]
+    x = torch.randint(-1, 2, (tokens, inn), generator=g, device=DEV).to(F16)
+    want = torch.from_numpy(np64(x) @ np64(q).T)
+    for scales in (s.view(torch.float8_e8m0fnu), torch.ones((7, 11), device=DEV)):
+        assert torch.equal(B.linear_f8(x, q, scales).double().cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("tokens,out,inn", [(1, 256, 640), (7, 100, 333), (80, 300, 1000), (260, 512, 1024)])
+def test_gated(tokens, out, inn, dtype):
+    """The gate's exponential and quotient may be off by some 2^-22, which turns a rounding to 8 bits over (1/16 of a value) where the value lies that
+    near a tie: four columns of 1000 or fewer may do so, which is what is allowed beyond the bound of the product."""
+    g = rng(tokens + out)
+    q, s = weight(g, out, inn, "e8m0")
+    x = acts(g, tokens, 2 * inn, dtype)
+    x8, _ = O.quantise_rows(O.gated(np64(x)))
+    w = O.weight_values(np64(q), np64(s))
+    want = x8 @ w.T
+    flips = 4 / 16 * np.abs(x8).max(axis=1)[:, None] * np.abs(w).max(axis=1)[None, :]
+    y = B.linear_f8(x, q, s, gated=True, out_dtype=F32)
+    err = np.abs(np64(y) - want)
+    bound = tolerance(x8, w, F32, want)
+    assert (err <= bound + flips).all()
+    assert (err <= bound).mean() > 0.9
+    # quantised before is the same
+    rows = B.quantise_f8(x, gated=True)
+    assert torch.equal(B.linear_f8(rows, q, s, out_dtype=F32), y)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["f16", "bf16", "f32"])
+@pytest.mark.parametrize("n,width", [(1, 1), (1, 128), (3, 127), (2, 129), (5, 512), (4, 513), (9, 1000), (64, 4096)])
+def test_quantise(n, width, dtype):
+    """bit for bit: with powers of two for scales the rounding to 8 bits is the only one"""
+    g = rng(n * width)
+    x = acts(g, n, width, dtype)
+    x *= torch.exp2(torch.randint(-10, 10, (n, 1), generator=g, device=DEV).float()).to(dtype)
+    x[0, 0] = 448.0          # the edge of a power of two
+    if width > 200:
+        x[-1, :128] = 0      # a block of zeros
+    r = B.quantise_f8(x)
+    want, e = O.quantise_rows(np64(x))
+    kb = e.shape[1]
+    assert np.array_equal(r.scales[:, :kb].cpu().numpy().astype(int) - 127, e)
+    assert np.array_equal(np64(r.values()), want)
+    assert not r.q.view(torch.uint8)[:, width:].any()
+
+
+def test_quantise_ties_subnormals_and_every_value():
+    values = torch.arange(0, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    mids = (values[1:] + values[:-1]) / 2
+    x = torch.cat([values, mids, -values, -mids])
+    x = torch.nn.functional.pad(x.to(DEV), (0, 512 - x.numel())).view(4, 128).clone()
+    x[:, 0] = 448
+    want, e = O.quantise_rows(np64(x))
+    assert (e == 0).all()
+    assert np.array_equal(np64(B.quantise_f8(x).values()), want)
+    # far down: the scale stops at 2^-126
+    tiny = torch.full((1, 128), 2.0**-140, device=DEV)
+    tiny[0, 1] = 2.0**-133
+    r = B.quantise_f8(tiny)
+    assert r.scales[0, 0] == 1
+    assert np.array_equal(np64(r.q), O.round_e4m3(np64(tiny) * 2.0**126))
+    # and at the top: the scale is 2^120, 448 * 2^119 is less
+    top = torch.full((1, 128), torch.finfo(F32).max, device=DEV)
+    r = B.quantise_f8(top)
+    assert r.scales[0, 0] == 247 and np.array_equal(np64(r.q), O.round_e4m3(np64(top) * 2.0**-120))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("tokens", [3, 40, 200])
+def test_a_row_with_a_number_that_is_none_spoils_itself_alone(bad, tokens):
+    g = rng(4)
+    q, s = weight(g, 200, 700, "e8m0")
+    x = acts(g, tokens, 700, F16)
+    clean = B.linear_f8(x, q, s)
+    x[1, 333] = bad
+    y = B.linear_f8(x, q, s)
+    assert y[1].isnan().all()
+    keep = [i for i in range(tokens) if i != 1]
+    assert torch.equal(y[keep], clean[keep])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["f16", "bf16", "f32"])
+@pytest.mark.parametrize("out,inn", [(1, 1), (128, 128), (100, 200), (257, 1000), (512, 4096)])
+def test_quantise_weight(out, inn, dtype):
+    g = rng(out)
+    w = (torch.randn((out, inn), generator=g, device=DEV) * 0.02).to(dtype)
+    q, s = B.quantise_weight_f8(w)
+    want, e = O.quantise_weight(np64(w))
+    assert np.array_equal(s.view(torch.uint8).cpu().numpy().astype(int) - 127, e)
+    assert np.array_equal(O.weight_values(np64(q), np.ldexp(1.0, e)), want)
+    assert q.stride(0) % 128 == 0
+    # a layer of experts, one of them with rows apart
+    many = torch.zeros((2, out, inn + 3), dtype=dtype, device=DEV)[:, :, :inn]
+    many[1] = w
+    q2, s2 = B.quantise_weight_f8(many)
+    assert torch.equal(q2[1].view(torch.uint8), q.view(torch.uint8)) and torch.equal(s2[1].view(torch.uint8), s.view(torch.uint8))
+    assert not q2[0].view(torch.uint8).any() and (s2[0].view(torch.uint8) == 1).all()
+
+
+@pytest.mark.parametrize("tokens", [4, 100])
+def test_strides_and_alignment(tokens):
+    """rows apart, views that begin at odd elements, an output inside a larger one"""
+    g = rng(9)
+    out, inn = 200, 260
+    q, s = weight(g, out, inn, "f32")
+    base = acts(g, tokens, inn + 5, BF16)
+    wide = torch.empty((tokens, out + 7), dtype=BF16, device=DEV).fill_(7)
+    for first in (0, 1, 2):
+        x = base[:, first : first + inn]
+        want = B.linear_f8(x.contiguous(), q, s)
+        assert torch.equal(B.linear_f8(x, q, s), want)
+        y = wide[:, 1 : 1 + out]
+        B.linear_f8(x, q, s, y=y)
+        assert torch.equal(y, want) and (wide[:, 0] == 7).all() and (wide[:, 1 + out :] == 7).all()
+    # rows of the weight further apart than they have to be
+    far = torch.full((out, 512), 0x7F, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    far.view(torch.uint8)[:, :inn] = q.view(torch.uint8)
+    assert torch.equal(B.linear_f8(base[:, :inn], far[:, :inn], s), B.linear_f8(base[:, :inn], q, s))
+
+
+def test_no_tokens():
+    g = rng(1)
+    q, s = weight(g, 64, 128, "e8m0")
+    y = B.linear_f8(torch.empty((0, 128), dtype=F16, device=DEV), q, s)
+    assert tuple(y.shape) == (0, 64)
+    assert B.quantise_f8(torch.empty((0, 128), device=DEV)).q.shape[0] == 0
+
+
+def test_on_another_stream_and_with_a_workspace():
+    g = rng(2)
+    q, s = weight(g, 512, 1024, "e8m0")
+    x = acts(g, 33, 1024, F16)
+    want = B.linear_f8(x, q, s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = B.linear_f8(x, q, s, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, want)
+    ws = torch.full((B.f8_workspace_bytes(33, 1024, 33, 512),), 0xFF, dtype=torch.uint8, device=DEV)
+    assert torch.equal(B.linear_f8(x, q, s, workspace=ws), want)
+
+
+def test_graph_replays():
+    g = rng(3)
+    q, s = weight(g, 640, 1000, "f32")
+    x = acts(g, 70, 1000, BF16)
+    y = torch.zeros((70, 640), dtype=BF16, device=DEV)
+    ws = torch.empty(B.f8_workspace_bytes(70, 1000, 70, 640), dtype=torch.uint8, device=DEV)
+    B.linear_f8(x, q, s, y=y, workspace=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.linear_f8(x, q, s, y=y, workspace=ws)
+    for i in range(4):
+        x.copy_(acts(rng(50 + i), 70, 1000, BF16))
+        ws.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, B.linear_f8(x, q, s))
+
+
+def test_refusals():
+    g = rng(5)
+    q, s = weight(g, 64, 256, "e8m0")
+    x = acts(g, 2, 256, F16)
+    for call in (
+        lambda: B.linear_f8(x[:, :200], q, s),                                   # another width
+        lambda: B.linear_f8(x, q, s, gated=True),
+        lambda: B.linear_f8(x.double(), q, s),
+        lambda: B.linear_f8(x.t(), q, s),
+        lambda: B.linear_f8(x.cpu(), q, s),
+        lambda: B.linear_f8(x, q.float(), s),
+        lambda: B.linear_f8(x, q, s.float()[:, :1]),                             # a scale for each block
+        lambda: B.linear_f8(x, q, s.view(torch.uint8)),
+        lambda: B.linear_f8(x, q, s, y=torch.empty((2, 63), dtype=F16, device=DEV)),
+        lambda: B.linear_f8(x, q, s, y=torch.empty((2, 64), dtype=F16, device=DEV), out_dtype=F32),
+        lambda: B.quantise_f8(x[:, :255], gated=True),
+    ):
+        with pytest.raises(ValueError):
+            call()
+    odd = torch.zeros((64, 257), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)[:, :256]   # rows 257 bytes apart
+    with pytest.raises(B.BitStackError) as e:
+        B.linear_f8(x, odd, s)
+    assert e.value.code == -4
+    with pytest.raises(B.BitStackError) as e:
+        B.linear_f8(x, q, s, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    assert e.value.code == -6
