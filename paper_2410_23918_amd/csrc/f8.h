@@ -30,7 +30,7 @@ struct F8Params {
     int x_rows, rows;          // rows of x, of y
     int n_tiles;               // tiles of rows (an upper bound where they are grouped)
     int y_dtype, ws_f32;       // ws_f32: fp32 scales
-    int y_vec;                 // four consecutive outputs may be stored at once
+    int y_vec, y_vec16;        // four outputs, or 16 bytes of them, may be stored at once
 };
 
 // float of an element, and back
@@ -87,6 +87,7 @@ hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int ou
                                      unsigned char* s, hipStream_t st);
 hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st);
 hipError_t launch_f8_product(const F8Params& p, int experts, F8Tile* list, const int* offsets, hipStream_t st);
+void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
 // an upper bound on the work list's length, whatever tile the product takes
 size_t f8_worklist_entries(int rows, int experts);
 

@@ -95,6 +95,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     p.y_dtype = y_dtype;
     p.ws_f32 = w->scale_type == BITSTACK_S_F32;
     p.y_vec = ld_y % 4 == 0 && !misaligned(y, 4 * type_size(y_dtype));
+    p.y_vec16 = ld_y * type_size(y_dtype) % 16 == 0 && !misaligned(y, 16);
     const hipError_t e = launch_f8_product(p, w->experts, reinterpret_cast<F8Tile*>(ws + at.list), offsets, st);
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }

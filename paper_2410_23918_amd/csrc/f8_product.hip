@@ -14,6 +14,8 @@
 // operands agree, since they share the scale.  D: lane l holds rows 4 (l / 16) .. + 3 of the weight and token l % 16.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "f8.h"
 #include "kparams.h"
 
@@ -63,6 +65,12 @@ __device__ __forceinline__ void store4(const F8Params& p, int row, int n, const 
         else
             for (int i = 0; i < 4 && n + i < p.out; ++i) y[i] = h[i];
     }
+}
+
+template <class E>
+__device__ __forceinline__ v2u pack4(const v4f& v) {
+    typedef E v4e __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(v2u, v4e{E(v[0]), E(v[1]), E(v[2]), E(v[3])});
 }
 
 // How a tile is multiplied: the scales of the weight are powers of two, or fp32 numbers; or the outputs are fp32 (either scales)
@@ -242,6 +250,225 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
     }
 }
 
+// Larger tiles: eight wavefronts, WR x WT, each with 16 FR rows of the weight x 16 FT tokens; both operands go through LDS, a block of columns (a
+// step) at a time, in a ring that the loads fill directly.
+//   The two wavefronts of a SIMD take turns: while one reads its fragments of a step from LDS the other one multiplies, and a barrier ends each
+// phase.  Wavefronts 0-3 read step b in phase 2 b and multiply it in 2 b + 1, wavefronts 4-7 one phase later.  So the buffer of step b is free
+// after phase 2 b + 1, and the step RING further on is requested into it at the beginning of the next one.
+//   LDS: a row's 128 bytes, its 16-byte piece c at position c ^ f(row), f such that the sixteen rows that a fragment's read touches at a time
+// meet every bank once.  Row i of the weight's fragment j is row (i / 4) 4 FR + 4 j + i % 4 of the wavefront's tile, so that a lane ends with 4 FR neighbouring
+// outputs of a token.
+//   The activations' scales come with the step, four bytes a token (four steps' scales, of which one is used); the weight's, the same for 128
+// rows, are kept one to a lane for 64 steps.
+template <int FR, int FT, int WR, int WT, int MODE>
+struct F8TileShape {
+    static constexpr int kWaves = 8, kRows = 16 * FR * WR, kToks = 16 * FT * WT;
+    static constexpr int kStep = (kRows + kToks) * 128 + (kToks > 512 ? kToks : 512) * 4;   // bytes, a multiple of 128
+    static constexpr int kRing = 163840 / kStep < 4 ? 163840 / kStep : 4;
+    static constexpr int kSize = MODE == kModeExact ? 4 : 2, kOutLd = kRows * kSize + 16;   // the output tile in LDS
+    static constexpr int kLds = kRing * kStep > kToks * kOutLd ? kRing * kStep : kToks * kOutLd;
+    static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % (8 * kWaves) == 0, "whole loads, one weight scale a wavefront");
+};
+
+template <int FR, int FT, int WR, int WT, int MODE>
+__global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
+    typedef F8TileShape<FR, FT, WR, WT, MODE> S;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave % WR, wt = wave / WR;
+    const bool late = wave >= 4;
+    const int ln = lane & 15, kg = lane >> 4;
+    // ids are dealt round-robin to the 8 XCDs, whose L2s each fetch what their tiles read: every fourth row tile x every second token tile
+    const int nrt = (p.out + S::kRows - 1) / S::kRows, per_row = (p.n_tiles + 1) / 2;
+    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3;
+    const int rt = (xcd >> 1) + 4 * (place / per_row), tt = (xcd & 1) + 2 * (place % per_row);
+    if (rt >= nrt || tt >= p.n_tiles) return;
+    F8Tile t = {0, tt * S::kToks, min(S::kToks, p.rows - tt * S::kToks), 0};
+    if (p.tiles) t = p.tiles[tt];
+    const int expert = __builtin_amdgcn_readfirstlane(t.expert), row0 = __builtin_amdgcn_readfirstlane(t.row0),
+              rows = __builtin_amdgcn_readfirstlane(t.rows);
+    if (rows <= 0) return;
+    const int n0 = rt * S::kRows;
+
+    v4f acc[FR][FT];
+#pragma unroll
+    for (int j = 0; j < FR; ++j)
+#pragma unroll
+        for (int i = 0; i < FT; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    if (expert >= 0) {
+        const unsigned char* const wbase = p.w + (size_t(expert) * p.out + n0) * p.ldw;
+        const int w_rows = min(S::kRows, p.out - n0);
+        const v4i wrs = buffer_over(wbase, unsigned((w_rows - 1) * p.ldw + (p.in + 15) / 16 * 16));
+        const v4i xrs = buffer_over(p.x, unsigned(p.x_rows) * unsigned(p.kp));
+        const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
+        constexpr int kWLoads = S::kRows / 8 / S::kWaves, kXLoads = S::kToks / 8 / S::kWaves, kSLoads = (S::kToks + 64 * S::kWaves - 1) / (64 * S::kWaves);
+        constexpr int kLoads = kWLoads + kXLoads + kSLoads;
+        auto w_turn = [](int r) { return (r >> 1 & 1) | (r / (4 * FR) & 3) << 1; };
+        unsigned x_off[kXLoads], s_off[kSLoads];
+        // load i of the weight brings rows 8 (wave kWLoads + i) .. + 7 of the tile; past the last row the descriptor ends, and zeros arrive
+        const unsigned w_lane = unsigned(lane >> 3) * unsigned(p.ldw);
+        const unsigned w_load = unsigned(8 * wave * kWLoads) * unsigned(p.ldw), w_next = 8u * unsigned(p.ldw);
+        auto x_row = [&](int r) {   // of token r of the tile
+            int at = row0 + min(r, rows - 1);
+            if (p.index) at = p.index[at];
+            return at;
+        };
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i) {
+            const int r = 8 * (wave * kXLoads + i) + (lane >> 3), at = x_row(r);
+            x_off[i] = unsigned(at) < unsigned(p.x_rows) ? unsigned(at) * unsigned(p.kp) + unsigned((lane & 7) ^ (r >> 1 & 7)) * 16u : 0x80000000u;
+        }
+#pragma unroll
+        for (int i = 0; i < kSLoads; ++i) {   // tokens past the tile's: nothing is there to be read, and the LDS behind is the next step's, not yet asked for
+            const int r = 64 * (wave * kSLoads + i) + lane, at = x_row(r);
+            s_off[i] = unsigned(at) < unsigned(p.x_rows) ? unsigned(at) * unsigned(p.ks) : 0x80000000u;
+        }
+        const unsigned lds0 = lds_address(smem);
+        const int ragged = p.in % 128;
+        int q = 0;   // next step to request; past the last one zeros arrive
+        unsigned q_dst = lds0;
+        auto request = [&]() __attribute__((always_inline)) {
+            const int b = q;
+            const unsigned none = b < p.kb ? 0u : 0x80000000u, col = b < p.kb ? unsigned(b) * 128u : 0u;
+#pragma unroll
+            for (int i = 0; i < kWLoads; ++i) {
+                const int piece = (lane & 7) ^ w_turn(8 * (wave * kWLoads + i) + (lane >> 3));
+                unsigned off = (w_lane + unsigned(piece) * 16u) | none;
+                if (ragged && b == p.kb - 1 && piece * 16 >= ragged) off = 0x80000000u;   // zeros past the last column's piece
+                load_to_lds(wrs, q_dst + unsigned(wave * kWLoads + i) * 1024u, off, col + w_load + unsigned(i) * w_next);
+            }
+#pragma unroll
+            for (int i = 0; i < kXLoads; ++i) load_to_lds(xrs, q_dst + S::kRows * 128u + unsigned(wave * kXLoads + i) * 1024u, x_off[i] | none, col);
+#pragma unroll
+            for (int i = 0; i < kSLoads; ++i)
+                load4_to_lds(xsrs, q_dst + (S::kRows + S::kToks) * 128u + unsigned(wave * kSLoads + i) * 256u, s_off[i] | none, (col >> 7) & ~3u);
+            ++q;
+            q_dst = q_dst == lds0 + (S::kRing - 1) * S::kStep ? lds0 : q_dst + S::kStep;
+        };
+        // fragments: a lane's row has the turn (ln / 2) % 8 in both operands
+        const int wrow = wr * 16 * FR + (ln >> 2) * 4 * FR + (ln & 3), xrow = wt * 16 * FT + ln;
+        const unsigned p0 = unsigned(kg ^ (ln >> 1 & 7)) * 16u;
+        const unsigned w_frag = lds0 + unsigned(wrow) * 128u + p0, x_frag = lds0 + unsigned(S::kRows + xrow) * 128u + p0;
+        const unsigned s_frag = lds0 + (S::kRows + S::kToks) * 128u + xrow * 4u;
+        unsigned r_src = 0;   // of the step to be read next, from lds0
+        auto read_piece = [&](unsigned at) __attribute__((always_inline)) { return join(read_lds<v4i>(at), read_lds<v4i>(at ^ 64u)); };   // pieces kg, kg + 4
+        auto read_w = [&](int j) __attribute__((always_inline)) { return read_piece(w_frag + r_src + j * 512); };
+        auto read_x = [&](int i) __attribute__((always_inline)) { return read_piece(x_frag + r_src + i * 2048); };
+        auto read_s = [&](int i, int b) __attribute__((always_inline)) { return int(read_lds<unsigned char>(s_frag + r_src + i * 64 + (b & 3))); };
+        // the weight's scales of 64 steps, one to a lane
+        const bool s_f32 = MODE == kModeF32 || (MODE == kModeExact && p.ws_f32);
+        const size_t s_row = (size_t(expert) * ((p.out + 127) / 128) + min(n0 + wr * 16 * FR, p.out - 1) / 128) * p.kb;
+        int scales = 0;
+        auto load_scales = [&](int b0) {
+            const int b = min(b0 + lane, p.kb - 1);
+            const int v = s_f32 ? static_cast<const int*>(p.ws)[s_row + b] : static_cast<const unsigned char*>(p.ws)[s_row + b];
+            asm volatile("v_mov_b32 %0, %1" : "=v"(scales) : "v"(v));   // waited for here, not at every step's use
+        };
+        v8i w[FR], x[FT];
+        int xs[FT], sw = 0;
+        auto read = [&](int b) __attribute__((always_inline)) {
+            if (ragged % 16 && b == p.kb - 1 && !late) {
+                // The last block ends inside a 16-byte piece, and the weight's rows may go on with anything: the wavefronts that read first clear the
+                // rows that they read, which are all (the other ones come after a barrier)
+                for (int r = wr * 16 * FR + lane; r < (wr + 1) * 16 * FR; r += 64) {
+                    const unsigned at = lds0 + r_src + unsigned(r) * 128u + unsigned(ragged / 16 ^ w_turn(r)) * 16u;
+                    for (int e = ragged % 16; e < 16; ++e) write_lds<unsigned char>(at + e, 0);
+                }
+                wavefront_lds_order();
+            }
+#pragma unroll
+            for (int i = 0; i < FT; ++i) xs[i] = read_s(i, b);
+#pragma unroll
+            for (int j = 0; j < FR; ++j) w[j] = read_w(j);
+#pragma unroll
+            for (int i = 0; i < FT; ++i) x[i] = read_x(i);
+            if ((b & 63) == 0) load_scales(b);
+            sw = __builtin_amdgcn_readlane(scales, b & 63);
+            r_src = r_src == (S::kRing - 1) * S::kStep ? 0 : r_src + S::kStep;
+        };
+        auto products = [&]() __attribute__((always_inline)) {
+            __builtin_amdgcn_s_setprio(1);
+            multiply<FR, FT, MODE>(acc, w, x, xs, sw, s_f32);
+            __builtin_amdgcn_s_setprio(0);
+        };
+        constexpr int kAhead = (S::kRing - 2) * kLoads;   // loads of later steps that may still be on their way when a step has to be there
+#pragma unroll
+        for (int i = 0; i < S::kRing; ++i) request();
+        loads_barrier<kAhead + kLoads>();   // step 0
+        // (a loop for each side: with branches inside, the compiler moves the products past the barriers)
+        if (!late) {
+            for (int b = 0; b < p.kb; ++b) {
+                if (b) request();   // step b + RING - 1
+                read(b);
+                lds_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                products();
+                __builtin_amdgcn_sched_barrier(0);
+                loads_barrier<kAhead>();   // step b + 1
+            }
+            lds_barrier();
+        } else {
+            loads_barrier<kAhead>();   // step 1
+            for (int b = 0; b < p.kb; ++b) {
+                read(b);
+                loads_barrier<kAhead>();   // step b + 1
+                request();                 // step b + RING
+                __builtin_amdgcn_sched_barrier(0);
+                products();
+                __builtin_amdgcn_sched_barrier(0);
+                lds_barrier();
+            }
+        }
+        loads_barrier<0>();   // nothing may land in LDS any more
+    }
+    // the tile's outputs meet in LDS, token by token, and leave in 16-byte pieces
+    constexpr int kSize = S::kSize, kLd = S::kOutLd;
+    if (expert < 0) __syncthreads();   // (else the last barrier has passed)
+    unsigned char* const mine = smem + (wt * 16 * FT + ln) * kLd + (wr * 16 * FR + kg * 4 * FR) * kSize;
+    auto put = [&](auto turn) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FT; ++i)
+#pragma unroll
+            for (int j = 0; j < FR; ++j) turn(acc[j][i], mine + i * 16 * kLd + j * 4 * kSize);
+    };
+    if constexpr (MODE == kModeExact) put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v4f*>(to) = v; });
+    else if (p.y_dtype == BITSTACK_T_F16) put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v2u*>(to) = pack4<_Float16>(v); });
+    else put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v2u*>(to) = pack4<__bf16>(v); });
+    __syncthreads();
+    constexpr int kPieces = S::kRows * kSize / 16, kEach = 16 / kSize;
+    for (int k = tid; k < S::kToks * kPieces; k += 64 * S::kWaves) {
+        const int tok = k / kPieces, piece = k % kPieces, n = n0 + piece * kEach;
+        if (tok >= rows) break;
+        if (n >= p.out) continue;
+        const unsigned char* const from = smem + tok * kLd + piece * 16;
+        unsigned char* const y = static_cast<unsigned char*>(p.y) + (size_t(row0 + tok) * p.ldy + n) * kSize;
+        if (p.y_vec16 && n + kEach <= p.out) {
+            *reinterpret_cast<v4i*>(y) = *reinterpret_cast<const v4i*>(from);
+        } else {
+            for (int e = 0; e < kEach && n + e < p.out; ++e) {
+                if constexpr (kSize == 4) reinterpret_cast<float*>(y)[e] = reinterpret_cast<const float*>(from)[e];
+                else reinterpret_cast<unsigned short*>(y)[e] = reinterpret_cast<const unsigned short*>(from)[e];
+            }
+        }
+    }
+}
+
+template <int FR, int FT, int WR, int WT, int MODE>
+static hipError_t tiles(const F8Params& p, hipStream_t st) {
+    typedef F8TileShape<FR, FT, WR, WT, MODE> S;
+    static std::atomic<bool> attr_set{false};   // setting the attribute twice is harmless
+    if (!attr_set) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_f8_tile<FR, FT, WR, WT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+        if (e != hipSuccess) return e;
+        attr_set = true;
+    }
+    const unsigned nrt = unsigned((p.out + S::kRows - 1) / S::kRows);
+    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE>), dim3(8 * ((nrt + 3) / 4) * unsigned((p.n_tiles + 1) / 2)), dim3(512), S::kLds, st, p);
+    return hipGetLastError();
+}
+
 template <int FR, int FT, int DEPTH>
 static void slices(const F8Params& p, hipStream_t st) {
     const int nrt = (p.out + 16 * FR - 1) / (16 * FR);
@@ -251,11 +478,26 @@ static void slices(const F8Params& p, hipStream_t st) {
     else hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, kModeE8M0>), grid, dim3(512), 0, st, p);
 }
 
+static std::atomic<int> g_forced{0};   // measurement hook: 0 = the choice below
+void f8_force_kernel(int kernel) { g_forced = kernel; }
+
 size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2 + size_t(rows < experts ? rows : experts); }
+
+enum F8Kernel { kSlices16 = 16, kSlices64 = 64, kTile128 = 128, kTile256 = 256 };   // rows of y in a tile
+
+template <int FR, int FT, int WR, int WT>
+static hipError_t tiles_of(const F8Params& p, hipStream_t st) {
+    if (p.ws_f32) return tiles<FR, FT, WR, WT, kModeF32>(p, st);
+    return tiles<FR, FT, WR, WT, kModeE8M0>(p, st);
+}
 
 hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, const int* offsets, hipStream_t st) {
     F8Params p = args;
-    const int tile_rows = p.rows <= 16 ? 16 : 64;
+    const bool exact = p.y_dtype == BITSTACK_T_F32;
+    int kernel = g_forced.load();
+    if (kernel != kSlices16 && kernel != kSlices64 && kernel != kTile128 && kernel != kTile256) kernel = p.rows <= 16 ? kSlices16 : p.rows <= 256 ? kSlices64 : p.rows <= 512 ? kTile128 : kTile256;
+    if (exact && kernel == kTile256) kernel = kTile128;
+    const int tile_rows = kernel;
     p.n_tiles = (p.rows + tile_rows - 1) / tile_rows;
     if (offsets) {
         // every group's rows, rounded up to tiles, and those of the rows past the last group
@@ -264,9 +506,12 @@ hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, co
         const hipError_t e = launch_f8_worklist(offsets, experts, p.rows, tile_rows, list, p.n_tiles, st);
         if (e != hipSuccess) return e;
     }
-    if (tile_rows == 16) slices<1, 1, 4>(p, st);
-    else slices<4, 4, 1>(p, st);
-    return hipGetLastError();
+    switch (kernel) {
+        case kSlices16: slices<1, 1, 4>(p, st); return hipGetLastError();
+        case kSlices64: slices<4, 4, 1>(p, st); return hipGetLastError();
+        case kTile128: return exact ? tiles<4, 4, 4, 2, kModeExact>(p, st) : tiles_of<4, 4, 4, 2>(p, st);
+        default: return tiles_of<8, 4, 2, 4>(p, st);
+    }
 }
 
 }  // namespace bitstack
