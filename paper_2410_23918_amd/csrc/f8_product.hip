@@ -14,6 +14,7 @@
 // operands agree, since they share the scale.  D: lane l holds rows 4 (l / 16) .. + 3 of the weight and token l % 16.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "f8.h"
@@ -104,39 +105,49 @@ __device__ __forceinline__ v4f mfma_halves(const Halves& w, const Halves& x) {
     return c;
 }
 
-// acc += a block's products of FR x FT fragments, with its scales (xs: of the lane's token in each fragment; sw: the weight's, in bits).  D's
-// columns are the tokens: a lane's four results have one scale.
-template <int FR, int FT, int MODE>
-__device__ __forceinline__ void multiply(v4f (&acc)[FR][FT], const v8i (&w)[FR], const v8i (&x)[FT], const int (&xs)[FT], int sw, bool sw_f32) {
+// acc += a block's products of FR fragments of the weight and one of the activations, with their scales (xs: of the lane's token; sw: the
+// weight's, in bits).  D's columns are the tokens: a lane's four results have one scale.
+template <int FR, int MODE, class Weights>
+__device__ __forceinline__ void multiply(v4f* const (&acc)[FR], const Weights (&w)[FR], const v8i& x, int xs, int sw, bool sw_f32) {
     if constexpr (MODE == kModeExact) {
-        const float f = sw_f32 ? __int_as_float(sw) : scale_of(sw);
-        Halves wh[FR];
+        const float f = sw_f32 ? __int_as_float(sw) : scale_of(sw), g = scale_of(xs);
+        const Halves xh = to_halves(x);
 #pragma unroll
-        for (int j = 0; j < FR; ++j) wh[j] = to_halves(w[j]);
+        for (int j = 0; j < FR; ++j) {
+            const v4f part = mfma_halves(w[j], xh);
 #pragma unroll
-        for (int i = 0; i < FT; ++i) {
-            const Halves xh = to_halves(x[i]);
-            const float g = scale_of(xs[i]);
-#pragma unroll
-            for (int j = 0; j < FR; ++j) {
-                const v4f part = mfma_halves(wh[j], xh);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[j][i][v] = fmaf(part[v] * g, f, acc[j][i][v]);
-            }
+            for (int v = 0; v < 4; ++v) (*acc[j])[v] = fmaf(part[v] * g, f, (*acc[j])[v]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < FT; ++i)
+        for (int j = 0; j < FR; ++j) {
+            if constexpr (MODE == kModeF32) {
+                const v4f part = mfma_f8(w[j], x, v4f{0.0f, 0.0f, 0.0f, 0.0f}, kOne, xs);
 #pragma unroll
-            for (int j = 0; j < FR; ++j) {
-                if constexpr (MODE == kModeF32) {
-                    const v4f part = mfma_f8(w[j], x[i], v4f{0.0f, 0.0f, 0.0f, 0.0f}, kOne, xs[i]);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[j][i][v] = fmaf(part[v], __int_as_float(sw), acc[j][i][v]);
-                } else {
-                    acc[j][i] = mfma_f8(w[j], x[i], acc[j][i], sw, xs[i]);
-                }
+                for (int v = 0; v < 4; ++v) (*acc[j])[v] = fmaf(part[v], __int_as_float(sw), (*acc[j])[v]);
+            } else {
+                *acc[j] = mfma_f8(w[j], x, *acc[j], sw, xs);
             }
+        }
+    }
+}
+// the same for FT fragments of the activations; after(i) follows those of fragment i
+template <int FR, int FT, int MODE, class After>
+__device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[FR], const v8i (&x)[FT], const int (&xs)[FT], int sw, bool sw_f32, After after) {
+    typedef typename std::conditional<MODE == kModeExact, Halves, v8i>::type Weights;
+    Weights f[FR];
+#pragma unroll
+    for (int j = 0; j < FR; ++j) {
+        if constexpr (MODE == kModeExact) f[j] = to_halves(w[j]);
+        else f[j] = w[j];
+    }
+#pragma unroll
+    for (int i = 0; i < FT; ++i) {
+        v4f* to[FR];
+#pragma unroll
+        for (int j = 0; j < FR; ++j) to[j] = &acc[j][i];
+        multiply<FR, MODE>(to, f, x[i], xs[i], sw, sw_f32);
+        after(i);
     }
 }
 
@@ -223,7 +234,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
             for (int j = 0; j < FR; ++j) w[j] = join(s.w[j][0], s.w[j][1]);
 #pragma unroll
             for (int i = 0; i < FT; ++i) x[i] = join(s.x[i][0], s.x[i][1]);
-            multiply<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32);
+            multiply_all<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32, [](int) {});
         };
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) load(st[d], wave + 8 * d);
@@ -264,13 +275,13 @@ template <int FR, int FT, int WR, int WT, int MODE>
 struct F8TileShape {
     static constexpr int kWaves = 8, kRows = 16 * FR * WR, kToks = 16 * FT * WT;
     static constexpr int kStep = (kRows + kToks) * 128 + (kToks > 512 ? kToks : 512) * 4;   // bytes, a multiple of 128
-    static constexpr int kRing = 163840 / kStep < 4 ? 163840 / kStep : 4;
+    static constexpr int kRing = (163840 - 256) / kStep < 4 ? (163840 - 256) / kStep : 4;
     static constexpr int kSize = MODE == kModeExact ? 4 : 2, kOutLd = kRows * kSize + 16;   // the output tile in LDS
-    static constexpr int kLds = kRing * kStep > kToks * kOutLd ? kRing * kStep : kToks * kOutLd;
+    static constexpr int kRingLds = kRing * kStep + 256, kLds = kRingLds > kToks * kOutLd ? kRingLds : kToks * kOutLd;
     static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % (8 * kWaves) == 0, "whole loads, one weight scale a wavefront");
 };
 
-template <int FR, int FT, int WR, int WT, int MODE>
+template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
 __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     typedef F8TileShape<FR, FT, WR, WT, MODE> S;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -304,7 +315,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         const v4i xrs = buffer_over(p.x, unsigned(p.x_rows) * unsigned(p.kp));
         const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
         constexpr int kWLoads = S::kRows / 8 / S::kWaves, kXLoads = S::kToks / 8 / S::kWaves, kSLoads = (S::kToks + 64 * S::kWaves - 1) / (64 * S::kWaves);
-        constexpr int kLoads = kWLoads + kXLoads + kSLoads;
+        constexpr int kLoads = kWLoads + kXLoads + kSLoads + (TOUCH ? 1 : 0);
         auto w_turn = [](int r) { return (r >> 1 & 1) | (r / (4 * FR) & 3) << 1; };
         unsigned x_off[kXLoads], s_off[kSLoads];
         // load i of the weight brings rows 8 (wave kWLoads + i) .. + 7 of the tile; past the last row the descriptor ends, and zeros arrive
@@ -327,25 +338,54 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         }
         const unsigned lds0 = lds_address(smem);
         const int ragged = p.in % 128;
+        // TOUCH: what is requested has a step and a half to arrive, less than a miss of the L2 takes.  So one of the workgroups that are on an XCD at a time
+        // and read the same rows touches each step's lines kTouch steps ahead (a line of 128 bytes a lane, into 256 bytes of LDS that nobody reads).  28672 x
+        // 8192, 2048 tokens: 460 -> 424 us.  Where all tiles are there at once, or few of them share rows, the touches cost more than
+        // they bring (14336 x 4096, 1024 tokens: 53 -> 56 us; 8 experts of 14336 x 4096, 2048 tokens twice: 325 -> 364).
+        constexpr int kTouch = 4;
+        const bool touch_w = wave * 64 < S::kRows;
+        const int touch_mask = (touch_w ? p.touch_w : p.touch_x) - 1, touch_mine = (touch_w ? place % per_row : place / per_row) & touch_mask;
+        unsigned touch_off = 0x80000000u;
+        if (TOUCH) {
+            if (touch_w) {
+                touch_off = unsigned(64 * wave + lane) * unsigned(p.ldw);
+            } else if (wave * 64 < S::kRows + S::kToks) {
+                const int at = x_row(64 * wave - S::kRows + lane);
+                if (unsigned(at) < unsigned(p.x_rows)) touch_off = unsigned(at) * unsigned(p.kp);
+            }
+        }
         int q = 0;   // next step to request; past the last one zeros arrive
         unsigned q_dst = lds0;
-        auto request = [&]() __attribute__((always_inline)) {
-            const int b = q;
-            const unsigned none = b < p.kb ? 0u : 0x80000000u, col = b < p.kb ? unsigned(b) * 128u : 0u;
+        // part `part` of `parts` of a step's loads
+        auto request = [&](int part, int parts) __attribute__((always_inline)) {
+            const unsigned none = q < p.kb ? 0u : 0x80000000u, col = q < p.kb ? unsigned(q) * 128u : 0u;
 #pragma unroll
             for (int i = 0; i < kWLoads; ++i) {
+                if (i % parts != part) continue;
                 const int piece = (lane & 7) ^ w_turn(8 * (wave * kWLoads + i) + (lane >> 3));
                 unsigned off = (w_lane + unsigned(piece) * 16u) | none;
-                if (ragged && b == p.kb - 1 && piece * 16 >= ragged) off = 0x80000000u;   // zeros past the last column's piece
+                if (ragged && q == p.kb - 1 && piece * 16 >= ragged) off = 0x80000000u;   // zeros past the last column's piece
                 load_to_lds(wrs, q_dst + unsigned(wave * kWLoads + i) * 1024u, off, col + w_load + unsigned(i) * w_next);
             }
 #pragma unroll
-            for (int i = 0; i < kXLoads; ++i) load_to_lds(xrs, q_dst + S::kRows * 128u + unsigned(wave * kXLoads + i) * 1024u, x_off[i] | none, col);
+            for (int i = 0; i < kXLoads; ++i) {
+                if ((kWLoads + i) % parts != part) continue;
+                load_to_lds(xrs, q_dst + S::kRows * 128u + unsigned(wave * kXLoads + i) * 1024u, x_off[i] | none, col);
+            }
 #pragma unroll
-            for (int i = 0; i < kSLoads; ++i)
+            for (int i = 0; i < kSLoads; ++i) {
+                if ((kWLoads + kXLoads + i) % parts != part) continue;
                 load4_to_lds(xsrs, q_dst + (S::kRows + S::kToks) * 128u + unsigned(wave * kSLoads + i) * 256u, s_off[i] | none, (col >> 7) & ~3u);
-            ++q;
-            q_dst = q_dst == lds0 + (S::kRing - 1) * S::kStep ? lds0 : q_dst + S::kStep;
+            }
+            if (part == parts - 1) {
+                if (TOUCH) {
+                    const int b = q + kTouch;
+                    const bool on = b < p.kb && (b & touch_mask) == touch_mine;
+                    load4_to_lds(touch_w ? wrs : xrs, lds0 + S::kRing * S::kStep, on ? touch_off : 0x80000000u, on ? unsigned(b) * 128u : 0u);
+                }
+                ++q;
+                q_dst = q_dst == lds0 + (S::kRing - 1) * S::kStep ? lds0 : q_dst + S::kStep;
+            }
         };
         // fragments: a lane's row has the turn (ln / 2) % 8 in both operands
         const int wrow = wr * 16 * FR + (ln >> 2) * 4 * FR + (ln & 3), xrow = wt * 16 * FT + ln;
@@ -388,23 +428,24 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             sw = __builtin_amdgcn_readlane(scales, b & 63);
             r_src = r_src == (S::kRing - 1) * S::kStep ? 0 : r_src + S::kStep;
         };
-        auto products = [&]() __attribute__((always_inline)) {
+        auto products = [&](auto after) __attribute__((always_inline)) {
             __builtin_amdgcn_s_setprio(1);
-            multiply<FR, FT, MODE>(acc, w, x, xs, sw, s_f32);
+            multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, s_f32, after);
             __builtin_amdgcn_s_setprio(0);
         };
-        constexpr int kAhead = (S::kRing - 2) * kLoads;   // loads of later steps that may still be on their way when a step has to be there
+        // loads that may still be on their way when a step has to be there: those of later steps and its own touch, the last of its loads
+        constexpr int kAhead = (S::kRing - 2) * kLoads + (TOUCH ? 1 : 0);
 #pragma unroll
-        for (int i = 0; i < S::kRing; ++i) request();
+        for (int i = 0; i < S::kRing; ++i) request(0, 1);
         loads_barrier<kAhead + kLoads>();   // step 0
         // (a loop for each side: with branches inside, the compiler moves the products past the barriers)
         if (!late) {
             for (int b = 0; b < p.kb; ++b) {
-                if (b) request();   // step b + RING - 1
                 read(b);
+                if (b) request(0, 1);   // step b + RING - 1
                 lds_barrier();
                 __builtin_amdgcn_sched_barrier(0);
-                products();
+                products([](int) {});
                 __builtin_amdgcn_sched_barrier(0);
                 loads_barrier<kAhead>();   // step b + 1
             }
@@ -414,9 +455,12 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             for (int b = 0; b < p.kb; ++b) {
                 read(b);
                 loads_barrier<kAhead>();   // step b + 1
-                request();                 // step b + RING
                 __builtin_amdgcn_sched_barrier(0);
-                products();
+                products([&](int i) __attribute__((always_inline)) {   // step b + RING, between the products
+                    __builtin_amdgcn_sched_barrier(0);
+                    request(i, FT);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
                 __builtin_amdgcn_sched_barrier(0);
                 lds_barrier();
             }
@@ -455,17 +499,22 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     }
 }
 
-template <int FR, int FT, int WR, int WT, int MODE>
-static hipError_t tiles(const F8Params& p, hipStream_t st) {
+template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
+static hipError_t tiles(F8Params p, hipStream_t st) {
     typedef F8TileShape<FR, FT, WR, WT, MODE> S;
     static std::atomic<bool> attr_set{false};   // setting the attribute twice is harmless
     if (!attr_set) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_f8_tile<FR, FT, WR, WT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
         if (e != hipSuccess) return e;
         attr_set = true;
     }
     const unsigned nrt = unsigned((p.out + S::kRows - 1) / S::kRows);
-    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE>), dim3(8 * ((nrt + 3) / 4) * unsigned((p.n_tiles + 1) / 2)), dim3(512), S::kLds, st, p);
+    // workgroups on an XCD at a time (32) that read the same rows of the weight, of the tokens
+    const int per_row = (p.n_tiles + 1) / 2;
+    auto power = [](int n) { return n >= 8 ? 8 : n >= 4 ? 4 : n >= 2 ? 2 : 1; };
+    p.touch_w = power(std::min(32, per_row));
+    p.touch_x = power(32 / std::min(32, per_row));
+    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), dim3(8 * ((nrt + 3) / 4) * unsigned(per_row)), dim3(512), S::kLds, st, p);
     return hipGetLastError();
 }
 
@@ -485,12 +534,6 @@ size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2
 
 enum F8Kernel { kSlices16 = 16, kSlices64 = 64, kTile128 = 128, kTile256 = 256 };   // rows of y in a tile
 
-template <int FR, int FT, int WR, int WT>
-static hipError_t tiles_of(const F8Params& p, hipStream_t st) {
-    if (p.ws_f32) return tiles<FR, FT, WR, WT, kModeF32>(p, st);
-    return tiles<FR, FT, WR, WT, kModeE8M0>(p, st);
-}
-
 hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, const int* offsets, hipStream_t st) {
     F8Params p = args;
     const bool exact = p.y_dtype == BITSTACK_T_F32;
@@ -509,8 +552,15 @@ hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, co
     switch (kernel) {
         case kSlices16: slices<1, 1, 4>(p, st); return hipGetLastError();
         case kSlices64: slices<4, 4, 1>(p, st); return hipGetLastError();
-        case kTile128: return exact ? tiles<4, 4, 4, 2, kModeExact>(p, st) : tiles_of<4, 4, 4, 2>(p, st);
-        default: return tiles_of<8, 4, 2, 4>(p, st);
+        case kTile128:
+            if (exact) return tiles<4, 4, 4, 2, kModeExact, false>(p, st);
+            return p.ws_f32 ? tiles<4, 4, 4, 2, kModeF32, false>(p, st) : tiles<4, 4, 4, 2, kModeE8M0, false>(p, st);
+        default: {
+            // (touching: see the kernel; 256 tiles are all there at once)
+            const bool touch = !offsets && size_t((p.out + 255) / 256) * p.n_tiles > 256;
+            if (p.ws_f32) return touch ? tiles<8, 4, 2, 4, kModeF32, true>(p, st) : tiles<8, 4, 2, 4, kModeF32, false>(p, st);
+            return touch ? tiles<8, 4, 2, 4, kModeE8M0, true>(p, st) : tiles<8, 4, 2, 4, kModeE8M0, false>(p, st);
+        }
     }
 }
 
