@@ -28,6 +28,8 @@ struct F8Params {
     size_t ldw, ldy;
     int out, in, kb, kp, ks;   // kb: blocks of columns, kp = 128 kb, ks = kb rounded up to 4
     int x_rows, rows;          // rows of x, of y
+    float* part;               // partial sums, [slices][rows][out rounded up to 4]
+    int slices, slice_blocks;  // of the columns; blocks in one
     int n_tiles;               // tiles of rows (an upper bound where they are grouped)
     int y_dtype, ws_f32;       // ws_f32: fp32 scales
     int touch_w, touch_x;      // k_f8_tile: how many workgroups share the touching of the weight's lines, of the tokens' (powers of two)
@@ -88,6 +90,11 @@ hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int ou
                                      unsigned char* s, hipStream_t st);
 hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st);
 hipError_t launch_f8_product(const F8Params& p, int experts, F8Tile* list, const int* offsets, hipStream_t st);
+struct F8Plan {
+    int kernel, slices;
+};
+F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact);
+size_t f8_partial_bytes(int rows, int out, int in, int experts);   // for any type of y, grouped or not
 void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
 // an upper bound on the work list's length, whatever tile the product takes
 size_t f8_worklist_entries(int rows, int experts);

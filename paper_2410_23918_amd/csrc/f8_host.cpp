@@ -19,14 +19,15 @@ size_t type_size(int t) { return t == BITSTACK_T_F32 ? 4 : 2; }
 bool columns_ok(int in) { return in >= 1 && in <= kMaxIn; }
 
 struct Workspace {
-    size_t q, scales, list, total;
+    size_t q, scales, list, part, total;
 };
-Workspace workspace_of(int x_rows, int in, int y_rows, int experts, bool quantised) {
+Workspace workspace_of(int x_rows, int in, int y_rows, int out, int experts, bool quantised) {
     Workspace w;
     w.q = 0;
     w.scales = quantised ? 0 : align256(size_t(x_rows) * bitstack_f8_row_bytes(in));
     w.list = quantised ? 0 : w.scales + align256(size_t(x_rows) * bitstack_f8_row_scales(in));
-    w.total = w.list + align256(f8_worklist_entries(y_rows, experts) * sizeof(F8Tile));
+    w.part = w.list + align256(f8_worklist_entries(y_rows, experts) * sizeof(F8Tile));
+    w.total = w.part + align256(f8_partial_bytes(y_rows, out, in, experts));
     return w;
 }
 
@@ -59,8 +60,8 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
     const bool quantised = x->dtype == BITSTACK_T_F8;
-    const Workspace at = workspace_of(x->rows, w->in, y_rows, w->experts, quantised);
-    if (!quantised || offsets) {
+    const Workspace at = workspace_of(x->rows, w->in, y_rows, w->out, w->experts, quantised);
+    if (!quantised || offsets || at.total > at.part) {
         if (!workspace) return BITSTACK_E_NULL;
         if (misaligned(workspace, 256)) return BITSTACK_E_ALIGN;
         if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
@@ -83,6 +84,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     p.ws = w->scales;
     p.y = y;
     p.index = index;
+    p.part = reinterpret_cast<float*>(ws + at.part);
     p.ldw = w->ld;
     p.ldy = ld_y;
     p.out = w->out;
@@ -137,7 +139,7 @@ int bitstack_f8_quantise_weight(const void* w, int w_dtype, size_t ld, int out, 
 size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int experts) {
     if (x_rows < 0 || y_rows < 0 || !columns_ok(in) || out < 1 || out > kMaxOut || experts < 1 || experts > kMaxExperts) return 0;
     if (size_t(x_rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return 0;
-    return workspace_of(x_rows, in, y_rows, experts, false).total;
+    return workspace_of(x_rows, in, y_rows, out, experts, false).total;
 }
 
 int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, void* y, int y_dtype, size_t ld_y,

@@ -291,10 +291,11 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     const bool late = wave >= 4;
     const int ln = lane & 15, kg = lane >> 4;
     // ids are dealt round-robin to the 8 XCDs, whose L2s each fetch what their tiles read: every fourth row tile x every second token tile
-    const int nrt = (p.out + S::kRows - 1) / S::kRows, per_row = (p.n_tiles + 1) / 2;
-    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3;
+    const int nrt = (p.out + S::kRows - 1) / S::kRows, per_row = (p.n_tiles + 1) / 2, per_slice = (nrt + 3) / 4 * per_row;
+    const int xcd = blockIdx.x & 7, slice = (blockIdx.x >> 3) / per_slice, place = (blockIdx.x >> 3) % per_slice;
     const int rt = (xcd >> 1) + 4 * (place / per_row), tt = (xcd & 1) + 2 * (place % per_row);
     if (rt >= nrt || tt >= p.n_tiles) return;
+    const int first = slice * p.slice_blocks, last = min(first + p.slice_blocks, p.kb);   // blocks of columns
     F8Tile t = {0, tt * S::kToks, min(S::kToks, p.rows - tt * S::kToks), 0};
     if (p.tiles) t = p.tiles[tt];
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), row0 = __builtin_amdgcn_readfirstlane(t.row0),
@@ -354,11 +355,11 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
                 if (unsigned(at) < unsigned(p.x_rows)) touch_off = unsigned(at) * unsigned(p.kp);
             }
         }
-        int q = 0;   // next step to request; past the last one zeros arrive
+        int q = first;   // next step to request; past the last one zeros arrive
         unsigned q_dst = lds0;
         // part `part` of `parts` of a step's loads
         auto request = [&](int part, int parts) __attribute__((always_inline)) {
-            const unsigned none = q < p.kb ? 0u : 0x80000000u, col = q < p.kb ? unsigned(q) * 128u : 0u;
+            const unsigned none = q < last ? 0u : 0x80000000u, col = q < last ? unsigned(q) * 128u : 0u;
 #pragma unroll
             for (int i = 0; i < kWLoads; ++i) {
                 if (i % parts != part) continue;
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             if (part == parts - 1) {
                 if (TOUCH) {
                     const int b = q + kTouch;
-                    const bool on = b < p.kb && (b & touch_mask) == touch_mine;
+                    const bool on = b < last && (b & touch_mask) == touch_mine;
                     load4_to_lds(touch_w ? wrs : xrs, lds0 + S::kRing * S::kStep, on ? touch_off : 0x80000000u, on ? unsigned(b) * 128u : 0u);
                 }
                 ++q;
@@ -424,8 +425,8 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             for (int j = 0; j < FR; ++j) w[j] = read_w(j);
 #pragma unroll
             for (int i = 0; i < FT; ++i) x[i] = read_x(i);
-            if ((b & 63) == 0) load_scales(b);
-            sw = __builtin_amdgcn_readlane(scales, b & 63);
+            if ((b - first & 63) == 0) load_scales(b);
+            sw = __builtin_amdgcn_readlane(scales, b - first & 63);
             r_src = r_src == (S::kRing - 1) * S::kStep ? 0 : r_src + S::kStep;
         };
         auto products = [&](auto after) __attribute__((always_inline)) {
@@ -440,9 +441,9 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         loads_barrier<kAhead + kLoads>();   // step 0
         // (a loop for each side: with branches inside, the compiler moves the products past the barriers)
         if (!late) {
-            for (int b = 0; b < p.kb; ++b) {
+            for (int b = first; b < last; ++b) {
                 read(b);
-                if (b) request(0, 1);   // step b + RING - 1
+                if (b > first) request(0, 1);   // step b + RING - 1
                 lds_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 products([](int) {});
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             lds_barrier();
         } else {
             loads_barrier<kAhead>();   // step 1
-            for (int b = 0; b < p.kb; ++b) {
+            for (int b = first; b < last; ++b) {
                 read(b);
                 loads_barrier<kAhead>();   // step b + 1
                 __builtin_amdgcn_sched_barrier(0);
@@ -466,6 +467,19 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             }
         }
         loads_barrier<0>();   // nothing may land in LDS any more
+    }
+    if (p.slices > 1) {   // a partial sum: k_f8_join adds them up
+        const int ld = (p.out + 3) / 4 * 4;
+#pragma unroll
+        for (int i = 0; i < FT; ++i) {
+            const int tok = wt * 16 * FT + 16 * i + ln, n = n0 + wr * 16 * FR + kg * 4 * FR;
+            if (tok >= rows) continue;
+            float* const to = p.part + (size_t(slice) * p.rows + row0 + tok) * ld + n;
+#pragma unroll
+            for (int j = 0; j < FR; ++j)
+                if (n + 4 * j < p.out) *reinterpret_cast<v4f*>(to + 4 * j) = acc[j][i];
+        }
+        return;
     }
     // the tile's outputs meet in LDS, token by token, and leave in 16-byte pieces
     constexpr int kSize = S::kSize, kLd = S::kOutLd;
@@ -499,6 +513,17 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     }
 }
 
+// y from the partial sums of p.slices column slices, [slice][row][out rounded up to 4], added up in order
+__global__ __launch_bounds__(256) void k_f8_join(F8Params p) {
+    const int quads = (p.out + 3) / 4;
+    const size_t at = size_t(blockIdx.x) * 256 + threadIdx.x, each = size_t(p.rows) * quads;
+    if (at >= each) return;
+    const v4f* const from = reinterpret_cast<const v4f*>(p.part) + at;
+    v4f sum = from[0];
+    for (int s = 1; s < p.slices; ++s) sum += from[s * each];
+    store4(p, int(at / quads), int(at % quads) * 4, sum);
+}
+
 template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
 static hipError_t tiles(F8Params p, hipStream_t st) {
     typedef F8TileShape<FR, FT, WR, WT, MODE> S;
@@ -514,7 +539,11 @@ static hipError_t tiles(F8Params p, hipStream_t st) {
     auto power = [](int n) { return n >= 8 ? 8 : n >= 4 ? 4 : n >= 2 ? 2 : 1; };
     p.touch_w = power(std::min(32, per_row));
     p.touch_x = power(32 / std::min(32, per_row));
-    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), dim3(8 * ((nrt + 3) / 4) * unsigned(per_row)), dim3(512), S::kLds, st, p);
+    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), dim3(8 * ((nrt + 3) / 4) * unsigned(per_row * p.slices)), dim3(512), S::kLds, st, p);
+    if (p.slices > 1) {
+        const size_t quads = size_t(p.rows) * ((p.out + 3) / 4);
+        hipLaunchKernelGGL(k_f8_join, dim3(unsigned((quads + 255) / 256)), dim3(256), 0, st, p);
+    }
     return hipGetLastError();
 }
 
@@ -527,20 +556,48 @@ static void slices(const F8Params& p, hipStream_t st) {
     else hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, kModeE8M0>), grid, dim3(512), 0, st, p);
 }
 
-static std::atomic<int> g_forced{0};   // measurement hook: 0 = the choice below
-void f8_force_kernel(int kernel) { g_forced = kernel; }
-
 size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2 + size_t(rows < experts ? rows : experts); }
 
 enum F8Kernel { kSlices16 = 16, kSlices64 = 64, kTile128 = 128, kTile256 = 256 };   // rows of y in a tile
 
+static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * column slices, 0 = the choice below
+void f8_force_kernel(int kernel) { g_forced = kernel; }
+
+// Kernel and column slices of a product, from sizes alone (the workspace holds the partial sums)
+F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact) {
+    const int forced = g_forced.load(), kb = (in + 127) / 128;
+    F8Plan plan{forced % 1024, forced / 1024};
+    if (plan.kernel != kSlices16 && plan.kernel != kSlices64 && plan.kernel != kTile128 && plan.kernel != kTile256) {
+        plan.kernel = rows <= 16 ? kSlices16 : rows <= 64 ? kSlices64 : rows <= 512 ? kTile128 : kTile256;
+        plan.slices = 0;
+    }
+    if (exact && plan.kernel == kTile256) plan.kernel = kTile128;
+    if (plan.kernel < kTile128) plan.slices = 1;
+    if (plan.slices == 0) {
+        const size_t tiles = size_t((out + 255) / 256) * ((rows + plan.kernel - 1) / plan.kernel + (grouped ? std::min(rows, experts) / 2 : 0));
+        plan.slices = int(std::min<size_t>(256 / std::max<size_t>(tiles, 1), kb / 8));
+    }
+    plan.slices = std::max(1, std::min(plan.slices, kb));
+    const int each = (kb + plan.slices - 1) / plan.slices;
+    plan.slices = (kb + each - 1) / each;   // none of them empty
+    return plan;
+}
+size_t f8_partial_bytes(int rows, int out, int in, int experts) {
+    size_t most = 0;
+    for (int k = 0; k < 4; ++k) {
+        const int slices = f8_plan(rows, out, in, experts, k & 1, k >> 1).slices;
+        if (slices > 1) most = std::max(most, size_t(slices) * rows * ((out + 3) / 4 * 4) * 4);
+    }
+    return most;
+}
+
 hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, const int* offsets, hipStream_t st) {
     F8Params p = args;
     const bool exact = p.y_dtype == BITSTACK_T_F32;
-    int kernel = g_forced.load();
-    if (kernel != kSlices16 && kernel != kSlices64 && kernel != kTile128 && kernel != kTile256) kernel = p.rows <= 16 ? kSlices16 : p.rows <= 256 ? kSlices64 : p.rows <= 512 ? kTile128 : kTile256;
-    if (exact && kernel == kTile256) kernel = kTile128;
-    const int tile_rows = kernel;
+    const F8Plan plan = f8_plan(p.rows, p.out, p.in, experts, offsets != nullptr, exact);
+    const int kernel = plan.kernel, tile_rows = kernel;
+    p.slices = plan.slices;
+    p.slice_blocks = (p.kb + plan.slices - 1) / plan.slices;
     p.n_tiles = (p.rows + tile_rows - 1) / tile_rows;
     if (offsets) {
         // every group's rows, rounded up to tiles, and those of the rows past the last group
