@@ -40,13 +40,13 @@ enum { BITSTACK_S_E8M0 = 0, BITSTACK_S_F32 = 1 };
 
 /* ---- into 8 bits */
 
-/* Bytes from one row of 8-bit activations to the next: in, rounded up to 128 (what lies between is zero); and from one
- * row of their scales to the next: ceil(in / 128), rounded up to 4.  0 for an unsupported `in`. */
+/* Bytes from one row of 8-bit activations to the next: in, rounded up to 128 (what lies between is zero); and the scales
+ * of a row: ceil(in / 128), rounded up to 4.  0 for an unsupported `in`. */
 size_t bitstack_f8_row_bytes(int in);
 size_t bitstack_f8_row_scales(int in);
 
 /* x [rows][in] of x_dtype, ld elements from row to row  ->  q [rows][bitstack_f8_row_bytes(in)], 16-byte aligned, and
- * scales [rows][bitstack_f8_row_scales(in)].
+ * scales, 4-byte aligned, four blocks of a row side by side: [bitstack_f8_row_scales(in) / 4][rows][4].
  * gated = 1: x is [rows][2 in], a gate g and a value u side by side, and what is brought to 8 bits is
  * g / (1 + exp(-g)) * u, in fp32.  Several products that read the same activations share one such call. */
 int bitstack_f8_quantise(const void* x, int x_dtype, size_t ld, int rows, int in, int gated, void* q, void* scales,

@@ -19,7 +19,7 @@ struct F8Tile {
 
 struct F8Params {
     const unsigned char* x;    // [x_rows][kp], e4m3, zero past `in`
-    const unsigned char* xs;   // [x_rows][ks] biased exponents
+    const unsigned char* xs;   // [ks / 4][x_rows][4] biased exponents
     const unsigned char* w;    // [experts][out] rows of e4m3, ldw bytes apart
     const void* ws;            // [experts][ceil(out / 128)][kb]
     void* y;

@@ -36,7 +36,7 @@ int check_rows(const bitstack_f8_rows_t& x, int in) {
     if (size_t(x.rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return BITSTACK_E_RANGE;
     if (x.dtype == BITSTACK_T_F8) {
         if (x.rows && (!x.x || !x.scales)) return BITSTACK_E_NULL;
-        if (misaligned(x.x, 16)) return BITSTACK_E_ALIGN;
+        if (misaligned(x.x, 16) || misaligned(x.scales, 4)) return BITSTACK_E_ALIGN;
         return BITSTACK_OK;
     }
     if (!real_type(x.dtype) || (x.gated != 0 && x.gated != 1)) return BITSTACK_E_ARG;
@@ -118,7 +118,7 @@ int bitstack_f8_quantise(const void* x, int x_dtype, size_t ld, int rows, int in
     if (rc) return rc;
     if (rows == 0) return BITSTACK_OK;
     if (!q || !scales) return BITSTACK_E_NULL;
-    if (misaligned(q, 16)) return BITSTACK_E_ALIGN;
+    if (misaligned(q, 16) || misaligned(scales, 4)) return BITSTACK_E_ALIGN;
     const hipError_t e = launch_f8_quantise(x, x_dtype, ld, rows, in, gated != 0, static_cast<unsigned char*>(q),
                                             static_cast<unsigned char*>(scales), static_cast<hipStream_t>(stream));
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);

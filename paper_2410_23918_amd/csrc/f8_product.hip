@@ -196,7 +196,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
             if (p.index) r = p.index[r];
             const bool there = unsigned(r) < unsigned(p.x_rows);
             x_off[i] = there ? unsigned(r) * unsigned(p.kp) + kg * 16 : 0x80000000u;
-            xs_off[i] = there ? unsigned(r) * unsigned(p.ks) : 0x80000000u;
+            xs_off[i] = there ? unsigned(r) * 4u : 0x80000000u;
         }
         struct Stage {
             v4i w[FR][2], x[FT][2];
@@ -216,7 +216,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
             for (int i = 0; i < FT; ++i) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) s.x[i][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int((x_off[i] + col + h * 64) | oob), 0, 0));
-                s.xs[i] = __builtin_amdgcn_raw_buffer_load_b8(xsr, int((xs_off[i] + b) | oob), 0, 0);
+                s.xs[i] = __builtin_amdgcn_raw_buffer_load_b8(xsr, int((xs_off[i] + (b & 3)) | oob), int(in ? unsigned(b >> 2) * unsigned(p.x_rows) * 4u : 0u), 0);
             }
             if (s_f32) s.sw = __builtin_amdgcn_raw_buffer_load_b32(sr, int((unsigned(b) * 4u) | oob), 0, 0);
             else s.sw = __builtin_amdgcn_raw_buffer_load_b8(sr, int(unsigned(b) | oob), 0, 0);
@@ -274,11 +274,11 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
 template <int FR, int FT, int WR, int WT, int MODE>
 struct F8TileShape {
     static constexpr int kWaves = 8, kRows = 16 * FR * WR, kToks = 16 * FT * WT;
-    static constexpr int kStep = (kRows + kToks) * 128 + (kToks > 512 ? kToks : 512) * 4;   // bytes, a multiple of 128
+    static constexpr int kStep = (kRows + kToks) * 128 + 4 * 256;   // bytes, a multiple of 128 (the scales of 4 x 64 tokens)
     static constexpr int kRing = (163840 - 256) / kStep < 4 ? (163840 - 256) / kStep : 4;
     static constexpr int kSize = MODE == kModeExact ? 4 : 2, kOutLd = kRows * kSize + 16;   // the output tile in LDS
     static constexpr int kRingLds = kRing * kStep + 256, kLds = kRingLds > kToks * kOutLd ? kRingLds : kToks * kOutLd;
-    static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % (8 * kWaves) == 0, "whole loads, one weight scale a wavefront");
+    static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % 64 == 0 && kToks <= 256, "whole loads, one weight scale a wavefront, scales for the first four wavefronts");
 };
 
 template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
@@ -315,10 +315,10 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         const v4i wrs = buffer_over(wbase, unsigned((w_rows - 1) * p.ldw + (p.in + 15) / 16 * 16));
         const v4i xrs = buffer_over(p.x, unsigned(p.x_rows) * unsigned(p.kp));
         const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
-        constexpr int kWLoads = S::kRows / 8 / S::kWaves, kXLoads = S::kToks / 8 / S::kWaves, kSLoads = (S::kToks + 64 * S::kWaves - 1) / (64 * S::kWaves);
-        constexpr int kLoads = kWLoads + kXLoads + kSLoads + (TOUCH ? 1 : 0);
+        constexpr int kWLoads = S::kRows / 8 / S::kWaves, kXLoads = S::kToks / 8 / S::kWaves;
+        constexpr int kLoads = kWLoads + kXLoads + (TOUCH ? 1 : 0);   // of a step; one more for those that load scales
         auto w_turn = [](int r) { return (r >> 1 & 1) | (r / (4 * FR) & 3) << 1; };
-        unsigned x_off[kXLoads], s_off[kSLoads];
+        unsigned x_off[kXLoads];
         // load i of the weight brings rows 8 (wave kWLoads + i) .. + 7 of the tile; past the last row the descriptor ends, and zeros arrive
         const unsigned w_lane = unsigned(lane >> 3) * unsigned(p.ldw);
         const unsigned w_load = unsigned(8 * wave * kWLoads) * unsigned(p.ldw), w_next = 8u * unsigned(p.ldw);
@@ -332,11 +332,10 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             const int r = 8 * (wave * kXLoads + i) + (lane >> 3), at = x_row(r);
             x_off[i] = unsigned(at) < unsigned(p.x_rows) ? unsigned(at) * unsigned(p.kp) + unsigned((lane & 7) ^ (r >> 1 & 7)) * 16u : 0x80000000u;
         }
-#pragma unroll
-        for (int i = 0; i < kSLoads; ++i) {   // tokens past the tile's: nothing is there to be read, and the LDS behind is the next step's, not yet asked for
-            const int r = 64 * (wave * kSLoads + i) + lane, at = x_row(r);
-            s_off[i] = unsigned(at) < unsigned(p.x_rows) ? unsigned(at) * unsigned(p.ks) : 0x80000000u;
-        }
+        // The scales of tokens 64 wave .. + 63, a word for four blocks: the first four wavefronts load them
+        const bool s_mine = 64 * wave < S::kToks;
+        const int s_at = s_mine ? x_row(64 * wave + lane) : -1;
+        const unsigned s_off = unsigned(s_at) < unsigned(p.x_rows) ? unsigned(s_at) * 4u : 0x80000000u;
         const unsigned lds0 = lds_address(smem);
         const int ragged = p.in % 128;
         // TOUCH: what is requested has a step and a half to arrive, less than a miss of the L2 takes.  So one of the workgroups that are on an XCD at a time
@@ -357,8 +356,8 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         }
         int q = first;   // next step to request; past the last one zeros arrive
         unsigned q_dst = lds0;
-        // part `part` of `parts` of a step's loads
-        auto request = [&](int part, int parts) __attribute__((always_inline)) {
+        // part `part` of `parts` of a step's loads; scales_too: in the first four wavefronts
+        auto request = [&](bool scales_too, int part, int parts) __attribute__((always_inline)) {
             const unsigned none = q < last ? 0u : 0x80000000u, col = q < last ? unsigned(q) * 128u : 0u;
 #pragma unroll
             for (int i = 0; i < kWLoads; ++i) {
@@ -373,11 +372,8 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
                 if ((kWLoads + i) % parts != part) continue;
                 load_to_lds(xrs, q_dst + S::kRows * 128u + unsigned(wave * kXLoads + i) * 1024u, x_off[i] | none, col);
             }
-#pragma unroll
-            for (int i = 0; i < kSLoads; ++i) {
-                if ((kWLoads + kXLoads + i) % parts != part) continue;
-                load4_to_lds(xsrs, q_dst + (S::kRows + S::kToks) * 128u + unsigned(wave * kSLoads + i) * 256u, s_off[i] | none, (col >> 7) & ~3u);
-            }
+            if (scales_too && part == 0)
+                load4_to_lds(xsrs, q_dst + (S::kRows + S::kToks) * 128u + unsigned(wave) * 256u, s_off | none, q < last ? unsigned(q >> 2) * unsigned(p.x_rows) * 4u : 0u);
             if (part == parts - 1) {
                 if (TOUCH) {
                     const int b = q + kTouch;
@@ -434,16 +430,16 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, s_f32, after);
             __builtin_amdgcn_s_setprio(0);
         };
-        // loads that may still be on their way when a step has to be there: those of later steps and its own touch, the last of its loads
-        constexpr int kAhead = (S::kRing - 2) * kLoads + (TOUCH ? 1 : 0);
-#pragma unroll
-        for (int i = 0; i < S::kRing; ++i) request(0, 1);
-        loads_barrier<kAhead + kLoads>();   // step 0
-        // (a loop for each side: with branches inside, the compiler moves the products past the barriers)
+        // A loop for each side: with branches inside, the compiler moves the products past the barriers.  kAhead: loads that may still be on their way when a
+        // step has to be there, those of later steps and its own touch, the last of its loads.
         if (!late) {
+            constexpr int kAhead = (S::kRing - 2) * (kLoads + 1) + (TOUCH ? 1 : 0);
+#pragma unroll
+            for (int i = 0; i < S::kRing; ++i) request(true, 0, 1);
+            loads_barrier<kAhead + kLoads + 1>();   // step 0
             for (int b = first; b < last; ++b) {
                 read(b);
-                if (b > first) request(0, 1);   // step b + RING - 1
+                if (b > first) request(true, 0, 1);   // step b + RING - 1
                 lds_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 products([](int) {});
@@ -452,14 +448,18 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             }
             lds_barrier();
         } else {
-            loads_barrier<kAhead>();   // step 1
+            constexpr int kAhead = (S::kRing - 2) * kLoads + (TOUCH ? 1 : 0);
+#pragma unroll
+            for (int i = 0; i < S::kRing; ++i) request(false, 0, 1);
+            loads_barrier<kAhead + kLoads>();   // step 0
+            loads_barrier<kAhead>();            // step 1
             for (int b = first; b < last; ++b) {
                 read(b);
                 loads_barrier<kAhead>();   // step b + 1
                 __builtin_amdgcn_sched_barrier(0);
                 products([&](int i) __attribute__((always_inline)) {   // step b + RING, between the products
                     __builtin_amdgcn_sched_barrier(0);
-                    request(i, FT);
+                    request(false, i, FT);
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 __builtin_amdgcn_sched_barrier(0);

@@ -19,23 +19,17 @@ __device__ __forceinline__ unsigned to_f8x4(float a, float b, float c, float d) 
 // |v| as an integer that orders like it, NaN and infinity above all others
 __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row.  Bound by memory: x is read
-// once and q written once, 16 and 8 bytes a lane.
+// Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row, whose scales are one word.
+// Bound by memory: x is read once and q written once, 16 and 8 bytes a lane.
 template <int T, bool GATED>
 __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, int vec, unsigned char* q,
-                                                     unsigned char* s, int kp, int ks) {
-    const int lane16 = threadIdx.x & 15;
+                                                     unsigned* s, int kp) {
+    const int lane = threadIdx.x & 63;
     const int per_row = (kp + 511) / 512;   // wavefronts
     const size_t wave = (size_t(blockIdx.x) * 256 + threadIdx.x) >> 6;
-    const int row = int(wave / per_row);
+    const int row = int(wave / per_row), word = int(wave % per_row);
     if (row >= rows) return;
-    const int block = int(wave % per_row) * 4 + ((threadIdx.x & 63) >> 4);
-    if (block >= ks) return;
-    if (block * kF8Block >= kp) {
-        if (lane16 == 0) s[size_t(row) * ks + block] = 127;   // the scales' padding
-        return;
-    }
-    const int col = block * kF8Block + lane16 * 8;
+    const int col = word * 512 + lane * 8;
     float v[8];
     const typename Elem<T>::type* const from = x + size_t(row) * ld + col;
     load_elems<T, 8>(from, in - col, vec, v);
@@ -59,8 +53,10 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
         const float r = f8_inverse(e);
         bytes = make_uint2(to_f8x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), to_f8x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
     }
-    *reinterpret_cast<uint2*>(q + size_t(row) * kp + col) = bytes;
-    if (lane16 == 0) s[size_t(row) * ks + block] = (unsigned char)e;
+    if (col < kp) *reinterpret_cast<uint2*>(q + size_t(row) * kp + col) = bytes;
+    const unsigned four = unsigned(__builtin_amdgcn_readlane(e, 0)) | unsigned(__builtin_amdgcn_readlane(e, 16)) << 8 |
+                          unsigned(__builtin_amdgcn_readlane(e, 32)) << 16 | unsigned(__builtin_amdgcn_readlane(e, 48)) << 24;
+    if (lane == 0) s[size_t(word) * rows + row] = four;
 }
 
 // A workgroup brings a block of 128 rows x 128 columns to 8 bits: sixteen lanes a row, sixteen rows a pass, the values in registers between
@@ -105,13 +101,14 @@ static bool vector_rows(const void* p, size_t ld, int size) { return reinterpret
 template <int T>
 static void quantise(const void* x, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s, hipStream_t st) {
     typedef typename Elem<T>::type E;
-    const int kp = (in + 127) / 128 * 128, ks = (kp / 128 + 3) / 4 * 4;
+    const int kp = (in + 127) / 128 * 128;
     // the halves of a gated row begin `in` elements apart
     const int vec = vector_rows(x, ld, sizeof(E)) && (!gated || size_t(in) * sizeof(E) % 16 == 0);
     const size_t waves = size_t(rows) * ((kp + 511) / 512);
     const unsigned grid = unsigned((waves + 3) / 4);
-    if (gated) hipLaunchKernelGGL((k_f8_quantise<T, true>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, s, kp, ks);
-    else hipLaunchKernelGGL((k_f8_quantise<T, false>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, s, kp, ks);
+    unsigned* const words = reinterpret_cast<unsigned*>(s);
+    if (gated) hipLaunchKernelGGL((k_f8_quantise<T, true>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp);
+    else hipLaunchKernelGGL((k_f8_quantise<T, false>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp);
 }
 
 hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,

@@ -69,7 +69,7 @@ def _f8_lib():
 
 class F8Rows(NamedTuple):
     """Activations in 8 bits, as quantise_f8 makes them: several products may read them.  q [rows, in rounded up to 128], scales
-    [rows, ceil(in / 128) rounded up to 4], `width` = in."""
+    [blocks / 4, rows, 4] (blocks: ceil(in / 128), rounded up to 4), `width` = in."""
     q: torch.Tensor
     scales: torch.Tensor
     width: int
@@ -77,7 +77,7 @@ class F8Rows(NamedTuple):
     def values(self) -> torch.Tensor:
         """the numbers they stand for, fp32 [rows, width]"""
         n, kb = self.q.shape[0], self.q.shape[1] // 128
-        s = self.scales[:, :kb].view(torch.float8_e8m0fnu).float()
+        s = self.scales.transpose(0, 1).reshape(n, -1)[:, :kb].contiguous().view(torch.float8_e8m0fnu).float()
         return (self.q.float().view(n, kb, 128) * s[:, :, None]).view(n, -1)[:, : self.width]
 
 
@@ -170,7 +170,7 @@ def _fill_rows(x, inn, gated):
         L = _f8_lib()
         _need(x.width == inn, f"x has {x.width} columns, the weight {inn}")
         _need(x.q.dtype is torch.float8_e4m3fn and x.q.is_contiguous() and x.scales.is_contiguous() and x.scales.element_size() == 1
-              and tuple(x.q.shape[1:]) == (L.bitstack_f8_row_bytes(inn),) and tuple(x.scales.shape) == (x.q.shape[0], L.bitstack_f8_row_scales(inn)),
+              and tuple(x.q.shape[1:]) == (L.bitstack_f8_row_bytes(inn),) and tuple(x.scales.shape) == (L.bitstack_f8_row_scales(inn) // 4, x.q.shape[0], 4),
               "x: as quantise_f8 makes it")
         _same_device(x.q.device, x.scales)
         a.x, a.scales, a.ld, a.dtype, a.rows, a.gated = x.q.data_ptr(), x.scales.data_ptr(), 0, T_F8, x.q.shape[0], 0
@@ -241,7 +241,7 @@ def quantise_f8(x, *, gated: bool = False, stream=None) -> F8Rows:
     n, inn = x.shape[0], x.shape[1] // (2 if gated else 1)
     with _On(x.device, stream, (x,)) as on:
         q = torch.empty((n, L.bitstack_f8_row_bytes(inn)), dtype=torch.float8_e4m3fn, device=x.device)
-        s = torch.empty((n, L.bitstack_f8_row_scales(inn)), dtype=torch.uint8, device=x.device)
+        s = torch.empty((L.bitstack_f8_row_scales(inn) // 4, n, 4), dtype=torch.uint8, device=x.device)
         _check(L.bitstack_f8_quantise(x.data_ptr(), t, ld, n, inn, int(gated), q.data_ptr(), s.data_ptr(), on.handle), "bitstack_f8_quantise")
     return F8Rows(q, s, inn)
 

@@ -141,7 +141,7 @@ def test_quantise(n, width, dtype):
     r = B.quantise_f8(x)
     want, e = O.quantise_rows(np64(x))
     kb = e.shape[1]
-    assert np.array_equal(r.scales[:, :kb].cpu().numpy().astype(int) - 127, e)
+    assert np.array_equal(r.scales.transpose(0, 1).reshape(n, -1)[:, :kb].cpu().numpy().astype(int) - 127, e)
     assert np.array_equal(np64(r.values()), want)
     assert not r.q.view(torch.uint8)[:, width:].any()
 
@@ -159,12 +159,12 @@ def test_quantise_ties_subnormals_and_every_value():
     tiny = torch.full((1, 128), 2.0**-140, device=DEV)
     tiny[0, 1] = 2.0**-133
     r = B.quantise_f8(tiny)
-    assert r.scales[0, 0] == 1
+    assert r.scales[0, 0, 0] == 1
     assert np.array_equal(np64(r.q), O.round_e4m3(np64(tiny) * 2.0**126))
     # and at the top: the scale is 2^120, 448 * 2^119 is less
     top = torch.full((1, 128), torch.finfo(F32).max, device=DEV)
     r = B.quantise_f8(top)
-    assert r.scales[0, 0] == 247 and np.array_equal(np64(r.q), O.round_e4m3(np64(top) * 2.0**-120))
+    assert r.scales[0, 0, 0] == 247 and np.array_equal(np64(r.q), O.round_e4m3(np64(top) * 2.0**-120))
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
