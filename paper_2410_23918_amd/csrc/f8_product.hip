@@ -275,7 +275,7 @@ template <int FR, int FT, int WR, int WT, int MODE>
 struct F8TileShape {
     static constexpr int kWaves = 8, kRows = 16 * FR * WR, kToks = 16 * FT * WT;
     static constexpr int kStep = (kRows + kToks) * 128 + 4 * 256;   // bytes, a multiple of 128 (the scales of 4 x 64 tokens)
-    static constexpr int kRing = (163840 - 256) / kStep < 4 ? (163840 - 256) / kStep : 4;
+    static constexpr int kRing = (163840 - 256) / kStep < 6 ? (163840 - 256) / kStep : 6;
     static constexpr int kSize = MODE == kModeExact ? 4 : 2, kOutLd = kRows * kSize + 16;   // the output tile in LDS
     static constexpr int kRingLds = kRing * kStep + 256, kLds = kRingLds > kToks * kOutLd ? kRingLds : kToks * kOutLd;
     static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % 64 == 0 && kToks <= 256, "whole loads, one weight scale a wavefront, scales for the first four wavefronts");
@@ -457,11 +457,9 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
                 read(b);
                 loads_barrier<kAhead>();   // step b + 1
                 __builtin_amdgcn_sched_barrier(0);
-                products([&](int i) __attribute__((always_inline)) {   // step b + RING, between the products
-                    __builtin_amdgcn_sched_barrier(0);
-                    request(false, i, FT);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
+                request(false, 0, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                products([](int) {});
                 __builtin_amdgcn_sched_barrier(0);
                 lds_barrier();
             }
@@ -558,7 +556,8 @@ static void slices(const F8Params& p, hipStream_t st) {
 
 size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2 + size_t(rows < experts ? rows : experts); }
 
-enum F8Kernel { kSlices16 = 16, kSlices64 = 64, kTile128 = 128, kTile256 = 256 };   // rows of y in a tile
+enum F8Kernel { kSlices16 = 16, kSlices64 = 64, kTile64 = 65, kTile128 = 128, kTile128Wide = 129, kTile256 = 256 };
+static int rows_of_tile(int kernel) { return kernel == kTile64 ? 64 : kernel == kTile128Wide ? 128 : kernel; }   // of y
 
 static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * column slices, 0 = the choice below
 void f8_force_kernel(int kernel) { g_forced = kernel; }
@@ -567,14 +566,15 @@ void f8_force_kernel(int kernel) { g_forced = kernel; }
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact) {
     const int forced = g_forced.load(), kb = (in + 127) / 128;
     F8Plan plan{forced % 1024, forced / 1024};
-    if (plan.kernel != kSlices16 && plan.kernel != kSlices64 && plan.kernel != kTile128 && plan.kernel != kTile256) {
+    const int all[] = {kSlices16, kSlices64, kTile64, kTile128, kTile128Wide, kTile256};
+    if (std::find(std::begin(all), std::end(all), plan.kernel) == std::end(all)) {
         plan.kernel = rows <= 16 ? kSlices16 : rows <= 64 ? kSlices64 : rows <= 512 ? kTile128 : kTile256;
         plan.slices = 0;
     }
-    if (exact && plan.kernel == kTile256) plan.kernel = kTile128;
-    if (plan.kernel < kTile128) plan.slices = 1;
+    if (exact && plan.kernel == kTile256) plan.kernel = kTile128Wide;
+    if (plan.kernel <= kSlices64) plan.slices = 1;
     if (plan.slices == 0) {
-        const size_t tiles = size_t((out + 255) / 256) * ((rows + plan.kernel - 1) / plan.kernel + (grouped ? std::min(rows, experts) / 2 : 0));
+        const size_t tiles = size_t((out + 255) / 256) * ((rows + rows_of_tile(plan.kernel) - 1) / rows_of_tile(plan.kernel) + (grouped ? std::min(rows, experts) / 2 : 0));
         plan.slices = int(std::min<size_t>(256 / std::max<size_t>(tiles, 1), kb / 8));
     }
     plan.slices = std::max(1, std::min(plan.slices, kb));
@@ -595,7 +595,7 @@ hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, co
     F8Params p = args;
     const bool exact = p.y_dtype == BITSTACK_T_F32;
     const F8Plan plan = f8_plan(p.rows, p.out, p.in, experts, offsets != nullptr, exact);
-    const int kernel = plan.kernel, tile_rows = kernel;
+    const int kernel = plan.kernel, tile_rows = rows_of_tile(kernel);
     p.slices = plan.slices;
     p.slice_blocks = (p.kb + plan.slices - 1) / plan.slices;
     p.n_tiles = (p.rows + tile_rows - 1) / tile_rows;
@@ -609,7 +609,13 @@ hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, co
     switch (kernel) {
         case kSlices16: slices<1, 1, 4>(p, st); return hipGetLastError();
         case kSlices64: slices<4, 4, 1>(p, st); return hipGetLastError();
+        case kTile64:
+            if (exact) return tiles<2, 2, 4, 2, kModeExact, false>(p, st);
+            return p.ws_f32 ? tiles<2, 2, 4, 2, kModeF32, false>(p, st) : tiles<2, 2, 4, 2, kModeE8M0, false>(p, st);
         case kTile128:
+            if (exact) return tiles<2, 4, 4, 2, kModeExact, false>(p, st);
+            return p.ws_f32 ? tiles<2, 4, 4, 2, kModeF32, false>(p, st) : tiles<2, 4, 4, 2, kModeE8M0, false>(p, st);
+        case kTile128Wide:
             if (exact) return tiles<4, 4, 4, 2, kModeExact, false>(p, st);
             return p.ws_f32 ? tiles<4, 4, 4, 2, kModeF32, false>(p, st) : tiles<4, 4, 4, 2, kModeE8M0, false>(p, st);
         default: {
