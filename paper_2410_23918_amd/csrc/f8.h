@@ -28,7 +28,7 @@ struct F8Params {
     size_t ldw, ldy;
     int out, in, kb, kp, ks;   // kb: blocks of columns, kp = 128 kb, ks = kb rounded up to 4
     int x_rows, rows;          // rows of x, of y
-    float* part;               // partial sums, [slices][rows][out rounded up to 4]
+    float* part;               // partial sums of the column slices
     int slices, slice_blocks;  // of the columns; blocks in one
     int n_tiles;               // tiles of rows (an upper bound where they are grouped)
     int y_dtype, ws_f32;       // ws_f32: fp32 scales
@@ -91,7 +91,8 @@ hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int ou
 hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st);
 hipError_t launch_f8_product(const F8Params& p, int experts, F8Tile* list, const int* offsets, hipStream_t st);
 struct F8Plan {
-    int kernel, slices;
+    int kernel, slices, tile_rows, n_tiles;   // tile_rows: rows of y in a tile
+    size_t part_bytes;                        // partial sums
 };
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact);
 size_t f8_partial_bytes(int rows, int out, int in, int experts);   // for any type of y, grouped or not

@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "f8.h"
 #include "kparams.h"
@@ -466,17 +467,12 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         }
         loads_barrier<0>();   // nothing may land in LDS any more
     }
-    if (p.slices > 1) {   // a partial sum: k_f8_join adds them up
-        const int ld = (p.out + 3) / 4 * 4;
+    if (p.slices > 1) {   // partial sums, as the lanes hold them: k_f8_join adds them up
+        v4f* const to = reinterpret_cast<v4f*>(p.part) + ((size_t(slice) * nrt * p.n_tiles + size_t(rt) * p.n_tiles + tt) * 8 + wave) * (FR * FT * 64) + lane;
 #pragma unroll
-        for (int i = 0; i < FT; ++i) {
-            const int tok = wt * 16 * FT + 16 * i + ln, n = n0 + wr * 16 * FR + kg * 4 * FR;
-            if (tok >= rows) continue;
-            float* const to = p.part + (size_t(slice) * p.rows + row0 + tok) * ld + n;
+        for (int j = 0; j < FR; ++j)
 #pragma unroll
-            for (int j = 0; j < FR; ++j)
-                if (n + 4 * j < p.out) *reinterpret_cast<v4f*>(to + 4 * j) = acc[j][i];
-        }
+            for (int i = 0; i < FT; ++i) to[(j * FT + i) * 64] = acc[j][i];
         return;
     }
     // the tile's outputs meet in LDS, token by token, and leave in 16-byte pieces
@@ -511,15 +507,34 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     }
 }
 
-// y from the partial sums of p.slices column slices, [slice][row][out rounded up to 4], added up in order
+// y from the partial sums of p.slices column slices, added up in order: a wavefront takes what one of k_f8_tile's held of a tile, FR fragments
+// of 4 rows a lane at a time, which are 4 FR neighbouring outputs of a token.
+template <int FR, int FT, int WR, int WT>
 __global__ __launch_bounds__(256) void k_f8_join(F8Params p) {
-    const int quads = (p.out + 3) / 4;
-    const size_t at = size_t(blockIdx.x) * 256 + threadIdx.x, each = size_t(p.rows) * quads;
-    if (at >= each) return;
-    const v4f* const from = reinterpret_cast<const v4f*>(p.part) + at;
-    v4f sum = from[0];
-    for (int s = 1; s < p.slices; ++s) sum += from[s * each];
-    store4(p, int(at / quads), int(at % quads) * 4, sum);
+    const int lane = threadIdx.x & 63, ln = lane & 15, kg = lane >> 4;
+    const unsigned unit = blockIdx.x * 4 + (threadIdx.x >> 6);   // tile, wavefront of it, fragment of the activations
+    const int nrt = (p.out + 16 * FR * WR - 1) / (16 * FR * WR);
+    const unsigned tiles = unsigned(nrt) * unsigned(p.n_tiles);
+    const int i = unit % FT, wave = unit / FT % 8;
+    const unsigned tile = unit / (FT * 8);
+    if (tile >= tiles) return;
+    const int rt = int(tile / p.n_tiles), tt = int(tile % p.n_tiles);
+    constexpr int kToks = 16 * FT * WT;
+    F8Tile t = {0, tt * kToks, min(kToks, p.rows - tt * kToks), 0};
+    if (p.tiles) t = p.tiles[tt];
+    const int tok = wave / WR * 16 * FT + 16 * i + ln, n = rt * 16 * FR * WR + wave % WR * 16 * FR + kg * 4 * FR;
+    if (tok >= t.rows) return;
+    const v4f* from = reinterpret_cast<const v4f*>(p.part) + (size_t(tile) * 8 + wave) * (FR * FT * 64) + i * 64 + lane;
+    v4f sum[FR];
+#pragma unroll
+    for (int j = 0; j < FR; ++j) sum[j] = from[j * FT * 64];
+    for (int s = 1; s < p.slices; ++s) {
+        from += size_t(tiles) * 8 * (FR * FT * 64);
+#pragma unroll
+        for (int j = 0; j < FR; ++j) sum[j] += from[j * FT * 64];
+    }
+#pragma unroll
+    for (int j = 0; j < FR; ++j) store4(p, t.row0 + tok, n + 4 * j, sum[j]);
 }
 
 template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
@@ -539,8 +554,8 @@ static hipError_t tiles(F8Params p, hipStream_t st) {
     p.touch_x = power(32 / std::min(32, per_row));
     hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), dim3(8 * ((nrt + 3) / 4) * unsigned(per_row * p.slices)), dim3(512), S::kLds, st, p);
     if (p.slices > 1) {
-        const size_t quads = size_t(p.rows) * ((p.out + 3) / 4);
-        hipLaunchKernelGGL(k_f8_join, dim3(unsigned((quads + 255) / 256)), dim3(256), 0, st, p);
+        const size_t units = size_t(nrt) * p.n_tiles * 8 * FT;
+        hipLaunchKernelGGL((k_f8_join<FR, FT, WR, WT>), dim3(unsigned((units + 3) / 4)), dim3(256), 0, st, p);
     }
     return hipGetLastError();
 }
@@ -554,60 +569,92 @@ static void slices(const F8Params& p, hipStream_t st) {
     else hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, kModeE8M0>), grid, dim3(512), 0, st, p);
 }
 
-size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2 + size_t(rows < experts ? rows : experts); }
 
-enum F8Kernel { kSlices16 = 16, kSlices64 = 64, kTile64 = 65, kTile128 = 128, kTile128Wide = 129, kTile256 = 256 };
-static int rows_of_tile(int kernel) { return kernel == kTile64 ? 64 : kernel == kTile128Wide ? 128 : kernel; }   // of y
+// Kernels by their tile (rows of the weight x of y): 16 x 16, 64 x 16, 64 x 32, 64 x 64 without LDS, 128 x 64, 128 x 128, 256 x 128, 256 x 256
+enum F8Kernel { kSlices16 = 16, kSlices16Wide = 17, kSlices32 = 32, kSlices64 = 64, kTile64 = 65, kTile128 = 128, kTile128Wide = 129, kTile256 = 256 };
+struct F8KernelShape {
+    int kernel, rows, toks;
+};
+constexpr F8KernelShape kShapes[] = {{kSlices16, 16, 16}, {kSlices16Wide, 64, 16}, {kSlices32, 64, 32}, {kSlices64, 64, 64}, {kTile64, 128, 64}, {kTile128, 128, 128}, {kTile128Wide, 256, 128}, {kTile256, 256, 256}};
 
 static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * column slices, 0 = the choice below
 void f8_force_kernel(int kernel) { g_forced = kernel; }
 
+// Duration in microseconds, from timings of 30 shapes (1 to 2048 rows, 512 to 28672 x 1024 to 14336)
+static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, int kb, int experts, bool grouped, bool exact) {
+    // tiles of y's rows that have any: a group fills its last one by half, in the mean
+    const int groups = grouped ? std::min(rows, experts) : 1;
+    const double mt = grouped ? std::max<double>(groups, double(rows) / k.toks + 0.5 * groups) : (rows + k.toks - 1) / k.toks;
+    const double tiles = mt * ((out + k.rows - 1) / k.rows), rounds = std::ceil(tiles * slices / 256);
+    // the weights once, from memory
+    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.toks == 16 ? 4.7e6 : k.toks == 32 ? 4.2e6 : 3.6e6);
+    const double passes = (kb + 7) / 8, whole = std::floor(tiles / 1024), rest = (tiles - 1024 * whole) / 256;
+    double us;
+    if (k.kernel == kSlices16) {   // up to four workgroups on a compute unit
+        us = 3.5 + passes * (whole * 4.1 + (rest > 0 ? 0.3 + 0.95 * rest : 0.0));
+    } else if (k.kernel == kSlices16Wide || k.kernel == kSlices32) {   // two
+        const double more = k.toks == 16 ? (exact ? 3.0 : 2.4) : (exact ? 3.8 : 3.3);
+        us = 4.0 + passes * std::max(k.toks == 16 ? 1.9 : 2.1, 0.9 + more * tiles / 256);
+    } else if (k.kernel == kSlices64) {
+        us = 4.0 + rounds * passes * (exact ? 5.2 : 4.2);
+    } else {
+        const double step = k.kernel == kTile64 ? (exact ? 0.9 : 0.56) : k.kernel == kTile128 ? (exact ? 1.3 : 0.72) : k.kernel == kTile128Wide ? 1.1 : 1.7;
+        us = 4.5 + rounds * ((kb + slices - 1) / slices) * step;
+    }
+    return std::max(us, stream) + (slices > 1 ? 3.5 + slices * tiles * k.rows * k.toks * 8 / 4e6 : 0.0);
+}
+
 // Kernel and column slices of a product, from sizes alone (the workspace holds the partial sums)
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact) {
     const int forced = g_forced.load(), kb = (in + 127) / 128;
-    F8Plan plan{forced % 1024, forced / 1024};
-    const int all[] = {kSlices16, kSlices64, kTile64, kTile128, kTile128Wide, kTile256};
-    if (std::find(std::begin(all), std::end(all), plan.kernel) == std::end(all)) {
-        plan.kernel = rows <= 16 ? kSlices16 : rows <= 64 ? kSlices64 : rows <= 512 ? kTile128 : kTile256;
-        plan.slices = 0;
+    F8Plan plan{kShapes[0].kernel, 1, 0, 0, 0};
+    double best = 1e30;
+    for (const F8KernelShape& k : kShapes) {
+        if (exact && k.kernel >= kTile128Wide) continue;   // the operands as fp16 leave no registers for its sums
+        for (int slices : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (forced ? k.kernel != forced % 1024 || slices > 1 : slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
+            const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact);
+            if (us >= best) continue;
+            best = us;
+            plan = {k.kernel, slices, k.toks, 0, 0};
+        }
     }
-    if (exact && plan.kernel == kTile256) plan.kernel = kTile128Wide;
-    if (plan.kernel <= kSlices64) plan.slices = 1;
-    if (plan.slices == 0) {
-        const size_t tiles = size_t((out + 255) / 256) * ((rows + rows_of_tile(plan.kernel) - 1) / rows_of_tile(plan.kernel) + (grouped ? std::min(rows, experts) / 2 : 0));
-        plan.slices = int(std::min<size_t>(256 / std::max<size_t>(tiles, 1), kb / 8));
-    }
-    plan.slices = std::max(1, std::min(plan.slices, kb));
+    if (forced && forced % 1024 == plan.kernel && plan.kernel > kSlices64) plan.slices = std::max(1, std::min(forced / 1024, kb));
     const int each = (kb + plan.slices - 1) / plan.slices;
     plan.slices = (kb + each - 1) / each;   // none of them empty
+    plan.tile_rows = kShapes[0].toks;
+    for (const F8KernelShape& k : kShapes)
+        if (k.kernel == plan.kernel) {
+            plan.tile_rows = k.toks;
+            // every group's rows, rounded up to tiles, and those of the rows past the last group
+            plan.n_tiles = grouped ? rows / k.toks + 1 + std::min(rows, experts) : (rows + k.toks - 1) / k.toks;
+            if (plan.slices > 1) plan.part_bytes = size_t(plan.slices) * ((out + k.rows - 1) / k.rows) * plan.n_tiles * (k.rows * k.toks * 4);
+        }
     return plan;
 }
 size_t f8_partial_bytes(int rows, int out, int in, int experts) {
     size_t most = 0;
-    for (int k = 0; k < 4; ++k) {
-        const int slices = f8_plan(rows, out, in, experts, k & 1, k >> 1).slices;
-        if (slices > 1) most = std::max(most, size_t(slices) * rows * ((out + 3) / 4 * 4) * 4);
-    }
+    for (int k = 0; k < 4; ++k) most = std::max(most, f8_plan(rows, out, in, experts, k & 1, k >> 1).part_bytes);
     return most;
 }
+size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2 + size_t(rows < experts ? rows : experts); }
 
 hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, const int* offsets, hipStream_t st) {
     F8Params p = args;
     const bool exact = p.y_dtype == BITSTACK_T_F32;
     const F8Plan plan = f8_plan(p.rows, p.out, p.in, experts, offsets != nullptr, exact);
-    const int kernel = plan.kernel, tile_rows = rows_of_tile(kernel);
     p.slices = plan.slices;
     p.slice_blocks = (p.kb + plan.slices - 1) / plan.slices;
-    p.n_tiles = (p.rows + tile_rows - 1) / tile_rows;
+    p.n_tiles = plan.n_tiles;
     if (offsets) {
-        // every group's rows, rounded up to tiles, and those of the rows past the last group
-        p.n_tiles = p.rows / tile_rows + 1 + (p.rows < experts ? p.rows : experts);
         p.tiles = list;
-        const hipError_t e = launch_f8_worklist(offsets, experts, p.rows, tile_rows, list, p.n_tiles, st);
+        const hipError_t e = launch_f8_worklist(offsets, experts, p.rows, plan.tile_rows, list, p.n_tiles, st);
         if (e != hipSuccess) return e;
     }
-    switch (kernel) {
-        case kSlices16: slices<1, 1, 4>(p, st); return hipGetLastError();
+    switch (plan.kernel) {
+        case kSlices16: slices<1, 1, 2>(p, st); return hipGetLastError();
+        case kSlices16Wide: slices<4, 1, 1>(p, st); return hipGetLastError();
+        case kSlices32: slices<4, 2, 1>(p, st); return hipGetLastError();
         case kSlices64: slices<4, 4, 1>(p, st); return hipGetLastError();
         case kTile64:
             if (exact) return tiles<2, 2, 4, 2, kModeExact, false>(p, st);
@@ -616,7 +663,6 @@ hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, co
             if (exact) return tiles<2, 4, 4, 2, kModeExact, false>(p, st);
             return p.ws_f32 ? tiles<2, 4, 4, 2, kModeF32, false>(p, st) : tiles<2, 4, 4, 2, kModeE8M0, false>(p, st);
         case kTile128Wide:
-            if (exact) return tiles<4, 4, 4, 2, kModeExact, false>(p, st);
             return p.ws_f32 ? tiles<4, 4, 4, 2, kModeF32, false>(p, st) : tiles<4, 4, 4, 2, kModeE8M0, false>(p, st);
         default: {
             // (touching: see the kernel; 256 tiles are all there at once)

@@ -9,7 +9,7 @@ from test_gpu_experts import check_grouped
 from test_gpu_f8 import BF16, DEV, F16, F32, acts, np64, rng, tolerance, weight
 
 pytestmark = pytest.mark.gpu
-KERNELS = [16, 64, 65, 128, 129, 256, 65 + 2 * 1024, 128 + 3 * 1024, 256 + 2 * 1024]   # + 1024 x column slices, joined afterwards
+KERNELS = [16, 17, 32, 64, 65, 128, 129, 256, 65 + 2 * 1024, 128 + 3 * 1024, 256 + 2 * 1024]   # + 1024 x column slices, joined afterwards
 
 
 @pytest.fixture
