@@ -1,5 +1,5 @@
-// Around the products grouped by expert (f8_product.hip): which experts a token goes to and where its rows lie, the list of tiles that
-// the grouped product works through, and the weighted sums of a token's rows.
+// Around the products grouped by expert (f8_product.hip): which experts a token goes to and where its rows lie, and the
+// weighted sums of a token's rows.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -18,42 +18,6 @@ __device__ __forceinline__ void scan_lds(int* v, int n, OP op) {
         if (i < n) v[i] = mine;
         __syncthreads();
     }
-}
-
-// The tiles of the groups: group e has the rows [end[e - 1], end[e]), cut into pieces of tile_rows; the rows past the last group are one
-// more group, of zeros.
-__global__ __launch_bounds__(1024) void k_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles) {
-    __shared__ int end[kMaxExperts + 1], upto[kMaxExperts + 1];
-    const int i = threadIdx.x;
-    if (i < experts) end[i] = min(max(offsets[i + 1], 0), rows);
-    __syncthreads();
-    scan_lds(end, experts, [](int a, int b) { return max(a, b); });
-    if (i == 0) end[experts] = rows;
-    __syncthreads();
-    for (int e = i; e <= experts; e += 1024) upto[e] = (end[e] - (e ? end[e - 1] : 0) + tile_rows - 1) / tile_rows;
-    __syncthreads();
-    scan_lds(upto, experts, [](int a, int b) { return a + b; });
-    if (i == 0) upto[experts] += upto[experts - 1];
-    __syncthreads();
-    for (int t = i; t < n_tiles; t += 1024) {
-        int lo = 0, hi = experts + 1;   // the first group with upto > t
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (upto[mid] > t) hi = mid;
-            else lo = mid + 1;
-        }
-        F8Tile tile = {-1, 0, 0, 0};
-        if (lo <= experts) {
-            const int first = (lo ? end[lo - 1] : 0) + (t - (lo ? upto[lo - 1] : 0)) * tile_rows;
-            tile = {lo < experts ? lo : -1, first, min(tile_rows, end[lo] - first), 0};
-        }
-        tiles[t] = tile;
-    }
-}
-
-hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st) {
-    hipLaunchKernelGGL(k_f8_worklist, dim3(1), dim3(1024), 0, st, offsets, experts, rows, tile_rows, tiles, n_tiles);
-    return hipGetLastError();
 }
 
 // ---- routing.  Tokens are cut into chunks, one workgroup each, worked through 64 tokens at a time.  k_route_choose takes the top_k of every

@@ -18,7 +18,7 @@ struct F8Tile {
 };
 
 struct F8Params {
-    const unsigned char* x;    // [x_rows][kp], e4m3, zero past `in`
+    const unsigned char* x;    // [x_rows][kp], e4m3, zero past `in`; or (x_dtype) as it came, rows x_ld bytes apart
     const unsigned char* xs;   // [ks / 4][x_rows][4] biased exponents
     const unsigned char* w;    // [experts][out] rows of e4m3, ldw bytes apart
     const void* ws;            // [experts][ceil(out / 128)][kb]
@@ -28,6 +28,8 @@ struct F8Params {
     size_t ldw, ldy;
     int out, in, kb, kp, ks;   // kb: blocks of columns, kp = 128 kb, ks = kb rounded up to 4
     int x_rows, rows;          // rows of x, of y
+    int x_dtype, gated;        // BITSTACK_T_F8, or the type of what is to be brought to 8 bits on the way
+    unsigned x_bytes, x_ld;    // extent of x
     float* part;               // partial sums of the column slices
     int slices, slice_blocks;  // of the columns; blocks in one
     int n_tiles;               // tiles of rows (an upper bound where they are grouped)
@@ -84,21 +86,33 @@ __device__ __forceinline__ int f8_exponent(float amax) {
 }
 __device__ __forceinline__ float f8_inverse(int biased) { return __uint_as_float(unsigned(254 - biased) << 23); }   // 2^-e; biased <= 247
 
+// Four floats, at most 448 in magnitude, to e4m3 (round to nearest even)
+__device__ __forceinline__ unsigned f8_x4(float a, float b, float c, float d) {
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return unsigned(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
+}
+// |v| as an integer that orders like it, NaN and infinity above all others
+__device__ __forceinline__ unsigned f8_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ __forceinline__ float f8_gate(float g, float u) { return __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), u); }
+
+// The work list of a product grouped by expert: made by the launch that brings the activations to 8 bits, or (rows 0 there) by itself
+struct F8WorkList {
+    const int* offsets = nullptr;   // null: none
+    int experts = 0, rows = 0, tile_rows = 0, n_tiles = 0;
+    F8Tile* tiles = nullptr;
+};
 hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,
-                              hipStream_t st);
+                              const F8WorkList& list, hipStream_t st);
 hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int out, int in, unsigned char* q, size_t ld_q,
                                      unsigned char* s, hipStream_t st);
-hipError_t launch_f8_worklist(const int* offsets, int experts, int rows, int tile_rows, F8Tile* tiles, int n_tiles, hipStream_t st);
-hipError_t launch_f8_product(const F8Params& p, int experts, F8Tile* list, const int* offsets, hipStream_t st);
+// Kernel and column slices of a product, from sizes alone
 struct F8Plan {
     int kernel, slices, tile_rows, n_tiles;   // tile_rows: rows of y in a tile
     size_t part_bytes;                        // partial sums
 };
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact);
-size_t f8_partial_bytes(int rows, int out, int in, int experts);   // for any type of y, grouped or not
+hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
 void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
-// an upper bound on the work list's length, whatever tile the product takes
-size_t f8_worklist_entries(int rows, int experts);
 
 size_t route_workspace_bytes(int tokens, int experts, int top_k);
 struct RouteParams {

@@ -18,16 +18,17 @@ bool real_type(int t) { return t == BITSTACK_T_F16 || t == BITSTACK_T_F32 || t =
 size_t type_size(int t) { return t == BITSTACK_T_F32 ? 4 : 2; }
 bool columns_ok(int in) { return in >= 1 && in <= kMaxIn; }
 
+// What a call needs of the workspace.  `raw`: the product itself brings the activations to 8 bits.
 struct Workspace {
     size_t q, scales, list, part, total;
 };
-Workspace workspace_of(int x_rows, int in, int y_rows, int out, int experts, bool quantised) {
+Workspace workspace_of(int x_rows, int in, const F8Plan& plan, bool raw, bool grouped) {
     Workspace w;
     w.q = 0;
-    w.scales = quantised ? 0 : align256(size_t(x_rows) * bitstack_f8_row_bytes(in));
-    w.list = quantised ? 0 : w.scales + align256(size_t(x_rows) * bitstack_f8_row_scales(in));
-    w.part = w.list + align256(f8_worklist_entries(y_rows, experts) * sizeof(F8Tile));
-    w.total = w.part + align256(f8_partial_bytes(y_rows, out, in, experts));
+    w.scales = raw ? 0 : align256(size_t(x_rows) * bitstack_f8_row_bytes(in));
+    w.list = raw ? 0 : w.scales + align256(size_t(x_rows) * bitstack_f8_row_scales(in));
+    w.part = w.list + (grouped ? align256(size_t(plan.n_tiles) * sizeof(F8Tile)) : 0);
+    w.total = w.part + align256(plan.part_bytes);
     return w;
 }
 
@@ -46,44 +47,71 @@ int check_rows(const bitstack_f8_rows_t& x, int in) {
     return BITSTACK_OK;
 }
 
-int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, void* y,
-            int y_dtype, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+int check_call(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, int y_rows, int y_dtype) {
     if (y_rows < 0) return BITSTACK_E_RANGE;
     if (!columns_ok(w->in) || w->out < 1 || w->out > kMaxOut || w->experts < 1 || w->experts > kMaxExperts) return BITSTACK_E_SHAPE;
     if (w->scale_type != BITSTACK_S_E8M0 && w->scale_type != BITSTACK_S_F32) return BITSTACK_E_ARG;
     if (!real_type(y_dtype)) return BITSTACK_E_ARG;
-    int rc = check_rows(*x, w->in);
+    return check_rows(*x, w->in);
+}
+
+// Does the product bring the activations to 8 bits itself?  Few rows: every workgroup does so anew, for each 16 or 64 rows of the weight.  Their
+// 16-byte pieces have to be whole and in reach of 31-bit offsets.  (One token through 1024 x 4096: see the measurements at k_f8_slices.)
+bool raw_rows(const bitstack_f8_rows_t& x, int in, int y_rows, const F8Plan& plan) {
+    if (x.dtype == BITSTACK_T_F8 || y_rows > 16 || plan.tile_rows != 16 || in % 16 != 0 || x.rows < 1) return false;
+    const size_t size = type_size(x.dtype);
+    return !misaligned(x.x, 16) && (x.rows == 1 || x.ld * size % 16 == 0) && (size_t(x.rows - 1) * x.ld + (size_t(in) << x.gated)) * size <= kMaxRowBytes &&
+           (x.rows == 1 || x.ld * size <= kMaxRowBytes);
+}
+
+int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, void* y,
+            int y_dtype, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+    const int rc = check_call(x, w, y_rows, y_dtype);
     if (rc) return rc;
     if (y_rows == 0) return BITSTACK_OK;
     if (!w->q || !w->scales || !y) return BITSTACK_E_NULL;
     if (misaligned(w->q, 16) || w->ld % 16 || (w->scale_type == BITSTACK_S_F32 && misaligned(w->scales, 4))) return BITSTACK_E_ALIGN;
     if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
-    const bool quantised = x->dtype == BITSTACK_T_F8;
-    const Workspace at = workspace_of(x->rows, w->in, y_rows, w->out, w->experts, quantised);
-    if (!quantised || offsets || at.total > at.part) {
+    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32);
+    const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, w->in, y_rows, plan);
+    const Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
+    if (at.total) {
         if (!workspace) return BITSTACK_E_NULL;
         if (misaligned(workspace, 256)) return BITSTACK_E_ALIGN;
         if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    F8WorkList list;
+    if (offsets) list = {offsets, w->experts, y_rows, plan.tile_rows, plan.n_tiles, reinterpret_cast<F8Tile*>(ws + at.list)};
     F8Params p{};
+    p.x_dtype = BITSTACK_T_F8;
+    p.x_bytes = unsigned(size_t(x->rows) * bitstack_f8_row_bytes(w->in));
+    const bool rows_here = !quantised && !raw && x->rows > 0;
+    if (rows_here || offsets) {
+        const hipError_t e = launch_f8_quantise(x->x, rows_here ? x->dtype : int(BITSTACK_T_F16), x->ld, rows_here ? x->rows : 0, w->in, x->gated != 0, ws + at.q,
+                                                ws + at.scales, list, st);
+        if (e != hipSuccess) return hip_error(e);
+    }
+    p.x = ws + at.q;
+    p.xs = ws + at.scales;
     if (quantised) {
         p.x = static_cast<const unsigned char*>(x->x);
         p.xs = static_cast<const unsigned char*>(x->scales);
-    } else {
-        if (x->rows) {
-            const hipError_t e = launch_f8_quantise(x->x, x->dtype, x->ld, x->rows, w->in, x->gated != 0, ws + at.q, ws + at.scales, st);
-            if (e != hipSuccess) return hip_error(e);
-        }
-        p.x = ws + at.q;
-        p.xs = ws + at.scales;
+    } else if (raw) {
+        const size_t size = type_size(x->dtype);
+        p.x = static_cast<const unsigned char*>(x->x);
+        p.x_dtype = x->dtype;
+        p.gated = x->gated;
+        p.x_bytes = unsigned((size_t(x->rows - 1) * x->ld + (size_t(w->in) << x->gated)) * size);
+        p.x_ld = x->rows > 1 ? unsigned(x->ld * size) : 0;
     }
     p.w = static_cast<const unsigned char*>(w->q);
     p.ws = w->scales;
     p.y = y;
     p.index = index;
+    p.tiles = list.tiles;
     p.part = reinterpret_cast<float*>(ws + at.part);
     p.ldw = w->ld;
     p.ldy = ld_y;
@@ -98,7 +126,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     p.ws_f32 = w->scale_type == BITSTACK_S_F32;
     p.y_vec = ld_y % 4 == 0 && !misaligned(y, 4 * type_size(y_dtype));
     p.y_vec16 = ld_y * type_size(y_dtype) % 16 == 0 && !misaligned(y, 16);
-    const hipError_t e = launch_f8_product(p, w->experts, reinterpret_cast<F8Tile*>(ws + at.list), offsets, st);
+    const hipError_t e = launch_f8_product(p, plan, st);
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }
 
@@ -120,7 +148,7 @@ int bitstack_f8_quantise(const void* x, int x_dtype, size_t ld, int rows, int in
     if (!q || !scales) return BITSTACK_E_NULL;
     if (misaligned(q, 16) || misaligned(scales, 4)) return BITSTACK_E_ALIGN;
     const hipError_t e = launch_f8_quantise(x, x_dtype, ld, rows, in, gated != 0, static_cast<unsigned char*>(q),
-                                            static_cast<unsigned char*>(scales), static_cast<hipStream_t>(stream));
+                                            static_cast<unsigned char*>(scales), F8WorkList{}, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }
 
@@ -139,7 +167,19 @@ int bitstack_f8_quantise_weight(const void* w, int w_dtype, size_t ld, int out, 
 size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int experts) {
     if (x_rows < 0 || y_rows < 0 || !columns_ok(in) || out < 1 || out > kMaxOut || experts < 1 || experts > kMaxExperts) return 0;
     if (size_t(x_rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return 0;
-    return workspace_of(x_rows, in, y_rows, out, experts, false).total;
+    size_t most = 256;
+    for (int k = 0; k < 4; ++k)
+        if (y_rows) {
+            const size_t n = workspace_of(x_rows, in, f8_plan(y_rows, out, in, experts, k & 1, k >> 1), false, true).total;
+            most = n > most ? n : most;
+        }
+    return most;
+}
+
+size_t bitstack_f8_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, int y_rows, int y_dtype, int grouped) {
+    if (!x || !w || check_call(x, w, y_rows, y_dtype) || y_rows == 0) return 0;
+    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, grouped != 0, y_dtype == BITSTACK_T_F32);
+    return workspace_of(x->rows, w->in, plan, x->dtype == BITSTACK_T_F8 || raw_rows(*x, w->in, y_rows, plan), grouped != 0).total;
 }
 
 int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, void* y, int y_dtype, size_t ld_y,

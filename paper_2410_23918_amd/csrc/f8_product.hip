@@ -152,10 +152,46 @@ __device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[
     }
 }
 
+// The activations of a lane as they come: 32 columns of a token in a block, of type T, and (GATED) as many values to be gated
+constexpr int kRowsF8 = BITSTACK_T_F8;
+template <int T, bool GATED>
+struct RawColumns {
+    static constexpr int kPieces = 32 * int(sizeof(typename Elem<T>::type)) / 16;   // of 16 bytes
+    v4i v[kPieces], u[GATED ? kPieces : 1];
+};
+template <bool GATED>
+struct RawColumns<kRowsF8, GATED> {};
+template <int T, bool GATED>
+__device__ __forceinline__ void columns_to_f8(const RawColumns<T, GATED>& r, v8i& x, int& scale) {
+    typedef typename Elem<T>::type E;
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        constexpr int K = Elem<T>::kPer16;
+        typedef E piece __attribute__((ext_vector_type(K)));
+        v[i] = float(__builtin_bit_cast(piece, r.v[i / K])[i % K]);
+        if constexpr (GATED) v[i] = f8_gate(v[i], float(__builtin_bit_cast(piece, r.u[i / K])[i % K]));
+    }
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, f8_magnitude(v[i]));
+    m = max(m, unsigned(__shfl_xor(int(m), 16)));   // the other lanes of the token
+    m = max(m, unsigned(__shfl_xor(int(m), 32)));
+    const bool bad = m >= 0x7f800000u;
+    scale = bad ? kOne : f8_exponent(__uint_as_float(m));
+    const float inv = f8_inverse(scale);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) x[d] = bad ? 0x7f7f7f7f : int(f8_x4(v[4 * d] * inv, v[4 * d + 1] * inv, v[4 * d + 2] * inv, v[4 * d + 3] * inv));
+}
+
 // A tile of 16 FR rows of the weight x 16 FT tokens.  The eight wavefronts of a workgroup take every eighth block of columns each, straight
 // from memory into registers (nothing of a tile is read by two of them), DEPTH blocks ahead; their sums meet in LDS.
-template <int FR, int FT, int DEPTH, int MODE>
+//   T: type of the activations.  With one fragment of tokens they may come as they are and are brought to 8 bits on the way (a block of a token lies
+// in four lanes), by every workgroup anew: one launch instead of two.
+template <int FR, int FT, int DEPTH, int MODE, int T, bool GATED>
 __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
+    constexpr bool kRaw = T != kRowsF8;
+    static_assert(!kRaw || FT == 1, "one fragment of raw tokens");
     __shared__ v4f red[8 * FR * FT * 64];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -181,7 +217,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
         const int w_rows = min(16 * FR, p.out - n0);
         const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(wbase), 0,
                                                                             int((w_rows - 1) * p.ldw + (p.in + 15) / 16 * 16), 0x00020000);
-        const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p.x), 0, int(unsigned(p.x_rows) * unsigned(p.kp)), 0x00020000);
+        const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p.x), 0, int(unsigned(p.x_bytes)), 0x00020000);
         const bool s_f32 = MODE == kModeF32 || (MODE == kModeExact && p.ws_f32);
         const int s_size = s_f32 ? 4 : 1;
         const size_t s_row = (size_t(expert) * ((p.out + 127) / 128) + n0 / 128) * p.kb;
@@ -196,11 +232,12 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
             int r = row0 + min(16 * i + ln, rows - 1);
             if (p.index) r = p.index[r];
             const bool there = unsigned(r) < unsigned(p.x_rows);
-            x_off[i] = there ? unsigned(r) * unsigned(p.kp) + kg * 16 : 0x80000000u;
+            x_off[i] = !there ? 0x80000000u : kRaw ? unsigned(r) * unsigned(p.x_ld) : unsigned(r) * unsigned(p.kp) + kg * 16;
             xs_off[i] = there ? unsigned(r) * 4u : 0x80000000u;
         }
         struct Stage {
             v4i w[FR][2], x[FT][2];
+            RawColumns<T, GATED> raw;
             int xs[FT];
             int sw;
         };
@@ -215,6 +252,21 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
                 for (int h = 0; h < 2; ++h) s.w[j][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr, int((w_off[j] + col + h * 64) | oob), 0, 0));
 #pragma unroll
             for (int i = 0; i < FT; ++i) {
+                if constexpr (kRaw) {
+                    constexpr int kHalf = RawColumns<T, GATED>::kPieces / 2;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int c = b * 128 + h * 64 + kg * 16;
+                        const unsigned at = (x_off[i] + unsigned(c) * unsigned(sizeof(typename Elem<T>::type))) | oob | (c < p.in ? 0u : 0x80000000u);
+#pragma unroll
+                        for (int k = 0; k < kHalf; ++k) {
+                            s.raw.v[h * kHalf + k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int(at + k * 16), 0, 0));
+                            if constexpr (GATED)
+                                s.raw.u[h * kHalf + k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int(at + k * 16), p.in * int(sizeof(typename Elem<T>::type)), 0));
+                        }
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) s.x[i][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int((x_off[i] + col + h * 64) | oob), 0, 0));
                 s.xs[i] = __builtin_amdgcn_raw_buffer_load_b8(xsr, int((xs_off[i] + (b & 3)) | oob), int(in ? unsigned(b >> 2) * unsigned(p.x_rows) * 4u : 0u), 0);
@@ -234,7 +286,10 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
 #pragma unroll
             for (int j = 0; j < FR; ++j) w[j] = join(s.w[j][0], s.w[j][1]);
 #pragma unroll
-            for (int i = 0; i < FT; ++i) x[i] = join(s.x[i][0], s.x[i][1]);
+            for (int i = 0; i < FT; ++i) {
+                if constexpr (kRaw) columns_to_f8<T, GATED>(s.raw, x[i], s.xs[i]);
+                else x[i] = join(s.x[i][0], s.x[i][1]);
+            }
             multiply_all<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32, [](int) {});
         };
 #pragma unroll
@@ -560,15 +615,28 @@ static hipError_t tiles(F8Params p, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int FR, int FT, int DEPTH>
-static void slices(const F8Params& p, hipStream_t st) {
+template <int FR, int FT, int DEPTH, int MODE, int T, bool GATED>
+static void slices_as(const F8Params& p, hipStream_t st) {
     const int nrt = (p.out + 16 * FR - 1) / (16 * FR);
-    const dim3 grid(unsigned(8 * ((nrt + 7) / 8)) * unsigned(p.n_tiles));
-    if (p.y_dtype == BITSTACK_T_F32) hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, kModeExact>), grid, dim3(512), 0, st, p);
-    else if (p.ws_f32) hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, kModeF32>), grid, dim3(512), 0, st, p);
-    else hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, kModeE8M0>), grid, dim3(512), 0, st, p);
+    hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, MODE, T, GATED>), dim3(unsigned(8 * ((nrt + 7) / 8)) * unsigned(p.n_tiles)), dim3(512), 0, st, p);
 }
-
+template <int FR, int FT, int DEPTH, int T, bool GATED>
+static void slices_of(const F8Params& p, hipStream_t st) {
+    if (p.y_dtype == BITSTACK_T_F32) slices_as<FR, FT, DEPTH, kModeExact, T, GATED>(p, st);
+    else if (p.ws_f32) slices_as<FR, FT, DEPTH, kModeF32, T, GATED>(p, st);
+    else slices_as<FR, FT, DEPTH, kModeE8M0, T, GATED>(p, st);
+}
+template <int FR, int FT, int DEPTH>
+static hipError_t slices(const F8Params& p, hipStream_t st) {
+    if constexpr (FT == 1) {
+        if (p.x_dtype == BITSTACK_T_F16) p.gated ? slices_of<FR, FT, DEPTH, BITSTACK_T_F16, true>(p, st) : slices_of<FR, FT, DEPTH, BITSTACK_T_F16, false>(p, st);
+        else if (p.x_dtype == BITSTACK_T_BF16) p.gated ? slices_of<FR, FT, DEPTH, BITSTACK_T_BF16, true>(p, st) : slices_of<FR, FT, DEPTH, BITSTACK_T_BF16, false>(p, st);
+        else if (p.x_dtype == BITSTACK_T_F32) p.gated ? slices_of<FR, FT, DEPTH, BITSTACK_T_F32, true>(p, st) : slices_of<FR, FT, DEPTH, BITSTACK_T_F32, false>(p, st);
+        if (p.x_dtype != BITSTACK_T_F8) return hipGetLastError();
+    }
+    slices_of<FR, FT, DEPTH, BITSTACK_T_F8, false>(p, st);
+    return hipGetLastError();
+}
 
 // Kernels by their tile (rows of the weight x of y): 16 x 16, 64 x 16, 64 x 32, 64 x 64 without LDS, 128 x 64, 128 x 128, 256 x 128, 256 x 256
 enum F8Kernel { kSlices16 = 16, kSlices16Wide = 17, kSlices32 = 32, kSlices64 = 64, kTile64 = 65, kTile128 = 128, kTile128Wide = 129, kTile256 = 256 };
@@ -587,7 +655,7 @@ static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, 
     const double mt = grouped ? std::max<double>(groups, double(rows) / k.toks + 0.5 * groups) : (rows + k.toks - 1) / k.toks;
     const double tiles = mt * ((out + k.rows - 1) / k.rows), rounds = std::ceil(tiles * slices / 256);
     // the weights once, from memory
-    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.toks == 16 ? 4.7e6 : k.toks == 32 ? 4.2e6 : 3.6e6);
+    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.toks == 16 ? 4.7e6 : k.toks == 32 ? 4.2e6 : k.kernel == kSlices64 ? 3.6e6 : 4.0e6);
     const double passes = (kb + 7) / 8, whole = std::floor(tiles / 1024), rest = (tiles - 1024 * whole) / 256;
     double us;
     if (k.kernel == kSlices16) {   // up to four workgroups on a compute unit
@@ -610,6 +678,7 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact)
     F8Plan plan{kShapes[0].kernel, 1, 0, 0, 0};
     double best = 1e30;
     for (const F8KernelShape& k : kShapes) {
+        if (!forced && rows <= 16 && k.toks > 16) break;   // never faster
         if (exact && k.kernel >= kTile128Wide) continue;   // the operands as fp16 leave no registers for its sums
         for (int slices : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (forced ? k.kernel != forced % 1024 || slices > 1 : slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
@@ -632,30 +701,17 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact)
         }
     return plan;
 }
-size_t f8_partial_bytes(int rows, int out, int in, int experts) {
-    size_t most = 0;
-    for (int k = 0; k < 4; ++k) most = std::max(most, f8_plan(rows, out, in, experts, k & 1, k >> 1).part_bytes);
-    return most;
-}
-size_t f8_worklist_entries(int rows, int experts) { return size_t(rows) / 16 + 2 + size_t(rows < experts ? rows : experts); }
-
-hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, const int* offsets, hipStream_t st) {
+hipError_t launch_f8_product(const F8Params& args, const F8Plan& plan, hipStream_t st) {
     F8Params p = args;
-    const bool exact = p.y_dtype == BITSTACK_T_F32;
-    const F8Plan plan = f8_plan(p.rows, p.out, p.in, experts, offsets != nullptr, exact);
     p.slices = plan.slices;
     p.slice_blocks = (p.kb + plan.slices - 1) / plan.slices;
     p.n_tiles = plan.n_tiles;
-    if (offsets) {
-        p.tiles = list;
-        const hipError_t e = launch_f8_worklist(offsets, experts, p.rows, plan.tile_rows, list, p.n_tiles, st);
-        if (e != hipSuccess) return e;
-    }
+    const bool exact = p.y_dtype == BITSTACK_T_F32;
     switch (plan.kernel) {
-        case kSlices16: slices<1, 1, 2>(p, st); return hipGetLastError();
-        case kSlices16Wide: slices<4, 1, 1>(p, st); return hipGetLastError();
-        case kSlices32: slices<4, 2, 1>(p, st); return hipGetLastError();
-        case kSlices64: slices<4, 4, 1>(p, st); return hipGetLastError();
+        case kSlices16: return slices<1, 1, 2>(p, st);
+        case kSlices16Wide: return slices<4, 1, 1>(p, st);
+        case kSlices32: return slices<4, 2, 1>(p, st);
+        case kSlices64: return slices<4, 4, 1>(p, st);
         case kTile64:
             if (exact) return tiles<2, 2, 4, 2, kModeExact, false>(p, st);
             return p.ws_f32 ? tiles<2, 2, 4, 2, kModeF32, false>(p, st) : tiles<2, 2, 4, 2, kModeE8M0, false>(p, st);
@@ -666,7 +722,7 @@ hipError_t launch_f8_product(const F8Params& args, int experts, F8Tile* list, co
             return p.ws_f32 ? tiles<4, 4, 4, 2, kModeF32, false>(p, st) : tiles<4, 4, 4, 2, kModeE8M0, false>(p, st);
         default: {
             // (touching: see the kernel; 256 tiles are all there at once)
-            const bool touch = !offsets && size_t((p.out + 255) / 256) * p.n_tiles > 256;
+            const bool touch = !p.tiles && size_t((p.out + 255) / 256) * p.n_tiles > 256;
             if (p.ws_f32) return touch ? tiles<8, 4, 2, 4, kModeF32, true>(p, st) : tiles<8, 4, 2, 4, kModeF32, false>(p, st);
             return touch ? tiles<8, 4, 2, 4, kModeE8M0, true>(p, st) : tiles<8, 4, 2, 4, kModeE8M0, false>(p, st);
         }

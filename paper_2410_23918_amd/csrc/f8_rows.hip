@@ -10,23 +10,67 @@
 
 namespace bitstack {
 
-// Four floats, at most 448 in magnitude, to e4m3 (round to nearest even)
-__device__ __forceinline__ unsigned to_f8x4(float a, float b, float c, float d) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return unsigned(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
+// Inclusive scan of v[0 .. n) in LDS by a workgroup of 256, op associative
+template <class OP>
+__device__ __forceinline__ void scan256(int* v, int n, OP op) {
+    __shared__ int part[256];
+    const int i = threadIdx.x, each = (n + 255) / 256, first = i * each, last = min(first + each, n);
+    for (int k = first + 1; k < last; ++k) v[k] = op(v[k - 1], v[k]);
+    part[i] = first < last ? v[last - 1] : v[n - 1];
+    __syncthreads();
+    const int parts = (n + each - 1) / each;
+    for (int d = 1; d < parts; d <<= 1) {
+        const int mine = i >= d ? op(part[i - d], part[i]) : part[i];
+        __syncthreads();
+        part[i] = mine;
+        __syncthreads();
+    }
+    if (i > 0)
+        for (int k = first; k < last; ++k) v[k] = op(part[i - 1], v[k]);
+    __syncthreads();
 }
 
-// |v| as an integer that orders like it, NaN and infinity above all others
-__device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The tiles of the groups, by a workgroup of 256: group e has the rows [end[e - 1], end[e]), cut into pieces of tile_rows; the rows past the last group
+// are one more group, of zeros.  Offsets that fall, or pass the last row, are held to the rows there are.
+__device__ void make_work_list(const F8WorkList& l) {
+    __shared__ int end[kMaxExperts + 1], upto[kMaxExperts + 1];
+    const int i = threadIdx.x;
+    for (int e = i; e < l.experts; e += 256) end[e] = min(max(l.offsets[e + 1], 0), l.rows);
+    __syncthreads();
+    scan256(end, l.experts, [](int a, int b) { return max(a, b); });
+    if (i == 0) end[l.experts] = l.rows;
+    __syncthreads();
+    for (int e = i; e <= l.experts; e += 256) upto[e] = (end[e] - (e ? end[e - 1] : 0) + l.tile_rows - 1) / l.tile_rows;
+    __syncthreads();
+    scan256(upto, l.experts + 1, [](int a, int b) { return a + b; });
+    for (int t = i; t < l.n_tiles; t += 256) {
+        int lo = 0, hi = l.experts + 1;   // the first group with upto > t
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (upto[mid] > t) hi = mid;
+            else lo = mid + 1;
+        }
+        F8Tile tile = {-1, 0, 0, 0};
+        if (lo <= l.experts) {
+            const int first = (lo ? end[lo - 1] : 0) + (t - (lo ? upto[lo - 1] : 0)) * l.tile_rows;
+            tile = {lo < l.experts ? lo : -1, first, min(l.tile_rows, end[lo] - first), 0};
+        }
+        l.tiles[t] = tile;
+    }
+}
 
 // Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row, whose scales are one word.
-// Bound by memory: x is read once and q written once, 16 and 8 bytes a lane.
+// Bound by memory: x is read once and q written once, 16 and 8 bytes a lane.  The first workgroup makes the work list where there is one.
 template <int T, bool GATED>
 __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, int vec, unsigned char* q,
-                                                     unsigned* s, int kp) {
+                                                     unsigned* s, int kp, F8WorkList list) {
+    if (list.offsets && blockIdx.x == 0) {
+        make_work_list(list);
+        return;
+    }
     const int lane = threadIdx.x & 63;
     const int per_row = (kp + 511) / 512;   // wavefronts
-    const size_t wave = (size_t(blockIdx.x) * 256 + threadIdx.x) >> 6;
+    const size_t wave = (size_t(blockIdx.x - (list.offsets ? 1 : 0)) * 256 + threadIdx.x) >> 6;
     const int row = int(wave / per_row), word = int(wave % per_row);
     if (row >= rows) return;
     const int col = word * 512 + lane * 8;
@@ -37,11 +81,11 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
         float u[8];
         load_elems<T, 8>(from + in, in - col, vec, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(__fdiv_rn(v[i], __fadd_rn(1.0f, expf(-v[i]))), u[i]);
+        for (int i = 0; i < 8; ++i) v[i] = f8_gate(v[i], u[i]);
     }
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, magnitude_bits(v[i]));
+    for (int i = 0; i < 8; ++i) m = max(m, f8_magnitude(v[i]));
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) m = max(m, unsigned(__shfl_xor(int(m), d, 16)));
     uint2 bytes;
@@ -51,7 +95,7 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
     } else {
         e = f8_exponent(__uint_as_float(m));
         const float r = f8_inverse(e);
-        bytes = make_uint2(to_f8x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), to_f8x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
+        bytes = make_uint2(f8_x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), f8_x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
     }
     if (col < kp) *reinterpret_cast<uint2*>(q + size_t(row) * kp + col) = bytes;
     const unsigned four = unsigned(__builtin_amdgcn_readlane(e, 0)) | unsigned(__builtin_amdgcn_readlane(e, 16)) << 8 |
@@ -74,7 +118,7 @@ __global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<
         const int row = nblock * kF8Block + i * 16 + (threadIdx.x >> 4);
         load_elems<T, 8>(w + size_t(row) * ld + col, row < out ? in - col : 0, vec, v[i]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) m = max(m, magnitude_bits(v[i][k]));
+        for (int k = 0; k < 8; ++k) m = max(m, f8_magnitude(v[i][k]));
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) m = max(m, unsigned(__shfl_xor(int(m), d)));
@@ -89,8 +133,8 @@ __global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<
         const int row = nblock * kF8Block + i * 16 + (threadIdx.x >> 4);
         if (row >= out || col >= q_cols) continue;
         const uint2 bytes = bad ? make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu)
-                                : make_uint2(to_f8x4(v[i][0] * r, v[i][1] * r, v[i][2] * r, v[i][3] * r),
-                                             to_f8x4(v[i][4] * r, v[i][5] * r, v[i][6] * r, v[i][7] * r));
+                                : make_uint2(f8_x4(v[i][0] * r, v[i][1] * r, v[i][2] * r, v[i][3] * r),
+                                             f8_x4(v[i][4] * r, v[i][5] * r, v[i][6] * r, v[i][7] * r));
         *reinterpret_cast<uint2*>(q + size_t(row) * ld_q + col) = bytes;
     }
     if (threadIdx.x == 0) s[size_t(nblock) * kb + kblock] = (unsigned char)e;
@@ -99,23 +143,23 @@ __global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<
 static bool vector_rows(const void* p, size_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0; }
 
 template <int T>
-static void quantise(const void* x, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s, hipStream_t st) {
+static void quantise(const void* x, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s, const F8WorkList& list, hipStream_t st) {
     typedef typename Elem<T>::type E;
     const int kp = (in + 127) / 128 * 128;
     // the halves of a gated row begin `in` elements apart
     const int vec = vector_rows(x, ld, sizeof(E)) && (!gated || size_t(in) * sizeof(E) % 16 == 0);
     const size_t waves = size_t(rows) * ((kp + 511) / 512);
-    const unsigned grid = unsigned((waves + 3) / 4);
+    const unsigned grid = unsigned((waves + 3) / 4) + (list.offsets ? 1 : 0);
     unsigned* const words = reinterpret_cast<unsigned*>(s);
-    if (gated) hipLaunchKernelGGL((k_f8_quantise<T, true>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp);
-    else hipLaunchKernelGGL((k_f8_quantise<T, false>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp);
+    if (gated) hipLaunchKernelGGL((k_f8_quantise<T, true>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list);
+    else hipLaunchKernelGGL((k_f8_quantise<T, false>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list);
 }
 
 hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,
-                              hipStream_t st) {
-    if (dtype == BITSTACK_T_F16) quantise<BITSTACK_T_F16>(x, ld, rows, in, gated, q, s, st);
-    else if (dtype == BITSTACK_T_BF16) quantise<BITSTACK_T_BF16>(x, ld, rows, in, gated, q, s, st);
-    else quantise<BITSTACK_T_F32>(x, ld, rows, in, gated, q, s, st);
+                              const F8WorkList& list, hipStream_t st) {
+    if (dtype == BITSTACK_T_F16) quantise<BITSTACK_T_F16>(x, ld, rows, in, gated, q, s, list, st);
+    else if (dtype == BITSTACK_T_BF16) quantise<BITSTACK_T_BF16>(x, ld, rows, in, gated, q, s, list, st);
+    else quantise<BITSTACK_T_F32>(x, ld, rows, in, gated, q, s, list, st);
     return hipGetLastError();
 }
 

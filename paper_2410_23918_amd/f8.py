@@ -7,7 +7,6 @@ a multiple of 16 bytes apart.  Without `stream` everything runs on the current s
 to that stream, and the caller orders it with the streams that made the inputs and use the outputs."""
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import threading
 from typing import NamedTuple
@@ -55,6 +54,7 @@ def _f8_lib():
             ("bitstack_f8_quantise", i32, [vp, i32, sz, i32, i32, i32, vp, vp, vp]),
             ("bitstack_f8_quantise_weight", i32, [vp, i32, sz, i32, i32, vp, sz, vp, vp]),
             ("bitstack_f8_workspace_bytes", sz, [i32] * 5),
+            ("bitstack_f8_call_workspace_bytes", sz, [vp, vp, i32, i32, i32]),
             ("bitstack_f8_linear", i32, [vp, vp, vp, i32, sz, vp, sz, vp]),
             ("bitstack_f8_grouped_linear", i32, [vp, vp, vp, vp, i32, vp, i32, sz, vp, sz, vp]),
             ("bitstack_route_workspace_bytes", sz, [i32] * 3),
@@ -103,17 +103,11 @@ def _type(t: torch.Tensor, what: str) -> int:
 
 
 class _On:
-    """The stream of a call: its handle, and the context in which the call allocates (so that what it allocates belongs to that
-    stream).  Inputs used on another stream than the current one are kept from reuse until that stream has passed the call."""
+    """A stream that is not the current one of the tensors' device: its handle, and the context in which a call allocates, so that what it
+    allocates belongs to that stream.  Inputs are kept from reuse until the stream has passed the call."""
 
     def __init__(self, device, stream, inputs):
-        if device.type != "cuda":
-            raise ValueError(f"tensors on a GPU are needed, not on {device}")
-        self._ctx = None
         if stream is None:
-            if device.index == torch.cuda.current_device():
-                self.handle = torch._C._cuda_getCurrentRawStream(device.index)
-                return
             stream = torch.cuda.current_stream(device)
         else:
             _need(stream.device == device, "the stream is another device's")
@@ -122,15 +116,43 @@ class _On:
                     if t is not None:
                         t.record_stream(stream)
         self.handle = stream.cuda_stream
-        self._ctx = contextlib.ExitStack()
-        self._ctx.enter_context(torch.cuda.stream(stream))   # its device too
+        self._ctx = torch.cuda.stream(stream)   # its device too
 
     def __enter__(self):
-        return self
+        self._ctx.__enter__()
+        return self.handle
 
     def __exit__(self, *exc):
-        if self._ctx is not None:
-            self._ctx.close()
+        return self._ctx.__exit__(*exc)
+
+
+class _Current:
+    """The current stream of the current device: nothing to enter (entering costs as much as a small launch)."""
+
+    def __init__(self, index):
+        self.index = index
+
+    def __enter__(self):
+        return _raw_stream(self.index)
+
+    def __exit__(self, *exc):
+        return None
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current: dict = {}
+
+
+def _on(device, stream, inputs):
+    if device.type != "cuda":
+        raise ValueError(f"tensors on a GPU are needed, not on {device}")
+    index = device.index
+    if stream is None and index == torch._C._cuda_getDevice():
+        on = _current.get(index)
+        if on is None:
+            on = _current[index] = _Current(index)
+        return on
+    return _On(device, stream, inputs)
 
 
 def _same_device(device, *tensors):
@@ -140,9 +162,11 @@ def _same_device(device, *tensors):
 
 
 def _matrix(t: torch.Tensor, what: str):
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    """elements from row to row"""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what}: a matrix whose rows are contiguous is needed")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
 def _fill_weight(q, scales, grouped):
@@ -151,14 +175,15 @@ def _fill_weight(q, scales, grouped):
     kind = _SCALES.get(scales.dtype)
     if kind is None:
         raise ValueError(f"scales: float8_e8m0fnu or float32, not {scales.dtype}")
-    w = _args.w
-    shape = q.shape
-    _need(len(shape) == (3 if grouped else 2) and (q.stride(-1) == 1 or shape[-1] == 1), "q: rows of e4m3, [out, in] or [experts, out, in]")
-    e, out, inn = (shape[0] if grouped else 1), shape[-2], shape[-1]
-    ld = q.stride(-2) if out > 1 else -(-inn // 16) * 16
-    _need(not grouped or e == 1 or q.stride(0) == out * ld, "q: the experts' weights have to follow one another")
+    shape, stride = q.shape, q.stride()
+    _need(len(shape) == (3 if grouped else 2) and (stride[-1] == 1 or shape[-1] == 1), "q: rows of e4m3, [out, in] or [experts, out, in]")
+    out, inn = shape[-2], shape[-1]
+    e = shape[0] if grouped else 1
+    ld = stride[-2] if out > 1 else -(-inn // 16) * 16
+    _need(e == 1 or stride[0] == out * ld, "q: the experts' weights have to follow one another")
     want = (-(-out // 128), -(-inn // 128))
-    _need(tuple(scales.shape) == ((e, *want) if grouped else want) and scales.is_contiguous(), f"scales: one for each 128 x 128 block of q, {want}, contiguous")
+    _need(scales.shape == ((e, *want) if grouped else want) and scales.is_contiguous(), f"scales: one for each 128 x 128 block of q, {want}, contiguous")
+    w = _args.w
     w.q, w.ld, w.scales, w.scale_type, w.out, w.inn, w.experts = q.data_ptr(), ld, scales.data_ptr(), kind, out, inn, e
     return out, inn, e
 
@@ -172,45 +197,52 @@ def _fill_rows(x, inn, gated):
         _need(x.q.dtype is torch.float8_e4m3fn and x.q.is_contiguous() and x.scales.is_contiguous() and x.scales.element_size() == 1
               and tuple(x.q.shape[1:]) == (L.bitstack_f8_row_bytes(inn),) and tuple(x.scales.shape) == (L.bitstack_f8_row_scales(inn) // 4, x.q.shape[0], 4),
               "x: as quantise_f8 makes it")
-        _same_device(x.q.device, x.scales)
         a.x, a.scales, a.ld, a.dtype, a.rows, a.gated = x.q.data_ptr(), x.scales.data_ptr(), 0, T_F8, x.q.shape[0], 0
-        return x.q.shape[0], x.q.device, torch.float16, (x.q, x.scales)
+        return x.q.shape[0], torch.float16, x[:2]
     t = _type(x, "x")
     ld = _matrix(x, "x")
-    _need(x.shape[1] == (2 * inn if gated else inn), f"x has {x.shape[1]} columns, the weight {inn}{' (gated: twice as many are needed)' if gated else ''}")
-    a.x, a.scales, a.ld, a.dtype, a.rows, a.gated = x.data_ptr(), None, ld, t, x.shape[0], int(gated)
-    return x.shape[0], x.device, x.dtype, (x,)
+    rows, width = x.shape
+    if width != (2 * inn if gated else inn):
+        raise ValueError(f"x has {width} columns, the weight {inn}{' (gated: twice as many are needed)' if gated else ''}")
+    a.x, a.scales, a.ld, a.dtype, a.rows, a.gated = x.data_ptr(), None, ld, t, rows, 1 if gated else 0
+    return rows, x.dtype, (x,)
 
 
 def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, stream, grouped):
     L = _f8_lib()
     out, inn, experts = _fill_weight(q, scales, grouped)
-    x_rows, device, dtype, held = _fill_rows(x, inn, gated)
-    _same_device(device, q, scales, offsets, index, y, workspace)
-    rows = x_rows
+    rows, dtype, held = _fill_rows(x, inn, gated)
+    device = q.device
+    _same_device(device, scales, offsets, index, y, workspace, *held)
     if grouped:
-        _need(offsets.dtype is torch.int32 and offsets.is_contiguous() and tuple(offsets.shape) == (experts + 1,), "offsets: int32 [experts + 1]")
+        _need(offsets.dtype is torch.int32 and offsets.is_contiguous() and offsets.shape == (experts + 1,), "offsets: int32 [experts + 1]")
         if index is not None:
-            _need(index.dtype is torch.int32 and index.is_contiguous() and index.dim() == 1, "rows: int32 [rows of y]")
+            _need(index.dtype is torch.int32 and index.dim() == 1 and index.is_contiguous(), "rows: int32 [rows of y]")
             rows = index.shape[0]
-    with _On(device, stream, (*held, q, scales, offsets, index, y, workspace)) as on:
+    args = _args
+    with _on(device, stream, (*held, q, scales, offsets, index, y, workspace)) as handle:
         if y is None:
             y = torch.empty((rows, out), dtype=out_dtype or dtype, device=device)
+            ld_y = out
         else:
-            _need(tuple(y.shape) == (rows, out) and (out_dtype is None or y.dtype is out_dtype), f"y: [{rows}, {out}] is needed")
-        ld_y = _matrix(y, "y")
+            _need(y.shape == (rows, out) and (out_dtype is None or y.dtype is out_dtype), f"y: [{rows}, {out}] is needed")
+            ld_y = _matrix(y, "y")
+        t = _type(y, "y")
         if workspace is None:
-            nbytes = L.bitstack_f8_workspace_bytes(x_rows, inn, rows, out, experts)
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            nbytes = L.bitstack_f8_call_workspace_bytes(args.xp, args.wp, rows, t, grouped)
+            if nbytes:
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         else:
             _need(workspace.is_contiguous(), "workspace: contiguous")
             nbytes = workspace.numel() * workspace.element_size()
+        ws = None if workspace is None else workspace.data_ptr()
         if grouped:
-            _check(L.bitstack_f8_grouped_linear(_args.xp, _args.wp, offsets.data_ptr(), None if index is None else index.data_ptr(), rows, y.data_ptr(),
-                                                _type(y, "y"), ld_y, workspace.data_ptr(), nbytes, on.handle), "bitstack_f8_grouped_linear")
+            rc = L.bitstack_f8_grouped_linear(args.xp, args.wp, offsets.data_ptr(), None if index is None else index.data_ptr(), rows, y.data_ptr(), t, ld_y, ws,
+                                              nbytes, handle)
         else:
-            _check(L.bitstack_f8_linear(_args.xp, _args.wp, y.data_ptr(), _type(y, "y"), ld_y, workspace.data_ptr(), nbytes, on.handle),
-                   "bitstack_f8_linear")
+            rc = L.bitstack_f8_linear(args.xp, args.wp, y.data_ptr(), t, ld_y, ws, nbytes, handle)
+        if rc:
+            raise BitStackError(rc, "bitstack_f8_grouped_linear" if grouped else "bitstack_f8_linear")
     return y
 
 
@@ -239,10 +271,10 @@ def quantise_f8(x, *, gated: bool = False, stream=None) -> F8Rows:
     t, ld = _type(x, "x"), _matrix(x, "x")
     _need(not gated or x.shape[1] % 2 == 0, "gated: gate and value side by side are needed")
     n, inn = x.shape[0], x.shape[1] // (2 if gated else 1)
-    with _On(x.device, stream, (x,)) as on:
+    with _on(x.device, stream, (x,)) as handle:
         q = torch.empty((n, L.bitstack_f8_row_bytes(inn)), dtype=torch.float8_e4m3fn, device=x.device)
         s = torch.empty((L.bitstack_f8_row_scales(inn) // 4, n, 4), dtype=torch.uint8, device=x.device)
-        _check(L.bitstack_f8_quantise(x.data_ptr(), t, ld, n, inn, int(gated), q.data_ptr(), s.data_ptr(), on.handle), "bitstack_f8_quantise")
+        _check(L.bitstack_f8_quantise(x.data_ptr(), t, ld, n, inn, int(gated), q.data_ptr(), s.data_ptr(), handle), "bitstack_f8_quantise")
     return F8Rows(q, s, inn)
 
 
@@ -255,12 +287,12 @@ def quantise_weight_f8(w, *, stream=None):
     each = w if w.dim() == 3 else w[None]
     e, out, inn = each.shape
     ld_q = int(L.bitstack_f8_row_bytes(inn))
-    with _On(w.device, stream, (w,)) as on:
+    with _on(w.device, stream, (w,)) as handle:
         q = torch.empty((e, out, ld_q), dtype=torch.float8_e4m3fn, device=w.device)
         s = torch.empty((e, -(-out // 128), -(-inn // 128)), dtype=torch.float8_e8m0fnu, device=w.device)
         for i in range(e):
             _check(L.bitstack_f8_quantise_weight(each[i].data_ptr(), t, _matrix(each[i], "w"), out, inn, q[i].data_ptr(), ld_q, s[i].data_ptr(),
-                                                 on.handle), "bitstack_f8_quantise_weight")
+                                                 handle), "bitstack_f8_quantise_weight")
     q = q[:, :, :inn]
     return (q, s) if w.dim() == 3 else (q[0], s[0])
 
@@ -270,16 +302,18 @@ def route(logits, top_k: int, *, renormalise: bool = True, stream=None) -> Routi
     L = _f8_lib()
     t, ld = _type(logits, "logits"), _matrix(logits, "logits")
     n, e = logits.shape
-    with _On(logits.device, stream, (logits,)) as on:
+    with _on(logits.device, stream, (logits,)) as handle:
         nbytes = L.bitstack_route_workspace_bytes(n, e, top_k)
         if nbytes == 0:
             raise BitStackError(-2, "bitstack_route_workspace_bytes")
-        i32 = dict(dtype=torch.int32, device=logits.device)
-        r = Routing(torch.empty((n, top_k), **i32), torch.empty((n, top_k), dtype=torch.float32, device=logits.device), torch.empty((n, top_k), **i32),
-                    torch.empty(n * top_k, **i32), torch.empty(e + 1, **i32))
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
-        _check(L.bitstack_route(logits.data_ptr(), t, ld, n, e, top_k, int(renormalise), r.experts.data_ptr(), r.weights.data_ptr(), r.slots.data_ptr(),
-                                r.rows.data_ptr(), r.offsets.data_ptr(), ws.data_ptr(), nbytes, on.handle), "bitstack_route")
+        words = torch.empty((4, n, top_k), dtype=torch.int32, device=logits.device)
+        at = -(-(e + 1) // 64) * 64   # the offsets, then (256-byte aligned) the workspace
+        tail = torch.empty(at + nbytes // 4, dtype=torch.int32, device=logits.device)
+        experts, weights, slots, rows = words.unbind(0)
+        r = Routing(experts, weights.view(torch.float32), slots, rows.view(-1), tail[: e + 1])
+        p, step, o = words.data_ptr(), 4 * n * top_k, tail.data_ptr()
+        _check(L.bitstack_route(logits.data_ptr(), t, ld, n, e, top_k, int(renormalise), p, p + step, p + 2 * step, p + 3 * step, o, o + 4 * at, nbytes,
+                                handle), "bitstack_route")
     return r
 
 
@@ -291,11 +325,11 @@ def combine(h, slots, weights, *, y=None, stream=None):
           and slots.is_contiguous() and weights.is_contiguous(), "slots: int32, weights: float32, both [tokens, top_k] and contiguous")
     _same_device(h.device, slots, weights, y)
     n, k = slots.shape
-    with _On(h.device, stream, (h, slots, weights, y)) as on:
+    with _on(h.device, stream, (h, slots, weights, y)) as handle:
         if y is None:
             y = torch.empty((n, h.shape[1]), dtype=h.dtype, device=h.device)
         else:
             _need(tuple(y.shape) == (n, h.shape[1]) and y.dtype is h.dtype, "y: [tokens, width] of h's type")
         _check(L.bitstack_combine(h.data_ptr(), t, ld, h.shape[0], h.shape[1], slots.data_ptr(), weights.data_ptr(), n, k, y.data_ptr(), _matrix(y, "y"),
-                                  on.handle), "bitstack_combine")
+                                  handle), "bitstack_combine")
     return y

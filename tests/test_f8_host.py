@@ -27,6 +27,12 @@ def test_sizes(L):
     assert L.bitstack_f8_workspace_bytes(10, 300, 10, 64, 1) >= 10 * (384 + 4)
     for bad in ((-1, 300, 1, 64, 1), (1, 0, 1, 64, 1), (1, 300, -1, 64, 1), (1, 300, 1, 0, 1), (1, 300, 1, 64, 0), (1, 300, 1, 64, 1025), (1 << 20, 4096, 1, 64, 1)):
         assert L.bitstack_f8_workspace_bytes(*bad) == 0
+    from paper_2410_23918_amd.f8 import _Rows, _Weight
+    for tokens, grouped, dtype in ((1, 0, 0), (1, 1, 0), (40, 0, 2), (300, 1, 0), (5, 0, 3)):   # a call's own needs are no more than what is said ahead
+        n = L.bitstack_f8_call_workspace_bytes(C.byref(_Rows(P, P, 4096, dtype, tokens, 0)), C.byref(_Weight(P, 4096, P, 0, 512, 4096, 3 if grouped else 1)), tokens, 0, grouped)
+        assert n <= L.bitstack_f8_workspace_bytes(tokens, 4096, tokens, 512, 3 if grouped else 1)
+        assert (n == 0) == (not grouped and tokens <= 16)
+    assert L.bitstack_f8_call_workspace_bytes(None, None, 1, 0, 0) == 0
     for bad in ((-1, 8, 2), (1, 0, 1), (1, 8, 0), (1, 8, 9), (1, 1025, 1), (1, 64, 33)):
         assert L.bitstack_route_workspace_bytes(*bad) == 0
     with pytest.raises(B.BitStackError):
@@ -36,7 +42,7 @@ def test_sizes(L):
 def refused(L, code, x=None, w=None, **change):
     from paper_2410_23918_amd.f8 import _Rows, _Weight
     weight = dict(q=P, ld=256, scales=P, scale_type=0, out=64, inn=256, experts=1) | (w or {})
-    rows = dict(x=P, scales=P, ld=256, dtype=0, rows=4, gated=0) | (x or {})
+    rows = dict(x=P, scales=P, ld=256, dtype=0, rows=40, gated=0) | (x or {})
     a = dict(y=P, y_dtype=0, ld_y=64, ws=P, ws_bytes=1 << 20) | change
     args = (C.byref(_Rows(**rows)), C.byref(_Weight(**weight)))
     end = (a["y"], a["y_dtype"], a["ld_y"], a["ws"], a["ws_bytes"], None)
@@ -63,12 +69,12 @@ def test_refusals_of_the_products(L):
     refused(L, ALIGN, ws=P + 16)
     refused(L, SIZE, ws_bytes=100)
     from paper_2410_23918_amd.f8 import _Rows, _Weight
-    args = (C.byref(_Rows(P, P, 256, 0, 4, 0)), C.byref(_Weight(P, 256, P, 0, 64, 256, 3)))
+    args = (C.byref(_Rows(P, P, 256, 0, 40, 0)), C.byref(_Weight(P, 256, P, 0, 64, 256, 3)))
     grouped = lambda off, index, n: L.bitstack_f8_grouped_linear(*args, off, index, n, P, 0, 64, P, 1 << 20, None)
-    assert grouped(None, None, 4) == NULL
-    assert grouped(P, None, 5) == RANGE   # rows of y that x does not have
+    assert grouped(None, None, 40) == NULL
+    assert grouped(P, None, 41) == RANGE   # rows of y that x does not have
     assert grouped(P, None, -1) == RANGE
-    assert grouped(P + 2, None, 4) == ALIGN and grouped(P, P + 2, 4) == ALIGN
+    assert grouped(P + 2, None, 40) == ALIGN and grouped(P, P + 2, 40) == ALIGN
 
 
 def test_refusals_of_the_others(L):

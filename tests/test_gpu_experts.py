@@ -98,6 +98,20 @@ def test_grouped_gated():
         assert (np.abs(np64(y[a:b]) - want) <= tolerance(x8[a:b], w, F32, want)).all()
 
 
+@pytest.mark.parametrize("dtype", [F16, F32], ids=["f16", "f32"])
+def test_grouped_few_rows(dtype):
+    """one to a few tokens decoded: the products bring the rows to 8 bits themselves, gathered ones and ones from nowhere among them"""
+    g = rng(31)
+    q, s = weight(g, 200, 512, "e8m0", experts=9)
+    off = np.array([0, 0, 2, 2, 3, 3, 3, 9, 9, 9], np.int32)
+    offsets = torch.from_numpy(off).to(DEV)
+    x = acts(g, 4, 512, dtype) * 0.1
+    rows = torch.tensor([0, 3, 1, 2, -1, 4, 0, 1, 3, 2, 2], dtype=torch.int32, device=DEV)
+    y = B.grouped_linear_f8(x, q, s, offsets, rows)
+    check_grouped(y, x, q, s, off, rows.cpu().numpy(), dtype)
+    assert torch.equal(y, B.grouped_linear_f8(B.quantise_f8(x), q, s, offsets, rows, out_dtype=dtype))
+
+
 def test_grouped_without_rows():
     g = rng(10)
     q, s = weight(g, 64, 128, "e8m0", experts=3)

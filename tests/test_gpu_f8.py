@@ -169,10 +169,11 @@ def test_quantise_ties_subnormals_and_every_value():
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("tokens", [3, 40, 200])
-def test_a_row_with_a_number_that_is_none_spoils_itself_alone(bad, tokens):
+@pytest.mark.parametrize("inn", [700, 704])   # 704: few rows are brought to 8 bits by the product itself
+def test_a_row_with_a_number_that_is_none_spoils_itself_alone(bad, tokens, inn):
     g = rng(4)
-    q, s = weight(g, 200, 700, "e8m0")
-    x = acts(g, tokens, 700, F16)
+    q, s = weight(g, 200, inn, "e8m0")
+    x = acts(g, tokens, inn, F16)
     clean = B.linear_f8(x, q, s)
     x[1, 333] = bad
     y = B.linear_f8(x, q, s)
@@ -218,6 +219,23 @@ def test_strides_and_alignment(tokens):
     far = torch.full((out, 512), 0x7F, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
     far.view(torch.uint8)[:, :inn] = q.view(torch.uint8)
     assert torch.equal(B.linear_f8(base[:, :inn], far[:, :inn], s), B.linear_f8(base[:, :inn], q, s))
+
+
+@pytest.mark.parametrize("scales", ["e8m0", "f32"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["f16", "bf16", "f32"])
+@pytest.mark.parametrize("tokens,out,inn", [(1, 40, 16), (1, 512, 144), (3, 1000, 1040), (16, 333, 2048), (7, 5000, 272)])
+def test_few_rows_are_the_rows_quantised_before(tokens, out, inn, dtype, gated, scales):
+    """what the product itself brings to 8 bits is what the quantiser makes: the same bits, in the same order of sums; also from rows apart"""
+    g = rng(tokens + inn)
+    q, s = weight(g, out, inn, scales)
+    width = inn * (2 if gated else 1)
+    x = acts(g, tokens, width + 16, dtype)[:, 8 : 8 + width]
+    x[0, : min(inn, 128)] = 0   # a block of zeros
+    for out_dtype in (BF16, F32):
+        want = B.linear_f8(B.quantise_f8(x, gated=gated), q, s, out_dtype=out_dtype)
+        assert torch.equal(B.linear_f8(x, q, s, gated=gated, out_dtype=out_dtype), want)
+        assert torch.equal(B.linear_f8(x.contiguous(), q, s, gated=gated, out_dtype=out_dtype), want)
 
 
 def test_no_tokens():
@@ -284,5 +302,5 @@ def test_refusals():
         B.linear_f8(x, odd, s)
     assert e.value.code == -4
     with pytest.raises(B.BitStackError) as e:
-        B.linear_f8(x, q, s, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+        B.linear_f8(x.repeat(20, 1), q, s, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     assert e.value.code == -6
