@@ -34,51 +34,67 @@ __device__ __forceinline__ unsigned route_key(float l) {
 }
 __device__ __forceinline__ float route_value(unsigned key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
+// Over a wavefront, by row operations: each adds what lies 1, 2, 4, 8 lanes before, then the rows' last lanes; 0 where nothing lies
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_before(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+template <class OP>
+__device__ __forceinline__ int wave_all(int v, OP op) {
+    v = op(v, from_before<0x111, 0xf>(v));   // row_shr:1
+    v = op(v, from_before<0x112, 0xf>(v));
+    v = op(v, from_before<0x114, 0xf>(v));
+    v = op(v, from_before<0x118, 0xf>(v));
+    v = op(v, from_before<0x142, 0xa>(v));   // row_bcast:15
+    v = op(v, from_before<0x143, 0xc>(v));   // row_bcast:31
+    return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+    return unsigned(wave_all(int(v), [](int a, int b) { return int(max(unsigned(a), unsigned(b))); }));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
+    return __int_as_float(wave_all(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
 }
 
-// NL: experts per lane.  The j-th lane ends with the j-th choice (-1: none) and its weight.
+// A token's keys, NL to a lane
 template <int T, int NL>
-__device__ __forceinline__ void choose(const RouteParams& p, int token, int lane, int& expert, float& weight) {
+__device__ __forceinline__ void load_keys(const RouteParams& p, int token, int lane, unsigned (&key)[NL]) {
     const typename Elem<T>::type* const l = static_cast<const typename Elem<T>::type*>(p.logits) + size_t(token) * p.ld;
-    unsigned key[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
         const int e = i * 64 + lane;
         key[i] = e < p.experts ? route_key(float(l[e])) : 0;
     }
-    unsigned taken[NL];
+}
+
+// The j-th lane ends with the j-th choice (-1: none) and its weight.
+template <int NL>
+__device__ __forceinline__ void choose(const RouteParams& p, const unsigned (&key)[NL], int lane, int& expert, float& weight) {
+    unsigned left[NL];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) taken[i] = key[i];
-    unsigned mine = 0;
+    for (int i = 0; i < NL; ++i) left[i] = key[i];
+    unsigned mine = 0, first = 0;
     expert = -1;
     for (int j = 0; j < p.top_k; ++j) {
-        unsigned long long best = 0;
+        unsigned best = 0;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {   // the larger key, of equal ones the lower index
-            const unsigned long long c = (unsigned long long)(taken[i]) << 32 | (0xffffffffu - unsigned(i * 64 + lane));
-            best = c > best ? c : best;
-        }
+        for (int i = 0; i < NL; ++i) best = max(best, left[i]);
+        best = wave_max(best);
+        if (best == 0) break;
+        if (j == 0) first = best;
+        int e = -1;   // of equal ones the lowest
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const unsigned long long o = __shfl_xor(best, d);
-            best = o > best ? o : best;
+        for (int i = NL - 1; i >= 0; --i) {
+            const unsigned long long here = __ballot(left[i] == best);
+            if (here) e = i * 64 + __builtin_ctzll(here);
         }
-        const unsigned k = unsigned(best >> 32);
-        if (k == 0) break;
-        const int e = int(0xffffffffu - unsigned(best));
         if (lane == j) {
-            mine = k;
+            mine = best;
             expert = e;
         }
 #pragma unroll
         for (int i = 0; i < NL; ++i)
-            if (i * 64 + lane == e) taken[i] = 0;
+            if (i * 64 + lane == e) left[i] = 0;
     }
-    const float most = route_value(unsigned(__shfl(int(mine), 0)));
+    const float most = route_value(first);
     const float share = mine ? expf(route_value(mine) - most) : 0.0f;
     float total;
     if (p.renormalise) {
@@ -101,16 +117,27 @@ struct RouteLds {
 
 template <int T, int NL>
 __device__ __forceinline__ void choose_step(const RouteParams& p, RouteLds& s, int token0) {
-    const int lane = threadIdx.x & 63;
-    for (int t = threadIdx.x >> 6; t < kRouteStep && token0 + t < p.tokens; t += 16) {
-        int expert;
-        float weight;
-        choose<T, NL>(p, token0 + t, lane, expert, weight);
-        if (lane < p.top_k) {
-            const size_t at = size_t(token0 + t) * p.top_k + lane;
-            p.chosen[at] = expert;
-            p.weights[at] = weight;
-            s.chosen[t * p.top_k + lane] = short(expert);
+    // four tokens a wavefront; their logits are requested together where registers allow
+    constexpr int kEach = kRouteStep / 16, kTogether = NL <= 4 ? kEach : 1;
+    const int lane = threadIdx.x & 63, t0 = (threadIdx.x >> 6) * kEach;
+#pragma unroll
+    for (int g = 0; g < kEach; g += kTogether) {
+        unsigned key[kTogether][NL];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) load_keys<T, NL>(p, min(token0 + t0 + g + k, p.tokens - 1), lane, key[k]);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const int t = t0 + g + k;
+            if (token0 + t >= p.tokens) break;
+            int expert;
+            float weight;
+            choose<NL>(p, key[k], lane, expert, weight);
+            if (lane < p.top_k) {
+                const size_t at = size_t(token0 + t) * p.top_k + lane;
+                p.chosen[at] = expert;
+                p.weights[at] = weight;
+                s.chosen[t * p.top_k + lane] = short(expert);
+            }
         }
     }
 }
@@ -209,10 +236,22 @@ __global__ __launch_bounds__(1024) void k_route_place(RouteParams p) {
     RouteLds& s = *reinterpret_cast<RouteLds*>(smem);
     for (int e = threadIdx.x; e < p.experts; e += 1024) s.count[e] = s.base[e] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < p.chunks * p.experts; i += 1024) {
-        const int chunk = i / p.experts, e = i - chunk * p.experts, c = p.counts[i];
-        atomicAdd(&s.count[e], c);
-        if (chunk < int(blockIdx.x)) atomicAdd(&s.base[e], c);
+    // the counts of all chunks: as many threads as there are experts to a row of them, eight requests at a time
+    const int parts = max(1, 1024 / p.experts);
+    for (int e = threadIdx.x % p.experts, part = threadIdx.x / p.experts; part < parts && e < p.experts; part += parts) {
+        int all = 0, before = 0;
+        for (int c0 = part; c0 < p.chunks; c0 += 8 * parts) {
+            int c[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[k] = c0 + k * parts < p.chunks ? p.counts[size_t(c0 + k * parts) * p.experts + e] : 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                all += c[k];
+                before += c0 + k * parts < int(blockIdx.x) ? c[k] : 0;
+            }
+        }
+        atomicAdd(&s.count[e], all);   // whole numbers: the order does not matter
+        atomicAdd(&s.base[e], before);
     }
     __syncthreads();
     bases(p, s);

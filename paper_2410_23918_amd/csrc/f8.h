@@ -28,7 +28,7 @@ struct F8Params {
     size_t ldw, ldy;
     int out, in, kb, kp, ks;   // kb: blocks of columns, kp = 128 kb, ks = kb rounded up to 4
     int x_rows, rows;          // rows of x, of y
-    int x_dtype, gated;        // BITSTACK_T_F8, or the type of what is to be brought to 8 bits on the way
+    int x_dtype;               // BITSTACK_T_F8, or the type of what is to be brought to 8 bits on the way
     unsigned x_bytes, x_ld;    // extent of x
     float* part;               // partial sums of the column slices
     int slices, slice_blocks;  // of the columns; blocks in one
@@ -93,7 +93,8 @@ __device__ __forceinline__ unsigned f8_x4(float a, float b, float c, float d) {
 }
 // |v| as an integer that orders like it, NaN and infinity above all others
 __device__ __forceinline__ unsigned f8_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-__device__ __forceinline__ float f8_gate(float g, float u) { return __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), u); }
+// g / (1 + exp(-g)) u, by the hardware's exp2 and reciprocal (1 ulp each): relative error (3 + |g| / 2) 2^-24
+__device__ __forceinline__ float f8_gate(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
 
 // The work list of a product grouped by expert: made by the launch that brings the activations to 8 bits, or (rows 0 there) by itself
 struct F8WorkList {
@@ -107,7 +108,8 @@ hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int ou
                                      unsigned char* s, hipStream_t st);
 // Kernel and column slices of a product, from sizes alone
 struct F8Plan {
-    int kernel, slices, tile_rows, n_tiles;   // tile_rows: rows of y in a tile
+    int kernel, slices, tile_rows, n_tiles;   // tile_rows: rows of y in a tile; n_tiles: tiles of y's rows, at most
+    int tiles;                                // of the weight's rows and y's
     size_t part_bytes;                        // partial sums
 };
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact);

@@ -55,13 +55,14 @@ int check_call(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, int y
     return check_rows(*x, w->in);
 }
 
-// Does the product bring the activations to 8 bits itself?  Few rows: every workgroup does so anew, for each 16 or 64 rows of the weight.  Their
-// 16-byte pieces have to be whole and in reach of 31-bit offsets.  (One token through 1024 x 4096: see the measurements at k_f8_slices.)
-bool raw_rows(const bitstack_f8_rows_t& x, int in, int y_rows, const F8Plan& plan) {
-    if (x.dtype == BITSTACK_T_F8 || y_rows > 16 || plan.tile_rows != 16 || in % 16 != 0 || x.rows < 1) return false;
-    const size_t size = type_size(x.dtype);
-    return !misaligned(x.x, 16) && (x.rows == 1 || x.ld * size % 16 == 0) && (size_t(x.rows - 1) * x.ld + (size_t(in) << x.gated)) * size <= kMaxRowBytes &&
-           (x.rows == 1 || x.ld * size <= kMaxRowBytes);
+// Does the product bring the activations to 8 bits itself?  A few rows of 16 bits, not gated, in no groups (their work list is made by the launch that
+// quantises), in whole 16-byte pieces within reach of 31-bit offsets.  Every workgroup converts all columns anew, kb blocks for each tile of
+// 16 or 64 rows of the weight: up to 64 blocks on a compute unit (measurements at k_f8_slices; fp32 rows and gated ones take two to six times as
+// long there as a launch more).
+bool raw_rows(const bitstack_f8_rows_t& x, const bitstack_f8_weight_t& w, int y_rows, const F8Plan& plan, bool grouped) {
+    if (grouped || x.gated || (x.dtype != BITSTACK_T_F16 && x.dtype != BITSTACK_T_BF16) || y_rows > 16 || plan.tile_rows != 16 || w.in % 16 != 0) return false;
+    if (size_t(plan.tiles) * ((w.in + kF8Block - 1) / kF8Block) > 64 * 256) return false;
+    return !misaligned(x.x, 16) && (x.rows == 1 || (x.ld % 8 == 0 && x.ld <= kMaxRowBytes / 2)) && (size_t(x.rows - 1) * x.ld + w.in) * 2 <= kMaxRowBytes;
 }
 
 int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, void* y,
@@ -74,7 +75,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
     const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32);
-    const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, w->in, y_rows, plan);
+    const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
     const Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {
         if (!workspace) return BITSTACK_E_NULL;
@@ -100,12 +101,10 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
         p.x = static_cast<const unsigned char*>(x->x);
         p.xs = static_cast<const unsigned char*>(x->scales);
     } else if (raw) {
-        const size_t size = type_size(x->dtype);
         p.x = static_cast<const unsigned char*>(x->x);
         p.x_dtype = x->dtype;
-        p.gated = x->gated;
-        p.x_bytes = unsigned((size_t(x->rows - 1) * x->ld + (size_t(w->in) << x->gated)) * size);
-        p.x_ld = x->rows > 1 ? unsigned(x->ld * size) : 0;
+        p.x_bytes = unsigned((size_t(x->rows - 1) * x->ld + w->in) * 2);
+        p.x_ld = x->rows > 1 ? unsigned(x->ld * 2) : 0;
     }
     p.w = static_cast<const unsigned char*>(w->q);
     p.ws = w->scales;
@@ -179,7 +178,7 @@ size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int 
 size_t bitstack_f8_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, int y_rows, int y_dtype, int grouped) {
     if (!x || !w || check_call(x, w, y_rows, y_dtype) || y_rows == 0) return 0;
     const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, grouped != 0, y_dtype == BITSTACK_T_F32);
-    return workspace_of(x->rows, w->in, plan, x->dtype == BITSTACK_T_F8 || raw_rows(*x, w->in, y_rows, plan), grouped != 0).total;
+    return workspace_of(x->rows, w->in, plan, x->dtype == BITSTACK_T_F8 || raw_rows(*x, *w, y_rows, plan, grouped != 0), grouped != 0).total;
 }
 
 int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, void* y, int y_dtype, size_t ld_y,

@@ -152,29 +152,18 @@ __device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[
     }
 }
 
-// The activations of a lane as they come: 32 columns of a token in a block, of type T, and (GATED) as many values to be gated
+// The activations of a lane as they come, 32 columns of a token in a block, of type T (16 bits), to e4m3: what k_f8_quantise makes of them
 constexpr int kRowsF8 = BITSTACK_T_F8;
-template <int T, bool GATED>
-struct RawColumns {
-    static constexpr int kPieces = 32 * int(sizeof(typename Elem<T>::type)) / 16;   // of 16 bytes
-    v4i v[kPieces], u[GATED ? kPieces : 1];
-};
-template <bool GATED>
-struct RawColumns<kRowsF8, GATED> {};
-template <int T, bool GATED>
-__device__ __forceinline__ void columns_to_f8(const RawColumns<T, GATED>& r, v8i& x, int& scale) {
-    typedef typename Elem<T>::type E;
+template <int T>
+__device__ __forceinline__ void columns_to_f8(const v4i (&raw)[4], v8i& x, int& scale) {
+    typedef typename Elem<T>::type piece __attribute__((ext_vector_type(8)));
     float v[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        constexpr int K = Elem<T>::kPer16;
-        typedef E piece __attribute__((ext_vector_type(K)));
-        v[i] = float(__builtin_bit_cast(piece, r.v[i / K])[i % K]);
-        if constexpr (GATED) v[i] = f8_gate(v[i], float(__builtin_bit_cast(piece, r.u[i / K])[i % K]));
-    }
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) m = max(m, f8_magnitude(v[i]));
+    for (int i = 0; i < 32; ++i) {
+        v[i] = float(__builtin_bit_cast(piece, raw[i / 8])[i % 8]);
+        m = max(m, f8_magnitude(v[i]));
+    }
     m = max(m, unsigned(__shfl_xor(int(m), 16)));   // the other lanes of the token
     m = max(m, unsigned(__shfl_xor(int(m), 32)));
     const bool bad = m >= 0x7f800000u;
@@ -187,8 +176,9 @@ __device__ __forceinline__ void columns_to_f8(const RawColumns<T, GATED>& r, v8i
 // A tile of 16 FR rows of the weight x 16 FT tokens.  The eight wavefronts of a workgroup take every eighth block of columns each, straight
 // from memory into registers (nothing of a tile is read by two of them), DEPTH blocks ahead; their sums meet in LDS.
 //   T: type of the activations.  With one fragment of tokens they may come as they are and are brought to 8 bits on the way (a block of a token lies
-// in four lanes), by every workgroup anew: one launch instead of two.
-template <int FR, int FT, int DEPTH, int MODE, int T, bool GATED>
+// in four lanes), by every workgroup anew: one launch instead of two.  One token through 1024 x 4096: 7.0 us, 5.5 and 2.4 + a launch for the rows
+// quantised before; 14336 x 4096 16.7, 16.2 and 2.4; 4096 x 14336, where 256 workgroups convert 112 blocks each, 20.4, 14.4 and 2.5.
+template <int FR, int FT, int DEPTH, int MODE, int T>
 __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
     constexpr bool kRaw = T != kRowsF8;
     static_assert(!kRaw || FT == 1, "one fragment of raw tokens");
@@ -237,7 +227,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
         }
         struct Stage {
             v4i w[FR][2], x[FT][2];
-            RawColumns<T, GATED> raw;
+            v4i raw[kRaw ? 4 : 1];
             int xs[FT];
             int sw;
         };
@@ -253,17 +243,12 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
 #pragma unroll
             for (int i = 0; i < FT; ++i) {
                 if constexpr (kRaw) {
-                    constexpr int kHalf = RawColumns<T, GATED>::kPieces / 2;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int c = b * 128 + h * 64 + kg * 16;
-                        const unsigned at = (x_off[i] + unsigned(c) * unsigned(sizeof(typename Elem<T>::type))) | oob | (c < p.in ? 0u : 0x80000000u);
+                        const unsigned at = (x_off[i] + unsigned(c) * 2u) | oob | (c < p.in ? 0u : 0x80000000u);
 #pragma unroll
-                        for (int k = 0; k < kHalf; ++k) {
-                            s.raw.v[h * kHalf + k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int(at + k * 16), 0, 0));
-                            if constexpr (GATED)
-                                s.raw.u[h * kHalf + k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int(at + k * 16), p.in * int(sizeof(typename Elem<T>::type)), 0));
-                        }
+                        for (int k = 0; k < 2; ++k) s.raw[h * 2 + k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, int(at + k * 16), 0, 0));
                     }
                     continue;
                 }
@@ -287,7 +272,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
             for (int j = 0; j < FR; ++j) w[j] = join(s.w[j][0], s.w[j][1]);
 #pragma unroll
             for (int i = 0; i < FT; ++i) {
-                if constexpr (kRaw) columns_to_f8<T, GATED>(s.raw, x[i], s.xs[i]);
+                if constexpr (kRaw) columns_to_f8<T>(s.raw, x[i], s.xs[i]);
                 else x[i] = join(s.x[i][0], s.x[i][1]);
             }
             multiply_all<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32, [](int) {});
@@ -615,27 +600,25 @@ static hipError_t tiles(F8Params p, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int FR, int FT, int DEPTH, int MODE, int T, bool GATED>
+template <int FR, int FT, int DEPTH, int MODE, int T>
 static void slices_as(const F8Params& p, hipStream_t st) {
     const int nrt = (p.out + 16 * FR - 1) / (16 * FR);
-    hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, MODE, T, GATED>), dim3(unsigned(8 * ((nrt + 7) / 8)) * unsigned(p.n_tiles)), dim3(512), 0, st, p);
+    hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, MODE, T>), dim3(unsigned(8 * ((nrt + 7) / 8)) * unsigned(p.n_tiles)), dim3(512), 0, st, p);
 }
-template <int FR, int FT, int DEPTH, int T, bool GATED>
-static void slices_of(const F8Params& p, hipStream_t st) {
-    if (p.y_dtype == BITSTACK_T_F32) slices_as<FR, FT, DEPTH, kModeExact, T, GATED>(p, st);
-    else if (p.ws_f32) slices_as<FR, FT, DEPTH, kModeF32, T, GATED>(p, st);
-    else slices_as<FR, FT, DEPTH, kModeE8M0, T, GATED>(p, st);
+template <int FR, int FT, int DEPTH, int T>
+static hipError_t slices_of(const F8Params& p, hipStream_t st) {
+    if (p.y_dtype == BITSTACK_T_F32) slices_as<FR, FT, DEPTH, kModeExact, T>(p, st);
+    else if (p.ws_f32) slices_as<FR, FT, DEPTH, kModeF32, T>(p, st);
+    else slices_as<FR, FT, DEPTH, kModeE8M0, T>(p, st);
+    return hipGetLastError();
 }
 template <int FR, int FT, int DEPTH>
 static hipError_t slices(const F8Params& p, hipStream_t st) {
     if constexpr (FT == 1) {
-        if (p.x_dtype == BITSTACK_T_F16) p.gated ? slices_of<FR, FT, DEPTH, BITSTACK_T_F16, true>(p, st) : slices_of<FR, FT, DEPTH, BITSTACK_T_F16, false>(p, st);
-        else if (p.x_dtype == BITSTACK_T_BF16) p.gated ? slices_of<FR, FT, DEPTH, BITSTACK_T_BF16, true>(p, st) : slices_of<FR, FT, DEPTH, BITSTACK_T_BF16, false>(p, st);
-        else if (p.x_dtype == BITSTACK_T_F32) p.gated ? slices_of<FR, FT, DEPTH, BITSTACK_T_F32, true>(p, st) : slices_of<FR, FT, DEPTH, BITSTACK_T_F32, false>(p, st);
-        if (p.x_dtype != BITSTACK_T_F8) return hipGetLastError();
+        if (p.x_dtype == BITSTACK_T_F16) return slices_of<FR, FT, DEPTH, BITSTACK_T_F16>(p, st);
+        if (p.x_dtype == BITSTACK_T_BF16) return slices_of<FR, FT, DEPTH, BITSTACK_T_BF16>(p, st);
     }
-    slices_of<FR, FT, DEPTH, BITSTACK_T_F8, false>(p, st);
-    return hipGetLastError();
+    return slices_of<FR, FT, DEPTH, BITSTACK_T_F8>(p, st);
 }
 
 // Kernels by their tile (rows of the weight x of y): 16 x 16, 64 x 16, 64 x 32, 64 x 64 without LDS, 128 x 64, 128 x 128, 256 x 128, 256 x 256
@@ -675,7 +658,7 @@ static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, 
 // Kernel and column slices of a product, from sizes alone (the workspace holds the partial sums)
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact) {
     const int forced = g_forced.load(), kb = (in + 127) / 128;
-    F8Plan plan{kShapes[0].kernel, 1, 0, 0, 0};
+    F8Plan plan{kShapes[0].kernel, 1, 0, 0, 0, 0};
     double best = 1e30;
     for (const F8KernelShape& k : kShapes) {
         if (!forced && rows <= 16 && k.toks > 16) break;   // never faster
@@ -685,7 +668,7 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact)
             const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact);
             if (us >= best) continue;
             best = us;
-            plan = {k.kernel, slices, k.toks, 0, 0};
+            plan = {k.kernel, slices, k.toks, 0, 0, 0};
         }
     }
     if (forced && forced % 1024 == plan.kernel && plan.kernel > kSlices64) plan.slices = std::max(1, std::min(forced / 1024, kb));
@@ -697,7 +680,9 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact)
             plan.tile_rows = k.toks;
             // every group's rows, rounded up to tiles, and those of the rows past the last group
             plan.n_tiles = grouped ? rows / k.toks + 1 + std::min(rows, experts) : (rows + k.toks - 1) / k.toks;
-            if (plan.slices > 1) plan.part_bytes = size_t(plan.slices) * ((out + k.rows - 1) / k.rows) * plan.n_tiles * (k.rows * k.toks * 4);
+            const size_t tiles = size_t((out + k.rows - 1) / k.rows) * plan.n_tiles;
+            plan.tiles = int(std::min<size_t>(tiles, 0x7fffffff));
+            if (plan.slices > 1) plan.part_bytes = plan.slices * tiles * (k.rows * k.toks * 4);
         }
     return plan;
 }

@@ -59,9 +59,10 @@ __device__ void make_work_list(const F8WorkList& l) {
     }
 }
 
-// Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row, whose scales are one word.
-// Bound by memory: x is read once and q written once, 16 and 8 bytes a lane.  The first workgroup makes the work list where there is one.
-template <int T, bool GATED>
+// Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row, whose scales are one word, WORDS
+// times over.  Bound by memory: x is read once and q written once, 16 and 8 bytes a lane and word.  The first workgroup makes the work list where
+// there is one.
+template <int T, bool GATED, int WORDS>
 __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, int vec, unsigned char* q,
                                                      unsigned* s, int kp, F8WorkList list) {
     if (list.offsets && blockIdx.x == 0) {
@@ -69,38 +70,40 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
         return;
     }
     const int lane = threadIdx.x & 63;
-    const int per_row = (kp + 511) / 512;   // wavefronts
+    const int per_row = (kp + 512 * WORDS - 1) / (512 * WORDS);   // wavefronts
     const size_t wave = (size_t(blockIdx.x - (list.offsets ? 1 : 0)) * 256 + threadIdx.x) >> 6;
-    const int row = int(wave / per_row), word = int(wave % per_row);
+    const int row = int(wave / per_row), word0 = int(wave % per_row) * WORDS;
     if (row >= rows) return;
-    const int col = word * 512 + lane * 8;
-    float v[8];
-    const typename Elem<T>::type* const from = x + size_t(row) * ld + col;
-    load_elems<T, 8>(from, in - col, vec, v);
-    if constexpr (GATED) {
-        float u[8];
-        load_elems<T, 8>(from + in, in - col, vec, u);
+    float v[WORDS][8], u[GATED ? WORDS : 1][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = f8_gate(v[i], u[i]);
+    for (int k = 0; k < WORDS; ++k) {   // all requests first
+        const int col = (word0 + k) * 512 + lane * 8;
+        const typename Elem<T>::type* const from = x + size_t(row) * ld + col;
+        load_elems<T, 8>(from, in - col, vec, v[k]);
+        if constexpr (GATED) load_elems<T, 8>(from + in, in - col, vec, u[k]);
     }
-    unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, f8_magnitude(v[i]));
+    for (int k = 0; k < WORDS; ++k) {
+        const int word = word0 + k, col = word * 512 + lane * 8;
+        if (word * 512 >= kp) break;
+        unsigned m = 0;
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) m = max(m, unsigned(__shfl_xor(int(m), d, 16)));
-    uint2 bytes;
-    int e = 127;
-    if (m >= 0x7f800000u) {
-        bytes = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);   // a NaN or an infinity in the block: NaN
-    } else {
-        e = f8_exponent(__uint_as_float(m));
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (GATED) v[k][i] = f8_gate(v[k][i], u[k][i]);
+            m = max(m, f8_magnitude(v[k][i]));
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) m = max(m, unsigned(__shfl_xor(int(m), d, 16)));
+        const bool bad = m >= 0x7f800000u;   // a NaN or an infinity in the block: NaN
+        const int e = bad ? 127 : f8_exponent(__uint_as_float(m));
         const float r = f8_inverse(e);
-        bytes = make_uint2(f8_x4(v[0] * r, v[1] * r, v[2] * r, v[3] * r), f8_x4(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
+        const uint2 bytes = bad ? make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu)
+                                : make_uint2(f8_x4(v[k][0] * r, v[k][1] * r, v[k][2] * r, v[k][3] * r), f8_x4(v[k][4] * r, v[k][5] * r, v[k][6] * r, v[k][7] * r));
+        if (col < kp) *reinterpret_cast<uint2*>(q + size_t(row) * kp + col) = bytes;
+        const unsigned four = unsigned(__builtin_amdgcn_readlane(e, 0)) | unsigned(__builtin_amdgcn_readlane(e, 16)) << 8 |
+                              unsigned(__builtin_amdgcn_readlane(e, 32)) << 16 | unsigned(__builtin_amdgcn_readlane(e, 48)) << 24;
+        if (lane == 0) s[size_t(word) * rows + row] = four;
     }
-    if (col < kp) *reinterpret_cast<uint2*>(q + size_t(row) * kp + col) = bytes;
-    const unsigned four = unsigned(__builtin_amdgcn_readlane(e, 0)) | unsigned(__builtin_amdgcn_readlane(e, 16)) << 8 |
-                          unsigned(__builtin_amdgcn_readlane(e, 32)) << 16 | unsigned(__builtin_amdgcn_readlane(e, 48)) << 24;
-    if (lane == 0) s[size_t(word) * rows + row] = four;
 }
 
 // A workgroup brings a block of 128 rows x 128 columns to 8 bits: sixteen lanes a row, sixteen rows a pass, the values in registers between
@@ -148,11 +151,14 @@ static void quantise(const void* x, size_t ld, int rows, int in, bool gated, uns
     const int kp = (in + 127) / 128 * 128;
     // the halves of a gated row begin `in` elements apart
     const int vec = vector_rows(x, ld, sizeof(E)) && (!gated || size_t(in) * sizeof(E) % 16 == 0);
-    const size_t waves = size_t(rows) * ((kp + 511) / 512);
-    const unsigned grid = unsigned((waves + 3) / 4) + (list.offsets ? 1 : 0);
     unsigned* const words = reinterpret_cast<unsigned*>(s);
-    if (gated) hipLaunchKernelGGL((k_f8_quantise<T, true>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list);
-    else hipLaunchKernelGGL((k_f8_quantise<T, false>), dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list);
+    // with four words a wavefront there is enough to do for all compute units
+    const int each = size_t(rows) * ((kp + 2047) / 2048) >= 4096 ? 4 : 1;
+    const size_t waves = size_t(rows) * ((kp + 512 * each - 1) / (512 * each));
+    const unsigned grid = unsigned((waves + 3) / 4) + (list.offsets ? 1 : 0);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list); };
+    if (gated) each == 4 ? go(&k_f8_quantise<T, true, 4>) : go(&k_f8_quantise<T, true, 1>);
+    else each == 4 ? go(&k_f8_quantise<T, false, 4>) : go(&k_f8_quantise<T, false, 1>);
 }
 
 hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,
