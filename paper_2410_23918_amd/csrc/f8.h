@@ -34,7 +34,6 @@ struct F8Params {
     int slices, slice_blocks;  // of the columns; blocks in one
     int n_tiles;               // tiles of rows (an upper bound where they are grouped)
     int y_dtype, ws_f32;       // ws_f32: fp32 scales
-    int touch_w, touch_x;      // k_f8_tile: how many workgroups share the touching of the weight's lines, of the tokens' (powers of two)
     int y_vec, y_vec16;        // four outputs, or 16 bytes of them, may be stored at once
 };
 

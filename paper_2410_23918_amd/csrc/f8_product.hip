@@ -322,7 +322,51 @@ struct F8TileShape {
     static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % 64 == 0 && kToks <= 256, "whole loads, one weight scale a wavefront, scales for the first four wavefronts");
 };
 
-template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
+// A tile's sums leave the kernel (all LDS is free).  FR x FT fragments a wavefront, WR x WT wavefronts.
+template <class S, int FR, int FT, int WR>
+__device__ __forceinline__ void finish_tile(const F8Params& p, unsigned char* smem, const v4f (&acc)[FR][FT], size_t tile, int n0, int row0, int rows) {
+    const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % WR, wt = wave / WR;
+    if (p.slices > 1) {   // partial sums, as the lanes hold them: k_f8_join adds them up
+        v4f* const to = reinterpret_cast<v4f*>(p.part) + (tile * 8 + wave) * (FR * FT * 64) + lane;
+#pragma unroll
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int i = 0; i < FT; ++i) to[(j * FT + i) * 64] = acc[j][i];
+        return;
+    }
+    // the tile's outputs meet in LDS, token by token, and leave in 16-byte pieces
+    constexpr int kSize = S::kSize, kLd = S::kOutLd;
+    unsigned char* const mine = smem + (wt * 16 * FT + ln) * kLd + (wr * 16 * FR + kg * 4 * FR) * kSize;
+    auto put = [&](auto turn) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FT; ++i)
+#pragma unroll
+            for (int j = 0; j < FR; ++j) turn(acc[j][i], mine + i * 16 * kLd + j * 4 * kSize);
+    };
+    if constexpr (S::kSize == 4) put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v4f*>(to) = v; });
+    else if (p.y_dtype == BITSTACK_T_F16) put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v2u*>(to) = pack4<_Float16>(v); });
+    else put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v2u*>(to) = pack4<__bf16>(v); });
+    __syncthreads();
+    constexpr int kPieces = S::kRows * kSize / 16, kEach = 16 / kSize;
+    for (int k = tid; k < S::kToks * kPieces; k += 64 * S::kWaves) {
+        const int tok = k / kPieces, piece = k % kPieces, n = n0 + piece * kEach;
+        if (tok >= rows) break;
+        if (n >= p.out) continue;
+        const unsigned char* const from = smem + tok * kLd + piece * 16;
+        unsigned char* const y = static_cast<unsigned char*>(p.y) + (size_t(row0 + tok) * p.ldy + n) * kSize;
+        if (p.y_vec16 && n + kEach <= p.out) {
+            *reinterpret_cast<v4i*>(y) = *reinterpret_cast<const v4i*>(from);
+        } else {
+            for (int e = 0; e < kEach && n + e < p.out; ++e) {
+                if constexpr (kSize == 4) reinterpret_cast<float*>(y)[e] = reinterpret_cast<const float*>(from)[e];
+                else reinterpret_cast<unsigned short*>(y)[e] = reinterpret_cast<const unsigned short*>(from)[e];
+            }
+        }
+    }
+}
+
+template <int FR, int FT, int WR, int WT, int MODE>
 __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     typedef F8TileShape<FR, FT, WR, WT, MODE> S;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -357,7 +401,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         const v4i xrs = buffer_over(p.x, unsigned(p.x_rows) * unsigned(p.kp));
         const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
         constexpr int kWLoads = S::kRows / 8 / S::kWaves, kXLoads = S::kToks / 8 / S::kWaves;
-        constexpr int kLoads = kWLoads + kXLoads + (TOUCH ? 1 : 0);   // of a step; one more for those that load scales
+        constexpr int kLoads = kWLoads + kXLoads;   // of a step; one more for those that load scales
         auto w_turn = [](int r) { return (r >> 1 & 1) | (r / (4 * FR) & 3) << 1; };
         unsigned x_off[kXLoads];
         // load i of the weight brings rows 8 (wave kWLoads + i) .. + 7 of the tile; past the last row the descriptor ends, and zeros arrive
@@ -379,22 +423,6 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         const unsigned s_off = unsigned(s_at) < unsigned(p.x_rows) ? unsigned(s_at) * 4u : 0x80000000u;
         const unsigned lds0 = lds_address(smem);
         const int ragged = p.in % 128;
-        // TOUCH: what is requested has a step and a half to arrive, less than a miss of the L2 takes.  So one of the workgroups that are on an XCD at a time
-        // and read the same rows touches each step's lines kTouch steps ahead (a line of 128 bytes a lane, into 256 bytes of LDS that nobody reads).  28672 x
-        // 8192, 2048 tokens: 460 -> 424 us.  Where all tiles are there at once, or few of them share rows, the touches cost more than
-        // they bring (14336 x 4096, 1024 tokens: 53 -> 56 us; 8 experts of 14336 x 4096, 2048 tokens twice: 325 -> 364).
-        constexpr int kTouch = 4;
-        const bool touch_w = wave * 64 < S::kRows;
-        const int touch_mask = (touch_w ? p.touch_w : p.touch_x) - 1, touch_mine = (touch_w ? place % per_row : place / per_row) & touch_mask;
-        unsigned touch_off = 0x80000000u;
-        if (TOUCH) {
-            if (touch_w) {
-                touch_off = unsigned(64 * wave + lane) * unsigned(p.ldw);
-            } else if (wave * 64 < S::kRows + S::kToks) {
-                const int at = x_row(64 * wave - S::kRows + lane);
-                if (unsigned(at) < unsigned(p.x_rows)) touch_off = unsigned(at) * unsigned(p.kp);
-            }
-        }
         int q = first;   // next step to request; past the last one zeros arrive
         unsigned q_dst = lds0;
         // part `part` of `parts` of a step's loads; scales_too: in the first four wavefronts
@@ -416,11 +444,6 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             if (scales_too && part == 0)
                 load4_to_lds(xsrs, q_dst + (S::kRows + S::kToks) * 128u + unsigned(wave) * 256u, s_off | none, q < last ? unsigned(q >> 2) * unsigned(p.x_rows) * 4u : 0u);
             if (part == parts - 1) {
-                if (TOUCH) {
-                    const int b = q + kTouch;
-                    const bool on = b < last && (b & touch_mask) == touch_mine;
-                    load4_to_lds(touch_w ? wrs : xrs, lds0 + S::kRing * S::kStep, on ? touch_off : 0x80000000u, on ? unsigned(b) * 128u : 0u);
-                }
                 ++q;
                 q_dst = q_dst == lds0 + (S::kRing - 1) * S::kStep ? lds0 : q_dst + S::kStep;
             }
@@ -472,9 +495,9 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             __builtin_amdgcn_s_setprio(0);
         };
         // A loop for each side: with branches inside, the compiler moves the products past the barriers.  kAhead: loads that may still be on their way when a
-        // step has to be there, those of later steps and its own touch, the last of its loads.
+        // step has to be there, those of later ones.
         if (!late) {
-            constexpr int kAhead = (S::kRing - 2) * (kLoads + 1) + (TOUCH ? 1 : 0);
+            constexpr int kAhead = (S::kRing - 2) * (kLoads + 1);
 #pragma unroll
             for (int i = 0; i < S::kRing; ++i) request(true, 0, 1);
             loads_barrier<kAhead + kLoads + 1>();   // step 0
@@ -489,7 +512,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
             }
             lds_barrier();
         } else {
-            constexpr int kAhead = (S::kRing - 2) * kLoads + (TOUCH ? 1 : 0);
+            constexpr int kAhead = (S::kRing - 2) * kLoads;
 #pragma unroll
             for (int i = 0; i < S::kRing; ++i) request(false, 0, 1);
             loads_barrier<kAhead + kLoads>();   // step 0
@@ -507,44 +530,205 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
         }
         loads_barrier<0>();   // nothing may land in LDS any more
     }
-    if (p.slices > 1) {   // partial sums, as the lanes hold them: k_f8_join adds them up
-        v4f* const to = reinterpret_cast<v4f*>(p.part) + ((size_t(slice) * nrt * p.n_tiles + size_t(rt) * p.n_tiles + tt) * 8 + wave) * (FR * FT * 64) + lane;
+    finish_tile<S, FR, FT, WR>(p, smem, acc, size_t(slice) * nrt * p.n_tiles + size_t(rt) * p.n_tiles + tt, n0, row0, rows);
+}
+
+// The largest tile, 256 rows x 256 tokens, eight wavefronts of 128 x 64 that take turns as in k_f8_tile.  Two buffers for a step of both operands are all that LDS
+// has, and what is requested in the phase after a buffer's last read has less than two phases to arrive; all in one phase it also
+// comes faster than a compute unit takes it (16 clocks a load, 64 loads a step, a phase is 1024 clocks of products).  So the operands are
+// requested in turn: the weight in even phases; the tokens in odd ones, a step earlier, those that the first wavefronts read into the
+// buffer that these have just read, the others' into a ring of three.
+//   Up to 128 tokens the last four wavefronts have none and only load.
+//   28672 x 8192, 2048 tokens: 393 us, 2.45 PFLOP/s; the matrix cores work in 56 % of the clocks (both operands requested in one phase: 37 %, 460 us), of which
+// there are then 2.0 in a nanosecond and not 2.35: power is the bound.  Without the loads it takes 279 us, without the products 290.
+constexpr unsigned kBigW = 32768, kBigX = 16384, kBigS = 1024;                                          // bytes of a buffer
+constexpr unsigned kBigEarly = 2 * kBigW, kBigLate = kBigEarly + 2 * kBigX, kBigScales = kBigLate + 3 * kBigX;
+struct F8BigShape {
+    static constexpr int kWaves = 8, kRows = 256, kToks = 256, kSize = 2, kOutLd = kRows * kSize + 16;
+    static constexpr int kLds = int(kBigScales + 3 * kBigS);
+    static_assert(kLds <= 163840 && kToks * kOutLd <= kLds, "the output tile reuses the buffers");
+};
+template <int MODE>
+__global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
+    constexpr int FR = 8, FT = 4, WR = 2;
+    typedef F8BigShape S;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), side_wave = wave & 3;
+    const int wr = wave % WR;
+    const bool late = wave >= 4;
+    const int ln = lane & 15, kg = lane >> 4;
+    // ids are dealt round-robin to the 8 XCDs, whose L2s each fetch what their tiles read: every fourth row tile x every second token tile
+    const int nrt = (p.out + 255) / 256, per_row = (p.n_tiles + 1) / 2, per_slice = (nrt + 3) / 4 * per_row;
+    const int xcd = blockIdx.x & 7, slice = (blockIdx.x >> 3) / per_slice, place = (blockIdx.x >> 3) % per_slice;
+    const int rt = (xcd >> 1) + 4 * (place / per_row), tt = (xcd & 1) + 2 * (place % per_row);
+    if (rt >= nrt || tt >= p.n_tiles) return;
+    const int first = slice * p.slice_blocks, last = min(first + p.slice_blocks, p.kb);   // blocks of columns
+    F8Tile t = {0, tt * 256, min(256, p.rows - tt * 256), 0};
+    if (p.tiles) t = p.tiles[tt];
+    const int expert = __builtin_amdgcn_readfirstlane(t.expert), row0 = __builtin_amdgcn_readfirstlane(t.row0),
+              rows = __builtin_amdgcn_readfirstlane(t.rows);
+    if (rows <= 0) return;
+    const int n0 = rt * 256;
+
+    v4f acc[FR][FT];
 #pragma unroll
-        for (int j = 0; j < FR; ++j)
+    for (int j = 0; j < FR; ++j)
 #pragma unroll
-            for (int i = 0; i < FT; ++i) to[(j * FT + i) * 64] = acc[j][i];
-        return;
-    }
-    // the tile's outputs meet in LDS, token by token, and leave in 16-byte pieces
-    constexpr int kSize = S::kSize, kLd = S::kOutLd;
-    if (expert < 0) __syncthreads();   // (else the last barrier has passed)
-    unsigned char* const mine = smem + (wt * 16 * FT + ln) * kLd + (wr * 16 * FR + kg * 4 * FR) * kSize;
-    auto put = [&](auto turn) __attribute__((always_inline)) {
+        for (int i = 0; i < FT; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    if (expert >= 0) {
+        const unsigned char* const wbase = p.w + (size_t(expert) * p.out + n0) * p.ldw;
+        const int w_rows = min(256, p.out - n0);
+        const v4i wrs = buffer_over(wbase, unsigned((w_rows - 1) * p.ldw + (p.in + 15) / 16 * 16));
+        const v4i xrs = buffer_over(p.x, p.x_bytes);
+        const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
+        const unsigned lds0 = lds_address(smem);
+        const int ragged = p.in % 128;
+        auto x_row = [&](int r) {   // of token r of the tile
+            int at = row0 + min(r, rows - 1);
+            if (p.index) at = p.index[at];
+            return at;
+        };
+        // Load i of the weight brings rows 32 wave + 8 i .. + 7 of the tile, of the tokens as many; past the last row of the weight the descriptor ends, and
+        // zeros arrive.  Turns of the 16-byte pieces as in k_f8_tile; the weight's, (row / 2 % 2) + row / 32 % 4 * 2, is the same for a wavefront's loads.
+        const int w_piece = (lane & 7) ^ ((lane >> 4 & 1) | (wave & 3) << 1);
+        const unsigned w_lane = unsigned(lane >> 3) * unsigned(p.ldw) + unsigned(w_piece) * 16u, w_load = unsigned(32 * wave) * unsigned(p.ldw);
+        const unsigned w_tail = ragged && w_piece * 16 >= ragged ? 0x80000000u : w_lane;   // in the last block: zeros past the last column's piece
+        unsigned x_off[4];
 #pragma unroll
-        for (int i = 0; i < FT; ++i)
+        for (int i = 0; i < 4; ++i) {
+            const int r = 32 * wave + 8 * i + (lane >> 3), at = x_row(r);
+            x_off[i] = unsigned(at) < unsigned(p.x_rows) ? unsigned(at) * unsigned(p.kp) + unsigned((lane & 7) ^ (r >> 1 & 7)) * 16u : 0x80000000u;
+        }
+        // the scales of tokens 64 wave .. + 63, a word for four blocks: the first four wavefronts load them
+        const int s_at = late ? -1 : x_row(64 * wave + lane);
+        const unsigned s_off = unsigned(s_at) < unsigned(p.x_rows) ? unsigned(s_at) * 4u : 0x80000000u;
+        int qw = first, qx = first;   // next steps to request; past the last one zeros arrive
+        unsigned w_dst = lds0 + unsigned(wave) * 4096u, x_dst = lds0 + (late ? kBigLate : kBigEarly) + unsigned(side_wave) * 4096u, s_dst = lds0 + kBigScales + unsigned(side_wave) * 256u;
+        const unsigned x_end = x_dst + (late ? 3 : 2) * kBigX, s_end = s_dst + 3 * kBigS;
+        auto request_w = [&](int i) __attribute__((always_inline)) {
+            const bool in = qw < last;
+            const unsigned off = !in ? 0x80000000u : qw == p.kb - 1 ? w_tail : w_lane;
+            load_to_lds(wrs, w_dst + unsigned(i) * 1024u, off, (in ? unsigned(qw) * 128u : 0u) + w_load + unsigned(i) * 8u * unsigned(p.ldw));
+            if (i == 3) {
+                ++qw;
+                w_dst = w_dst < lds0 + kBigW ? w_dst + kBigW : w_dst - kBigW;
+            }
+        };
+        auto request_x = [&](int i, bool early_wave) __attribute__((always_inline)) {
+            const bool in = qx < last;
+            const unsigned none = in ? 0u : 0x80000000u;
+            load_to_lds(xrs, x_dst + unsigned(i) * 1024u, x_off[i] | none, in ? unsigned(qx) * 128u : 0u);
+            if (i < 3) return;
+            if (early_wave) load4_to_lds(xsrs, s_dst, s_off | none, in ? unsigned(qx >> 2) * unsigned(p.x_rows) * 4u : 0u);
+            ++qx;
+            x_dst = x_dst + kBigX == x_end ? x_end - (early_wave ? 2 : 3) * kBigX : x_dst + kBigX;
+            s_dst = s_dst + kBigS == s_end ? s_end - 3 * kBigS : s_dst + kBigS;
+        };
+        // fragments: a lane's row has the turn (ln / 2) % 8 in both operands
+        const int wrow = wr * 128 + (ln >> 2) * 32 + (ln & 3), xrow = (side_wave >> 1) * 64 + ln;   // of the side's tokens
+        const unsigned p0 = unsigned(kg ^ (ln >> 1 & 7)) * 16u;
+        unsigned w_src = lds0 + unsigned(wrow) * 128u + p0, x_src = lds0 + (late ? kBigLate : kBigEarly) + unsigned(xrow) * 128u + p0;
+        unsigned s_src = lds0 + kBigScales + unsigned((late ? 128 : 0) + xrow) * 4u;
+        const unsigned x_wrap = x_src + (late ? 2 : 1) * kBigX, s_wrap = s_src + 2 * kBigS;
+        const unsigned w_clear = lds0 + unsigned(wr * 128) * 128u;
+        auto read_piece = [&](unsigned at) __attribute__((always_inline)) { return join(read_lds<v4i>(at), read_lds<v4i>(at ^ 64u)); };   // pieces kg, kg + 4
+        // the weight's scales of 64 steps, one to a lane
+        const size_t s_row = (size_t(expert) * ((p.out + 127) / 128) + min(n0 + wr * 128, p.out - 1) / 128) * p.kb;
+        int scales = 0;
+        auto load_scales = [&](int b0) {
+            const int b = min(b0 + lane, p.kb - 1);
+            const int v = MODE == kModeF32 ? static_cast<const int*>(p.ws)[s_row + b] : static_cast<const unsigned char*>(p.ws)[s_row + b];
+            asm volatile("v_mov_b32 %0, %1" : "=v"(scales) : "v"(v));   // waited for here, not at every step's use
+        };
+        v8i w[FR], x[FT];
+        int xs[FT], sw = 0;
+        auto read = [&](int b, bool early_wave) __attribute__((always_inline)) {
+            if (early_wave && ragged % 16 && b == p.kb - 1) {
+                // the last block ends inside a 16-byte piece: cleared by those that read first, as in k_f8_tile
+                for (int r = lane; r < 128; r += 64) {
+                    const unsigned at = w_clear + ((b - first) & 1 ? kBigW : 0u) + unsigned(r) * 128u + unsigned(ragged / 16 ^ ((r >> 1 & 1) | (r >> 5 & 3) << 1)) * 16u;
+                    for (int e = ragged % 16; e < 16; ++e) write_lds<unsigned char>(at + e, 0);
+                }
+                wavefront_lds_order();
+            }
 #pragma unroll
-            for (int j = 0; j < FR; ++j) turn(acc[j][i], mine + i * 16 * kLd + j * 4 * kSize);
-    };
-    if constexpr (MODE == kModeExact) put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v4f*>(to) = v; });
-    else if (p.y_dtype == BITSTACK_T_F16) put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v2u*>(to) = pack4<_Float16>(v); });
-    else put([](const v4f& v, unsigned char* to) { *reinterpret_cast<v2u*>(to) = pack4<__bf16>(v); });
-    __syncthreads();
-    constexpr int kPieces = S::kRows * kSize / 16, kEach = 16 / kSize;
-    for (int k = tid; k < S::kToks * kPieces; k += 64 * S::kWaves) {
-        const int tok = k / kPieces, piece = k % kPieces, n = n0 + piece * kEach;
-        if (tok >= rows) break;
-        if (n >= p.out) continue;
-        const unsigned char* const from = smem + tok * kLd + piece * 16;
-        unsigned char* const y = static_cast<unsigned char*>(p.y) + (size_t(row0 + tok) * p.ldy + n) * kSize;
-        if (p.y_vec16 && n + kEach <= p.out) {
-            *reinterpret_cast<v4i*>(y) = *reinterpret_cast<const v4i*>(from);
-        } else {
-            for (int e = 0; e < kEach && n + e < p.out; ++e) {
-                if constexpr (kSize == 4) reinterpret_cast<float*>(y)[e] = reinterpret_cast<const float*>(from)[e];
-                else reinterpret_cast<unsigned short*>(y)[e] = reinterpret_cast<const unsigned short*>(from)[e];
+            for (int i = 0; i < FT; ++i) xs[i] = int(read_lds<unsigned char>(s_src + i * 64 + (b & 3)));
+#pragma unroll
+            for (int j = 0; j < FR; ++j) w[j] = read_piece(w_src + j * 512);
+#pragma unroll
+            for (int i = 0; i < FT; ++i) x[i] = read_piece(x_src + i * 2048);
+            if ((b - first & 63) == 0) load_scales(b);
+            sw = __builtin_amdgcn_readlane(scales, b - first & 63);
+            w_src = (b - first) & 1 ? w_src - kBigW : w_src + kBigW;
+            x_src = x_src == x_wrap ? x_wrap - (early_wave ? 1 : 2) * kBigX : x_src + kBigX;
+            s_src = s_src == s_wrap ? s_wrap - 2 * kBigS : s_src + kBigS;
+        };
+        auto products = [&](auto after) __attribute__((always_inline)) {
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, MODE == kModeF32, [&](int i) __attribute__((always_inline)) {
+                __builtin_amdgcn_sched_barrier(0);
+                after(i);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto begin = [&](bool early_wave) __attribute__((always_inline)) {   // two steps
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) request_w(i);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) request_x(i, early_wave);
+            }
+        };
+        // (a loop for each side: with branches inside, the compiler moves the products past the barriers)
+        if (!late) {
+            constexpr int kX = 5;   // loads of a step's tokens and scales
+            begin(true);
+            loads_barrier<4 + kX>();   // the first step
+            for (int b = first; b < last; ++b) {
+                read(b, true);
+                if (b > first) {   // the weight of step b + 1
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) request_w(i);
+                }
+                lds_barrier();
+                products([&](int i) __attribute__((always_inline)) { request_x(i, true); });   // the tokens of step b + 2
+                loads_barrier<kX>();                                                           // step b + 1
+            }
+            lds_barrier();
+        } else if (rows > 128) {
+            constexpr int kX = 4;
+            begin(false);
+            loads_barrier<4 + kX>();
+            lds_barrier();
+            for (int b = first; b < last; ++b) {
+                read(b, false);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) request_x(i, false);   // the tokens of step b + 2
+                loads_barrier<kX>();                               // step b + 1
+                products([&](int i) __attribute__((always_inline)) { request_w(i); });   // the weight of step b + 2
+                lds_barrier();
+            }
+        } else {   // no tokens here
+#pragma unroll
+            for (int i = 0; i < 8; ++i) request_w(i & 3);
+            loads_barrier<4>();
+            lds_barrier();
+            for (int b = first; b < last; ++b) {
+                loads_barrier<0>();   // step b + 1
+#pragma unroll
+                for (int i = 0; i < 4; ++i) request_w(i);   // step b + 2
+                lds_barrier();
             }
         }
+        loads_barrier<0>();   // nothing may land in LDS any more
     }
+    finish_tile<S, FR, FT, WR>(p, smem, acc, size_t(slice) * nrt * p.n_tiles + size_t(rt) * p.n_tiles + tt, n0, row0, rows);
 }
 
 // y from the partial sums of p.slices column slices, added up in order: a wavefront takes what one of k_f8_tile's held of a tile, FR fragments
@@ -577,27 +761,38 @@ __global__ __launch_bounds__(256) void k_f8_join(F8Params p) {
     for (int j = 0; j < FR; ++j) store4(p, t.row0 + tok, n + 4 * j, sum[j]);
 }
 
-template <int FR, int FT, int WR, int WT, int MODE, bool TOUCH>
-static hipError_t tiles(F8Params p, hipStream_t st) {
-    typedef F8TileShape<FR, FT, WR, WT, MODE> S;
-    static std::atomic<bool> attr_set{false};   // setting the attribute twice is harmless
-    if (!attr_set) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
-    const unsigned nrt = unsigned((p.out + S::kRows - 1) / S::kRows);
-    // workgroups on an XCD at a time (32) that read the same rows of the weight, of the tokens
-    const int per_row = (p.n_tiles + 1) / 2;
-    auto power = [](int n) { return n >= 8 ? 8 : n >= 4 ? 4 : n >= 2 ? 2 : 1; };
-    p.touch_w = power(std::min(32, per_row));
-    p.touch_x = power(32 / std::min(32, per_row));
-    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE, TOUCH>), dim3(8 * ((nrt + 3) / 4) * unsigned(per_row * p.slices)), dim3(512), S::kLds, st, p);
+static hipError_t allow_lds(const void* kernel, std::atomic<bool>& done, int bytes) {   // (doing it twice is harmless)
+    if (done) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done = true;
+    return e;
+}
+template <int FR, int FT, int WR, int WT>
+static hipError_t join(const F8Params& p, hipStream_t st) {
     if (p.slices > 1) {
-        const size_t units = size_t(nrt) * p.n_tiles * 8 * FT;
+        const size_t units = size_t((p.out + 16 * FR * WR - 1) / (16 * FR * WR)) * p.n_tiles * 8 * FT;
         hipLaunchKernelGGL((k_f8_join<FR, FT, WR, WT>), dim3(unsigned((units + 3) / 4)), dim3(256), 0, st, p);
     }
     return hipGetLastError();
+}
+template <int FR, int FT, int WR, int WT, int MODE>
+static hipError_t tiles(const F8Params& p, hipStream_t st) {
+    typedef F8TileShape<FR, FT, WR, WT, MODE> S;
+    static std::atomic<bool> done{false};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&k_f8_tile<FR, FT, WR, WT, MODE>), done, S::kLds);
+    if (e != hipSuccess) return e;
+    const unsigned nrt = unsigned((p.out + S::kRows - 1) / S::kRows), per_row = unsigned(p.n_tiles + 1) / 2;
+    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE>), dim3(8 * ((nrt + 3) / 4) * per_row * unsigned(p.slices)), dim3(512), S::kLds, st, p);
+    return join<FR, FT, WR, WT>(p, st);
+}
+template <int MODE>
+static hipError_t tiles256(const F8Params& p, hipStream_t st) {
+    static std::atomic<bool> done{false};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&k_f8_tile256<MODE>), done, F8BigShape::kLds);
+    if (e != hipSuccess) return e;
+    const unsigned nrt = unsigned((p.out + 255) / 256), per_row = unsigned(p.n_tiles + 1) / 2;
+    hipLaunchKernelGGL((k_f8_tile256<MODE>), dim3(8 * ((nrt + 3) / 4) * per_row * unsigned(p.slices)), dim3(512), F8BigShape::kLds, st, p);
+    return join<8, 4, 2, 4>(p, st);
 }
 
 template <int FR, int FT, int DEPTH, int MODE, int T>
@@ -698,19 +893,14 @@ hipError_t launch_f8_product(const F8Params& args, const F8Plan& plan, hipStream
         case kSlices32: return slices<4, 2, 1>(p, st);
         case kSlices64: return slices<4, 4, 1>(p, st);
         case kTile64:
-            if (exact) return tiles<2, 2, 4, 2, kModeExact, false>(p, st);
-            return p.ws_f32 ? tiles<2, 2, 4, 2, kModeF32, false>(p, st) : tiles<2, 2, 4, 2, kModeE8M0, false>(p, st);
+            if (exact) return tiles<2, 2, 4, 2, kModeExact>(p, st);
+            return p.ws_f32 ? tiles<2, 2, 4, 2, kModeF32>(p, st) : tiles<2, 2, 4, 2, kModeE8M0>(p, st);
         case kTile128:
-            if (exact) return tiles<2, 4, 4, 2, kModeExact, false>(p, st);
-            return p.ws_f32 ? tiles<2, 4, 4, 2, kModeF32, false>(p, st) : tiles<2, 4, 4, 2, kModeE8M0, false>(p, st);
+            if (exact) return tiles<2, 4, 4, 2, kModeExact>(p, st);
+            return p.ws_f32 ? tiles<2, 4, 4, 2, kModeF32>(p, st) : tiles<2, 4, 4, 2, kModeE8M0>(p, st);
         case kTile128Wide:
-            return p.ws_f32 ? tiles<4, 4, 4, 2, kModeF32, false>(p, st) : tiles<4, 4, 4, 2, kModeE8M0, false>(p, st);
-        default: {
-            // (touching: see the kernel; 256 tiles are all there at once)
-            const bool touch = !p.tiles && size_t((p.out + 255) / 256) * p.n_tiles > 256;
-            if (p.ws_f32) return touch ? tiles<8, 4, 2, 4, kModeF32, true>(p, st) : tiles<8, 4, 2, 4, kModeF32, false>(p, st);
-            return touch ? tiles<8, 4, 2, 4, kModeE8M0, true>(p, st) : tiles<8, 4, 2, 4, kModeE8M0, false>(p, st);
-        }
+            return p.ws_f32 ? tiles<4, 4, 4, 2, kModeF32>(p, st) : tiles<4, 4, 4, 2, kModeE8M0>(p, st);
+        default: return p.ws_f32 ? tiles256<kModeF32>(p, st) : tiles256<kModeE8M0>(p, st);
     }
 }
 

@@ -152,13 +152,13 @@ static void quantise(const void* x, size_t ld, int rows, int in, bool gated, uns
     // the halves of a gated row begin `in` elements apart
     const int vec = vector_rows(x, ld, sizeof(E)) && (!gated || size_t(in) * sizeof(E) % 16 == 0);
     unsigned* const words = reinterpret_cast<unsigned*>(s);
-    // with four words a wavefront there is enough to do for all compute units
-    const int each = size_t(rows) * ((kp + 2047) / 2048) >= 4096 ? 4 : 1;
+    // Gated rows, whose arithmetic hides no latency: four words a wavefront where that leaves enough wavefronts
+    const int each = gated && size_t(rows) * ((kp + 2047) / 2048) >= 4096 ? 4 : 1;
     const size_t waves = size_t(rows) * ((kp + 512 * each - 1) / (512 * each));
     const unsigned grid = unsigned((waves + 3) / 4) + (list.offsets ? 1 : 0);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list); };
     if (gated) each == 4 ? go(&k_f8_quantise<T, true, 4>) : go(&k_f8_quantise<T, true, 1>);
-    else each == 4 ? go(&k_f8_quantise<T, false, 4>) : go(&k_f8_quantise<T, false, 1>);
+    else go(&k_f8_quantise<T, false, 1>);
 }
 
 hipError_t launch_f8_quantise(const void* x, int dtype, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s,
