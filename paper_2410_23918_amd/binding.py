@@ -528,6 +528,17 @@ class PackedStack:
                "bitstack_restore_weight")
         return w_dense
 
+    def restore_weight_f8(self, n_loaded: int, w_dense=None, stream=None):
+        """The loaded prefix in 8 bits, (q, scales) as linear_f8 takes them: bitstack_restore_weight into w_dense (an fp16 scratch
+        [out][in], allocated unless given), then bitstack_f8_quantise_weight."""
+        import contextlib
+
+        import torch
+        from .f8 import quantise_weight_f8
+        # what is allocated here belongs to the stream that uses it
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            return quantise_weight_f8(self.restore_weight(n_loaded, w_dense=w_dense, stream=stream), stream=stream)
+
     def _y_for(self, x, y, out_dtype):
         import torch
         out_dtype = out_dtype or (y.dtype if y is not None else torch.float16)
