@@ -14,7 +14,7 @@ constexpr int kMaxExperts = 1024, kMaxTopK = 32;
 
 // one piece of a product: rows [row0, row0 + rows) of y with expert's weight; expert < 0: rows of zeros; rows 0: nothing
 struct F8Tile {
-    int expert, row0, rows, pad;
+    int expert, row0, rows, all;   // all: tiles that have rows, in every one
 };
 
 struct F8Params {
@@ -111,7 +111,7 @@ struct F8Plan {
     int tiles;                                // of the weight's rows and y's
     size_t part_bytes;                        // partial sums
 };
-F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact);
+F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32);
 hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
 void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
 

@@ -74,7 +74,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     if (misaligned(w->q, 16) || w->ld % 16 || (w->scale_type == BITSTACK_S_F32 && misaligned(w->scales, 4))) return BITSTACK_E_ALIGN;
     if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
-    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32);
+    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32);
     const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
     const Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {
@@ -167,9 +167,9 @@ size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int 
     if (x_rows < 0 || y_rows < 0 || !columns_ok(in) || out < 1 || out > kMaxOut || experts < 1 || experts > kMaxExperts) return 0;
     if (size_t(x_rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return 0;
     size_t most = 256;
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 8; ++k)
         if (y_rows) {
-            const size_t n = workspace_of(x_rows, in, f8_plan(y_rows, out, in, experts, k & 1, k >> 1), false, true).total;
+            const size_t n = workspace_of(x_rows, in, f8_plan(y_rows, out, in, experts, k & 1, k >> 1 & 1, k >> 2), false, true).total;
             most = n > most ? n : most;
         }
     return most;
@@ -177,7 +177,7 @@ size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int 
 
 size_t bitstack_f8_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, int y_rows, int y_dtype, int grouped) {
     if (!x || !w || check_call(x, w, y_rows, y_dtype) || y_rows == 0) return 0;
-    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, grouped != 0, y_dtype == BITSTACK_T_F32);
+    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, grouped != 0, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32);
     return workspace_of(x->rows, w->in, plan, x->dtype == BITSTACK_T_F8 || raw_rows(*x, *w, y_rows, plan, grouped != 0), grouped != 0).total;
 }
 

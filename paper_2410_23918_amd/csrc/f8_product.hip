@@ -316,11 +316,33 @@ template <int FR, int FT, int WR, int WT, int MODE>
 struct F8TileShape {
     static constexpr int kWaves = 8, kRows = 16 * FR * WR, kToks = 16 * FT * WT;
     static constexpr int kStep = (kRows + kToks) * 128 + 4 * 256;   // bytes, a multiple of 128 (the scales of 4 x 64 tokens)
-    static constexpr int kRing = (163840 - 256) / kStep < 6 ? (163840 - 256) / kStep : 6;
+    // Small tiles: two workgroups on a compute unit, with half the LDS each, so that one multiplies while the other one waits.  128 x 64, 1024 tokens
+    // through 4096 x 4096: 41 us and 31; 128 x 128 there, where two leave a ring of two: 28 and 36, so those stay alone.
+    static constexpr bool kTwo = kRows * kToks <= 128 * 64;
+    static constexpr int kRing = ((kTwo ? 81920 : 163840) - 256) / kStep;
     static constexpr int kSize = MODE == kModeExact ? 4 : 2, kOutLd = kRows * kSize + 16;   // the output tile in LDS
     static constexpr int kRingLds = kRing * kStep + 256, kLds = kRingLds > kToks * kOutLd ? kRingLds : kToks * kOutLd;
     static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % 64 == 0 && kToks <= 256, "whole loads, one weight scale a wavefront, scales for the first four wavefronts");
 };
+
+// The tile of a workgroup.  Ids are dealt round-robin to the 8 XCDs: each takes an eighth of the tiles there are, as many as the next to within one, neighbours
+// in an order in which a few tiles of tokens go through all rows of the weight, so that what 32 compute units read at a time meets in one L2.  (Every fourth
+// tile of rows x every second of tokens instead left half the XCDs with twice as many where there are three tiles of tokens: 14336 x 4096, 300 tokens, 256 x 128 in
+// five slices: 60.6 us, 41.5.)  Four tiles of tokens, eight in groups: 28672 x 8192, 2048 tokens 394 and 402 us, 8 experts' 4096 rows through 14336 x 4096 289 and 280.
+__device__ __forceinline__ bool tile_of(const F8Params& p, int nrt, int& rt, int& tt, int& slice) {
+    const unsigned together = p.tiles ? 8 : 4;
+    const unsigned nt = p.tiles ? unsigned(min(__builtin_amdgcn_readfirstlane(p.tiles[0].all), p.n_tiles)) : unsigned(p.n_tiles);
+    const unsigned each = unsigned(nrt) * nt, all = each * unsigned(p.slices), per = (all + 7) / 8, place = blockIdx.x >> 3;
+    unsigned v = (blockIdx.x & 7) * per + place;
+    if (place >= per || v >= all) return false;
+    slice = int(v / each);
+    v %= each;
+    const unsigned group = v / (unsigned(nrt) * together), size = min(together, nt - group * together);
+    v -= group * (unsigned(nrt) * together);
+    rt = int(v / size);
+    tt = int(group * together + v % size);
+    return true;
+}
 
 // A tile's sums leave the kernel (all LDS is free).  FR x FT fragments a wavefront, WR x WT wavefronts.
 template <class S, int FR, int FT, int WR>
@@ -367,7 +389,7 @@ __device__ __forceinline__ void finish_tile(const F8Params& p, unsigned char* sm
 }
 
 template <int FR, int FT, int WR, int WT, int MODE>
-__global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
+__global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 : 2)) void k_f8_tile(F8Params p) {
     typedef F8TileShape<FR, FT, WR, WT, MODE> S;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -375,11 +397,9 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile(F8Params p) {
     const int wr = wave % WR, wt = wave / WR;
     const bool late = wave >= 4;
     const int ln = lane & 15, kg = lane >> 4;
-    // ids are dealt round-robin to the 8 XCDs, whose L2s each fetch what their tiles read: every fourth row tile x every second token tile
-    const int nrt = (p.out + S::kRows - 1) / S::kRows, per_row = (p.n_tiles + 1) / 2, per_slice = (nrt + 3) / 4 * per_row;
-    const int xcd = blockIdx.x & 7, slice = (blockIdx.x >> 3) / per_slice, place = (blockIdx.x >> 3) % per_slice;
-    const int rt = (xcd >> 1) + 4 * (place / per_row), tt = (xcd & 1) + 2 * (place % per_row);
-    if (rt >= nrt || tt >= p.n_tiles) return;
+    const int nrt = (p.out + S::kRows - 1) / S::kRows;
+    int rt, tt, slice;
+    if (!tile_of(p, nrt, rt, tt, slice)) return;
     const int first = slice * p.slice_blocks, last = min(first + p.slice_blocks, p.kb);   // blocks of columns
     F8Tile t = {0, tt * S::kToks, min(S::kToks, p.rows - tt * S::kToks), 0};
     if (p.tiles) t = p.tiles[tt];
@@ -558,11 +578,9 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
     const int wr = wave % WR;
     const bool late = wave >= 4;
     const int ln = lane & 15, kg = lane >> 4;
-    // ids are dealt round-robin to the 8 XCDs, whose L2s each fetch what their tiles read: every fourth row tile x every second token tile
-    const int nrt = (p.out + 255) / 256, per_row = (p.n_tiles + 1) / 2, per_slice = (nrt + 3) / 4 * per_row;
-    const int xcd = blockIdx.x & 7, slice = (blockIdx.x >> 3) / per_slice, place = (blockIdx.x >> 3) % per_slice;
-    const int rt = (xcd >> 1) + 4 * (place / per_row), tt = (xcd & 1) + 2 * (place % per_row);
-    if (rt >= nrt || tt >= p.n_tiles) return;
+    const int nrt = (p.out + 255) / 256;
+    int rt, tt, slice;
+    if (!tile_of(p, nrt, rt, tt, slice)) return;
     const int first = slice * p.slice_blocks, last = min(first + p.slice_blocks, p.kb);   // blocks of columns
     F8Tile t = {0, tt * 256, min(256, p.rows - tt * 256), 0};
     if (p.tiles) t = p.tiles[tt];
@@ -767,6 +785,9 @@ static hipError_t allow_lds(const void* kernel, std::atomic<bool>& done, int byt
     if (e == hipSuccess) done = true;
     return e;
 }
+static unsigned tile_grid(const F8Params& p, int tile_rows) {
+    return 8 * ((unsigned((p.out + tile_rows - 1) / tile_rows) * unsigned(p.n_tiles) * unsigned(p.slices) + 7) / 8);
+}
 template <int FR, int FT, int WR, int WT>
 static hipError_t join(const F8Params& p, hipStream_t st) {
     if (p.slices > 1) {
@@ -781,8 +802,7 @@ static hipError_t tiles(const F8Params& p, hipStream_t st) {
     static std::atomic<bool> done{false};
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(&k_f8_tile<FR, FT, WR, WT, MODE>), done, S::kLds);
     if (e != hipSuccess) return e;
-    const unsigned nrt = unsigned((p.out + S::kRows - 1) / S::kRows), per_row = unsigned(p.n_tiles + 1) / 2;
-    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE>), dim3(8 * ((nrt + 3) / 4) * per_row * unsigned(p.slices)), dim3(512), S::kLds, st, p);
+    hipLaunchKernelGGL((k_f8_tile<FR, FT, WR, WT, MODE>), dim3(tile_grid(p, S::kRows)), dim3(512), S::kLds, st, p);
     return join<FR, FT, WR, WT>(p, st);
 }
 template <int MODE>
@@ -790,8 +810,7 @@ static hipError_t tiles256(const F8Params& p, hipStream_t st) {
     static std::atomic<bool> done{false};
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(&k_f8_tile256<MODE>), done, F8BigShape::kLds);
     if (e != hipSuccess) return e;
-    const unsigned nrt = unsigned((p.out + 255) / 256), per_row = unsigned(p.n_tiles + 1) / 2;
-    hipLaunchKernelGGL((k_f8_tile256<MODE>), dim3(8 * ((nrt + 3) / 4) * per_row * unsigned(p.slices)), dim3(512), F8BigShape::kLds, st, p);
+    hipLaunchKernelGGL((k_f8_tile256<MODE>), dim3(tile_grid(p, 256)), dim3(512), F8BigShape::kLds, st, p);
     return join<8, 4, 2, 4>(p, st);
 }
 
@@ -826,41 +845,49 @@ constexpr F8KernelShape kShapes[] = {{kSlices16, 16, 16}, {kSlices16Wide, 64, 16
 static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * column slices, 0 = the choice below
 void f8_force_kernel(int kernel) { g_forced = kernel; }
 
-// Duration in microseconds, from timings of 30 shapes (1 to 2048 rows, 512 to 28672 x 1024 to 14336)
-static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, int kb, int experts, bool grouped, bool exact) {
+// Duration in microseconds.  The constants were fitted to timings of every kernel on 65 products (1 to 3660 rows, 256 to 28672 x 512 to 14336, up to 64
+// experts, all types): what they choose is 0.7 % slower than the fastest, in the mean, 18 % at most.
+static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, int kb, int experts, bool grouped, bool exact, bool ws_f32) {
     // tiles of y's rows that have any: a group fills its last one by half, in the mean
     const int groups = grouped ? std::min(rows, experts) : 1;
     const double mt = grouped ? std::max<double>(groups, double(rows) / k.toks + 0.5 * groups) : (rows + k.toks - 1) / k.toks;
-    const double tiles = mt * ((out + k.rows - 1) / k.rows), rounds = std::ceil(tiles * slices / 256);
+    const double tiles = mt * ((out + k.rows - 1) / k.rows), rounds = tiles * slices / 256;
     // the weights once, from memory
-    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.toks == 16 ? 4.7e6 : k.toks == 32 ? 4.2e6 : k.kernel == kSlices64 ? 3.6e6 : 4.0e6);
-    const double passes = (kb + 7) / 8, whole = std::floor(tiles / 1024), rest = (tiles - 1024 * whole) / 256;
-    double us;
-    if (k.kernel == kSlices16) {   // up to four workgroups on a compute unit
-        us = 3.5 + passes * (whole * 4.1 + (rest > 0 ? 0.3 + 0.95 * rest : 0.0));
-    } else if (k.kernel == kSlices16Wide || k.kernel == kSlices32) {   // two
-        const double more = k.toks == 16 ? (exact ? 3.0 : 2.4) : (exact ? 3.8 : 3.3);
-        us = 4.0 + passes * std::max(k.toks == 16 ? 1.9 : 2.1, 0.9 + more * tiles / 256);
-    } else if (k.kernel == kSlices64) {
-        us = 4.0 + rounds * passes * (exact ? 5.2 : 4.2);
-    } else {
-        const double step = k.kernel == kTile64 ? (exact ? 0.9 : 0.56) : k.kernel == kTile128 ? (exact ? 1.3 : 0.72) : k.kernel == kTile128Wide ? 1.1 : 1.7;
-        us = 4.5 + rounds * ((kb + slices - 1) / slices) * step;
+    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.toks == 16 ? 4.5e6 : k.toks == 32 ? 3.4e6 : k.kernel == kSlices64 ? 2.7e6 : 5.1e6);
+    const double passes = (kb + 7) / 8, steps = (kb + slices - 1) / slices;
+    double us = 4.9;
+    switch (k.kernel) {
+        case kSlices16: {   // up to four workgroups on a compute unit
+            const double whole = std::floor(rounds / 4), rest = rounds - 4 * whole;
+            us = 3.5 + passes * (whole * 4.1 + (rest > 0 ? 0.14 + 1.2 * rest : 0.0));
+            break;
+        }
+        case kSlices16Wide: us = 4.0 + passes * std::max(1.9, 1.1 + (exact ? 2.7 : 2.2) * rounds); break;   // two
+        case kSlices32: us = 4.0 + passes * std::max(2.3, 1.1 + (exact ? 3.5 : 3.0) * rounds); break;
+        case kSlices64: us = 4.0 + passes * std::ceil(rounds) * 4.2; break;
+        case kTile64: {   // two, which take less than twice as long as one
+            const double one = exact ? 0.81 : 0.53, two = exact ? 1.43 : 0.83, whole = std::floor(rounds / 2), rest = rounds - 2 * whole;
+            us += steps * (whole * two + (rest > 1 ? two : rest > 0 ? one : 0.0));
+            break;
+        }
+        case kTile128: us += steps * std::ceil(rounds) * (exact ? 1.35 : 0.71); break;
+        case kTile128Wide: us += steps * std::ceil(rounds) * 1.02; break;
+        default: us += steps * std::ceil(rounds) * (ws_f32 ? 1.72 : 1.48);
     }
-    return std::max(us, stream) + (slices > 1 ? 3.5 + slices * tiles * k.rows * k.toks * 8 / 4e6 : 0.0);
+    return std::max(us, stream) + (slices > 1 ? 3.0 + slices * tiles * k.rows * k.toks * 8 / 5e6 : 0.0);
 }
 
 // Kernel and column slices of a product, from sizes alone (the workspace holds the partial sums)
-F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact) {
+F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32) {
     const int forced = g_forced.load(), kb = (in + 127) / 128;
     F8Plan plan{kShapes[0].kernel, 1, 0, 0, 0, 0};
     double best = 1e30;
     for (const F8KernelShape& k : kShapes) {
         if (!forced && rows <= 16 && k.toks > 16) break;   // never faster
         if (exact && k.kernel >= kTile128Wide) continue;   // the operands as fp16 leave no registers for its sums
-        for (int slices : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        for (int slices : {1, 2, 3, 4, 5, 6, 7, 8, 12, 16}) {
             if (forced ? k.kernel != forced % 1024 || slices > 1 : slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
-            const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact);
+            const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact, ws_f32);
             if (us >= best) continue;
             best = us;
             plan = {k.kernel, slices, k.toks, 0, 0, 0};

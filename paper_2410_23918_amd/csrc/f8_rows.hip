@@ -50,10 +50,10 @@ __device__ void make_work_list(const F8WorkList& l) {
             if (upto[mid] > t) hi = mid;
             else lo = mid + 1;
         }
-        F8Tile tile = {-1, 0, 0, 0};
+        F8Tile tile = {-1, 0, 0, upto[l.experts]};
         if (lo <= l.experts) {
             const int first = (lo ? end[lo - 1] : 0) + (t - (lo ? upto[lo - 1] : 0)) * l.tile_rows;
-            tile = {lo < l.experts ? lo : -1, first, min(l.tile_rows, end[lo] - first), 0};
+            tile = {lo < l.experts ? lo : -1, first, min(l.tile_rows, end[lo] - first), upto[l.experts]};
         }
         l.tiles[t] = tile;
     }

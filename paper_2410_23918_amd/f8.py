@@ -306,13 +306,14 @@ def route(logits, top_k: int, *, renormalise: bool = True, stream=None) -> Routi
         nbytes = L.bitstack_route_workspace_bytes(n, e, top_k)
         if nbytes == 0:
             raise BitStackError(-2, "bitstack_route_workspace_bytes")
-        words = torch.empty((4, n, top_k), dtype=torch.int32, device=logits.device)
-        at = -(-(e + 1) // 64) * 64   # the offsets, then (256-byte aligned) the workspace
-        tail = torch.empty(at + nbytes // 4, dtype=torch.int32, device=logits.device)
-        experts, weights, slots, rows = words.unbind(0)
-        r = Routing(experts, weights.view(torch.float32), slots, rows.view(-1), tail[: e + 1])
-        p, step, o = words.data_ptr(), 4 * n * top_k, tail.data_ptr()
-        _check(L.bitstack_route(logits.data_ptr(), t, ld, n, e, top_k, int(renormalise), p, p + step, p + 2 * step, p + 3 * step, o, o + 4 * at, nbytes,
+        # one allocation: experts, weights, slots, rows (each nk words), the offsets, then (256-byte aligned) the workspace
+        nk = n * top_k
+        at = -(-(4 * nk + e + 1) // 64) * 64
+        words = torch.empty(at + nbytes // 4, dtype=torch.int32, device=logits.device)
+        experts, weights, slots, rows, offsets, _ = words.split_with_sizes((nk, nk, nk, nk, e + 1, at - 4 * nk - e - 1 + nbytes // 4))
+        r = Routing(experts.view(n, top_k), weights.view(torch.float32).view(n, top_k), slots.view(n, top_k), rows, offsets)
+        p, step = words.data_ptr(), 4 * nk
+        _check(L.bitstack_route(logits.data_ptr(), t, ld, n, e, top_k, renormalise, p, p + step, p + 2 * step, p + 3 * step, p + 4 * step, p + 4 * at, nbytes,
                                 handle), "bitstack_route")
     return r
 
