@@ -173,8 +173,30 @@ __device__ __forceinline__ void columns_to_f8(const v4i (&raw)[4], v8i& x, int& 
     for (int d = 0; d < 8; ++d) x[d] = bad ? 0x7f7f7f7f : int(f8_x4(v[4 * d] * inv, v[4 * d + 1] * inv, v[4 * d + 2] * inv, v[4 * d + 3] * inv));
 }
 
+// The tile of a workgroup.  Ids are dealt round-robin to the 8 XCDs: each takes an eighth of the tiles there are, as many as the next to within one, neighbours
+// in an order in which a few tiles of tokens go through all rows of the weight, so that what 32 compute units read at a time meets in one L2.  (Every fourth
+// tile of rows x every second of tokens instead left half the XCDs with twice as many where there are three tiles of tokens: 14336 x 4096, 300 tokens, 256 x 128 in
+// five slices: 60.6 us, 41.5.)
+__device__ __forceinline__ bool tile_of(const F8Params& p, int nrt, unsigned together, int& rt, int& tt, int& slice) {
+    const unsigned nt = p.tiles ? unsigned(min(__builtin_amdgcn_readfirstlane(p.tiles[0].all), p.n_tiles)) : unsigned(p.n_tiles);
+    const unsigned each = unsigned(nrt) * nt, all = each * unsigned(p.slices), per = (all + 7) / 8, place = blockIdx.x >> 3;
+    unsigned v = (blockIdx.x & 7) * per + place;
+    if (place >= per || v >= all) return false;
+    slice = int(v / each);
+    v %= each;
+    const unsigned group = v / (unsigned(nrt) * together), size = min(together, nt - group * together);
+    v -= group * (unsigned(nrt) * together);
+    rt = int(v / size);
+    tt = int(group * together + v % size);
+    return true;
+}
+
 // A tile of 16 FR rows of the weight x 16 FT tokens.  The eight wavefronts of a workgroup take every eighth block of columns each, straight
 // from memory into registers (nothing of a tile is read by two of them), DEPTH blocks ahead; their sums meet in LDS.
+//   Bound by the stream of the weight, of which four wavefronts a SIMD keep 16 to 32 KB in flight on a compute unit: one token through two of eight 14336 x 4096
+// experts 24.9 us, 4.7 TB/s (16 rows as tokens stay in registers; tiles of 64 x 16, so that a block of the activations is read for 64 rows).  Small weights are bound by
+// the launch and three latencies (first load, LDS, store): 57 tokens through 1056 x 2001 in fp32, 16 x 16 tiles, 5.9 us.  With 32 and 64 tokens each
+// wavefront's operands come from L2 again for every 64 rows.
 //   T: type of the activations.  With one fragment of tokens they may come as they are and are brought to 8 bits on the way (a block of a token lies
 // in four lanes), by every workgroup anew: one launch instead of two.  One token through 1024 x 4096: 7.0 us, 5.5 and 2.4 + a launch for the rows
 // quantised before; 14336 x 4096 16.7, 16.2 and 2.4; 4096 x 14336, where 256 workgroups convert 112 blocks each, 20.4, 14.4 and 2.5.
@@ -186,11 +208,8 @@ __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ln = lane & 15, kg = lane >> 4;
-    // ids are dealt round-robin to the 8 XCDs: all token tiles of a row tile meet in one L2
-    const int nrt = (p.out + 16 * FR - 1) / (16 * FR);
-    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3;
-    const int rt = xcd + 8 * (place / p.n_tiles), tt = place % p.n_tiles;
-    if (rt >= nrt) return;
+    int rt, tt, slice;
+    if (!tile_of(p, (p.out + 16 * FR - 1) / (16 * FR), unsigned(p.n_tiles), rt, tt, slice)) return;
     F8Tile t = {0, tt * 16 * FT, min(16 * FT, p.rows - tt * 16 * FT), 0};
     if (p.tiles) t = p.tiles[tt];
     const int expert = __builtin_amdgcn_readfirstlane(t.expert), row0 = __builtin_amdgcn_readfirstlane(t.row0),
@@ -310,6 +329,10 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
 //   LDS: a row's 128 bytes, its 16-byte piece c at position c ^ f(row), f such that the sixteen rows that a fragment's read touches at a time
 // meet every bank once.  Row i of the weight's fragment j is row (i / 4) 4 FR + 4 j + i % 4 of the wavefront's tile, so that a lane ends with 4 FR neighbouring
 // outputs of a token.
+//   Bound by LDS and latency: a phase reads 32 to 64 KB of fragments (128 bytes a clock) and multiplies for 128 to 256 clocks; 128 x 64 takes 0.54 us a step alone and
+// 0.9 for two workgroups of a compute unit, 128 x 128 0.78, 256 x 128 1.08; products alone would take 0.12, 0.25 and 0.50.  300 tokens
+// through 4096 x 14336 (256 x 128, five column slices, fp32 scales): 36.6 us, 0.96 PFLOP/s, and 6.8 to join them.  64 experts' 342 rows through 1024 x 4096
+// (128 x 64): 51.8 us, 4.3 TB/s, the stream of the weights.
 //   The activations' scales come with the step, four bytes a token (four steps' scales, of which one is used); the weight's, the same for 128
 // rows, are kept one to a lane for 64 steps.
 template <int FR, int FT, int WR, int WT, int MODE>
@@ -324,25 +347,6 @@ struct F8TileShape {
     static constexpr int kRingLds = kRing * kStep + 256, kLds = kRingLds > kToks * kOutLd ? kRingLds : kToks * kOutLd;
     static_assert(WR * WT == 8 && WR <= 4 && kRing >= 2 && kLds <= 163840 && 16 * FR <= 128 && kRows % (8 * kWaves) == 0 && kToks % 64 == 0 && kToks <= 256, "whole loads, one weight scale a wavefront, scales for the first four wavefronts");
 };
-
-// The tile of a workgroup.  Ids are dealt round-robin to the 8 XCDs: each takes an eighth of the tiles there are, as many as the next to within one, neighbours
-// in an order in which a few tiles of tokens go through all rows of the weight, so that what 32 compute units read at a time meets in one L2.  (Every fourth
-// tile of rows x every second of tokens instead left half the XCDs with twice as many where there are three tiles of tokens: 14336 x 4096, 300 tokens, 256 x 128 in
-// five slices: 60.6 us, 41.5.)  Four tiles of tokens, eight in groups: 28672 x 8192, 2048 tokens 394 and 402 us, 8 experts' 4096 rows through 14336 x 4096 289 and 280.
-__device__ __forceinline__ bool tile_of(const F8Params& p, int nrt, int& rt, int& tt, int& slice) {
-    const unsigned together = p.tiles ? 8 : 4;
-    const unsigned nt = p.tiles ? unsigned(min(__builtin_amdgcn_readfirstlane(p.tiles[0].all), p.n_tiles)) : unsigned(p.n_tiles);
-    const unsigned each = unsigned(nrt) * nt, all = each * unsigned(p.slices), per = (all + 7) / 8, place = blockIdx.x >> 3;
-    unsigned v = (blockIdx.x & 7) * per + place;
-    if (place >= per || v >= all) return false;
-    slice = int(v / each);
-    v %= each;
-    const unsigned group = v / (unsigned(nrt) * together), size = min(together, nt - group * together);
-    v -= group * (unsigned(nrt) * together);
-    rt = int(v / size);
-    tt = int(group * together + v % size);
-    return true;
-}
 
 // A tile's sums leave the kernel (all LDS is free).  FR x FT fragments a wavefront, WR x WT wavefronts.
 template <class S, int FR, int FT, int WR>
@@ -399,7 +403,7 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
     const int ln = lane & 15, kg = lane >> 4;
     const int nrt = (p.out + S::kRows - 1) / S::kRows;
     int rt, tt, slice;
-    if (!tile_of(p, nrt, rt, tt, slice)) return;
+    if (!tile_of(p, nrt, p.tiles ? 8 : 4, rt, tt, slice)) return;
     const int first = slice * p.slice_blocks, last = min(first + p.slice_blocks, p.kb);   // blocks of columns
     F8Tile t = {0, tt * S::kToks, min(S::kToks, p.rows - tt * S::kToks), 0};
     if (p.tiles) t = p.tiles[tt];
@@ -580,7 +584,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
     const int ln = lane & 15, kg = lane >> 4;
     const int nrt = (p.out + 255) / 256;
     int rt, tt, slice;
-    if (!tile_of(p, nrt, rt, tt, slice)) return;
+    if (!tile_of(p, nrt, p.tiles ? 8 : 4, rt, tt, slice)) return;
     const int first = slice * p.slice_blocks, last = min(first + p.slice_blocks, p.kb);   // blocks of columns
     F8Tile t = {0, tt * 256, min(256, p.rows - tt * 256), 0};
     if (p.tiles) t = p.tiles[tt];
@@ -816,8 +820,7 @@ static hipError_t tiles256(const F8Params& p, hipStream_t st) {
 
 template <int FR, int FT, int DEPTH, int MODE, int T>
 static void slices_as(const F8Params& p, hipStream_t st) {
-    const int nrt = (p.out + 16 * FR - 1) / (16 * FR);
-    hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, MODE, T>), dim3(unsigned(8 * ((nrt + 7) / 8)) * unsigned(p.n_tiles)), dim3(512), 0, st, p);
+    hipLaunchKernelGGL((k_f8_slices<FR, FT, DEPTH, MODE, T>), dim3(tile_grid(p, 16 * FR)), dim3(512), 0, st, p);
 }
 template <int FR, int FT, int DEPTH, int T>
 static hipError_t slices_of(const F8Params& p, hipStream_t st) {
@@ -845,36 +848,36 @@ constexpr F8KernelShape kShapes[] = {{kSlices16, 16, 16}, {kSlices16Wide, 64, 16
 static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * column slices, 0 = the choice below
 void f8_force_kernel(int kernel) { g_forced = kernel; }
 
-// Duration in microseconds.  The constants were fitted to timings of every kernel on 65 products (1 to 3660 rows, 256 to 28672 x 512 to 14336, up to 64
-// experts, all types): what they choose is 0.7 % slower than the fastest, in the mean, 18 % at most.
+// Duration in microseconds.  The constants were fitted to timings of every kernel on 88 products (1 to 3660 rows, 256 to 28672 x 512 to 14336, up to 64
+// experts, all types): what they choose is 1.0 % slower than the fastest, in the mean, 15 % at most.
 static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, int kb, int experts, bool grouped, bool exact, bool ws_f32) {
     // tiles of y's rows that have any: a group fills its last one by half, in the mean
     const int groups = grouped ? std::min(rows, experts) : 1;
     const double mt = grouped ? std::max<double>(groups, double(rows) / k.toks + 0.5 * groups) : (rows + k.toks - 1) / k.toks;
     const double tiles = mt * ((out + k.rows - 1) / k.rows), rounds = tiles * slices / 256;
-    // the weights once, from memory
-    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.toks == 16 ? 4.5e6 : k.toks == 32 ? 3.4e6 : k.kernel == kSlices64 ? 2.7e6 : 5.1e6);
+    // the weights once, from memory, at the rate that a kernel was found to take them at most
+    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.kernel == kSlices64 ? 2.7e6 : k.kernel == kSlices32 ? 9e6 : 5.4e6);
     const double passes = (kb + 7) / 8, steps = (kb + slices - 1) / slices;
-    double us = 4.9;
+    double us = 4.15;
     switch (k.kernel) {
         case kSlices16: {   // up to four workgroups on a compute unit
             const double whole = std::floor(rounds / 4), rest = rounds - 4 * whole;
-            us = 3.5 + passes * (whole * 4.1 + (rest > 0 ? 0.14 + 1.2 * rest : 0.0));
+            us = 3.5 + passes * (whole * 4.46 + (rest > 0 ? 0.14 + 1.15 * rest : 0.0));
             break;
         }
-        case kSlices16Wide: us = 4.0 + passes * std::max(1.9, 1.1 + (exact ? 2.7 : 2.2) * rounds); break;   // two
-        case kSlices32: us = 4.0 + passes * std::max(2.3, 1.1 + (exact ? 3.5 : 3.0) * rounds); break;
-        case kSlices64: us = 4.0 + passes * std::ceil(rounds) * 4.2; break;
+        case kSlices16Wide: us = 4.0 + passes * std::max(1.93, 0.9 + (exact ? 3.08 : 2.48) * rounds); break;   // two
+        case kSlices32: us = 4.0 + passes * std::max(2.3, 0.9 + (exact ? 3.86 : 3.08) * rounds); break;
+        case kSlices64: us = 4.0 + passes * std::ceil(rounds) * 4.47; break;
         case kTile64: {   // two, which take less than twice as long as one
-            const double one = exact ? 0.81 : 0.53, two = exact ? 1.43 : 0.83, whole = std::floor(rounds / 2), rest = rounds - 2 * whole;
+            const double one = exact ? 0.88 : 0.542, two = exact ? 1.47 : 0.905, whole = std::floor(rounds / 2), rest = rounds - 2 * whole;
             us += steps * (whole * two + (rest > 1 ? two : rest > 0 ? one : 0.0));
             break;
         }
-        case kTile128: us += steps * std::ceil(rounds) * (exact ? 1.35 : 0.71); break;
-        case kTile128Wide: us += steps * std::ceil(rounds) * 1.02; break;
-        default: us += steps * std::ceil(rounds) * (ws_f32 ? 1.72 : 1.48);
+        case kTile128: us += steps * std::ceil(rounds) * (exact ? 1.46 : 0.78); break;
+        case kTile128Wide: us += steps * std::ceil(rounds) * 1.08; break;
+        default: us += steps * std::ceil(rounds) * (ws_f32 ? 1.87 : 1.61);
     }
-    return std::max(us, stream) + (slices > 1 ? 3.0 + slices * tiles * k.rows * k.toks * 8 / 5e6 : 0.0);
+    return std::max(us, stream) + (slices > 1 ? 4.0 + slices * tiles * k.rows * k.toks * 8 / 6.3e6 : 0.0);
 }
 
 // Kernel and column slices of a product, from sizes alone (the workspace holds the partial sums)
@@ -885,6 +888,8 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact,
     for (const F8KernelShape& k : kShapes) {
         if (!forced && rows <= 16 && k.toks > 16) break;   // never faster
         if (exact && k.kernel >= kTile128Wide) continue;   // the operands as fp16 leave no registers for its sums
+        // 1851 x 384 x 2048 in fp32: 14.6 us, 128 x 64 16.5; in 16 bits, where that has half the work, it is faster: 1920 x 272 x 1024 9.4, 7.9
+        if (!exact && k.kernel == kSlices64) continue;
         for (int slices : {1, 2, 3, 4, 5, 6, 7, 8, 12, 16}) {
             if (forced ? k.kernel != forced % 1024 || slices > 1 : slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
             const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact, ws_f32);
@@ -918,7 +923,9 @@ hipError_t launch_f8_product(const F8Params& args, const F8Plan& plan, hipStream
         case kSlices16: return slices<1, 1, 2>(p, st);
         case kSlices16Wide: return slices<4, 1, 1>(p, st);
         case kSlices32: return slices<4, 2, 1>(p, st);
-        case kSlices64: return slices<4, 4, 1>(p, st);
+        case kSlices64:
+            slices_as<4, 4, 1, kModeExact, BITSTACK_T_F8>(p, st);
+            return hipGetLastError();
         case kTile64:
             if (exact) return tiles<2, 2, 4, 2, kModeExact>(p, st);
             return p.ws_f32 ? tiles<2, 2, 4, 2, kModeF32>(p, st) : tiles<2, 2, 4, 2, kModeE8M0>(p, st);
