@@ -563,8 +563,9 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
 // requested in turn: the weight in even phases; the tokens in odd ones, a step earlier, those that the first wavefronts read into the
 // buffer that these have just read, the others' into a ring of three.
 //   Up to 128 tokens the last four wavefronts have none and only load.
-//   28672 x 8192, 2048 tokens: 393 us, 2.45 PFLOP/s; the matrix cores work in 56 % of the clocks (both operands requested in one phase: 37 %, 460 us), of which
-// there are then 2.0 in a nanosecond and not 2.35: power is the bound.  Without the loads it takes 279 us, without the products 290.
+//   28672 x 8192, 2048 tokens: 390 us, 2.47 PFLOP/s, 8192 x 8192, 8192 tokens 415, 2.65; the matrix cores work in 56 % of the clocks (both operands requested in one
+// phase: 37 %, 460 us), of which there are then 2.0 in a nanosecond and not 2.35: power is the bound.  Without the loads it takes 279 us, without the
+// products 290.  fp32 scales of the weight cost 20 % more: four multiply-adds a matrix instruction.
 constexpr unsigned kBigW = 32768, kBigX = 16384, kBigS = 1024;                                          // bytes of a buffer
 constexpr unsigned kBigEarly = 2 * kBigW, kBigLate = kBigEarly + 2 * kBigX, kBigScales = kBigLate + 3 * kBigX;
 struct F8BigShape {
@@ -754,7 +755,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
 }
 
 // y from the partial sums of p.slices column slices, added up in order: a wavefront takes what one of k_f8_tile's held of a tile, FR fragments
-// of 4 rows a lane at a time, which are 4 FR neighbouring outputs of a token.
+// of 4 rows a lane at a time, which are 4 FR neighbouring outputs of a token.  Bound by memory and the launch: five slices of 300 x 4096, 25 MB, 6.8 us.
 template <int FR, int FT, int WR, int WT>
 __global__ __launch_bounds__(256) void k_f8_join(F8Params p) {
     const int lane = threadIdx.x & 63, ln = lane & 15, kg = lane >> 4;
@@ -849,14 +850,14 @@ static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * colu
 void f8_force_kernel(int kernel) { g_forced = kernel; }
 
 // Duration in microseconds.  The constants were fitted to timings of every kernel on 88 products (1 to 3660 rows, 256 to 28672 x 512 to 14336, up to 64
-// experts, all types): what they choose is 1.0 % slower than the fastest, in the mean, 15 % at most.
+// experts, all types): what they choose is 1.1 % slower than the fastest, in the mean, 15 % at most.
 static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, int kb, int experts, bool grouped, bool exact, bool ws_f32) {
     // tiles of y's rows that have any: a group fills its last one by half, in the mean
     const int groups = grouped ? std::min(rows, experts) : 1;
     const double mt = grouped ? std::max<double>(groups, double(rows) / k.toks + 0.5 * groups) : (rows + k.toks - 1) / k.toks;
     const double tiles = mt * ((out + k.rows - 1) / k.rows), rounds = tiles * slices / 256;
     // the weights once, from memory, at the rate that a kernel was found to take them at most
-    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.kernel == kSlices64 ? 2.7e6 : k.kernel == kSlices32 ? 9e6 : 5.4e6);
+    const double stream = 4.0 + double(groups) * out * kb * 128 / (k.kernel == kSlices64 ? 2.7e6 : 5.4e6);
     const double passes = (kb + 7) / 8, steps = (kb + slices - 1) / slices;
     double us = 4.15;
     switch (k.kernel) {
