@@ -341,11 +341,21 @@ __global__ __launch_bounds__(256) void k_combine(CombineParams p) {
     }
 }
 
+template <int T>
+static void combine(CombineParams p, hipStream_t st) {
+    constexpr int kMost = 1 << 23;   // workgroups: a launch takes fewer than 2^32 threads
+    for (; p.tokens > 0; p.tokens -= kMost) {
+        hipLaunchKernelGGL((k_combine<T>), dim3(unsigned(std::min(p.tokens, kMost)), unsigned((p.width + 2047) / 2048)), dim3(256), 0, st, p);
+        p.slots += size_t(kMost) * p.top_k;
+        p.weights += size_t(kMost) * p.top_k;
+        p.y = static_cast<typename Elem<T>::type*>(p.y) + size_t(kMost) * p.ld_y;
+    }
+}
+
 hipError_t launch_combine(const CombineParams& p, int dtype, hipStream_t st) {
-    const dim3 grid(unsigned(p.tokens), unsigned((p.width + 2047) / 2048));
-    if (dtype == BITSTACK_T_F16) hipLaunchKernelGGL((k_combine<BITSTACK_T_F16>), grid, dim3(256), 0, st, p);
-    else if (dtype == BITSTACK_T_BF16) hipLaunchKernelGGL((k_combine<BITSTACK_T_BF16>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((k_combine<BITSTACK_T_F32>), grid, dim3(256), 0, st, p);
+    if (dtype == BITSTACK_T_F16) combine<BITSTACK_T_F16>(p, st);
+    else if (dtype == BITSTACK_T_BF16) combine<BITSTACK_T_BF16>(p, st);
+    else combine<BITSTACK_T_F32>(p, st);
     return hipGetLastError();
 }
 

@@ -182,7 +182,8 @@ def _fill_weight(q, scales, grouped):
     ld = stride[-2] if out > 1 else -(-inn // 16) * 16
     _need(e == 1 or stride[0] == out * ld, "q: the experts' weights have to follow one another")
     want = (-(-out // 128), -(-inn // 128))
-    _need(scales.shape == ((e, *want) if grouped else want) and scales.is_contiguous(), f"scales: one for each 128 x 128 block of q, {want}, contiguous")
+    if scales.shape != ((e, *want) if grouped else want) or not scales.is_contiguous():
+        raise ValueError(f"scales: one for each 128 x 128 block of q, {want}, contiguous")
     w = _args.w
     w.q, w.ld, w.scales, w.scale_type, w.out, w.inn, w.experts = q.data_ptr(), ld, scales.data_ptr(), kind, out, inn, e
     return out, inn, e
@@ -193,7 +194,8 @@ def _fill_rows(x, inn, gated):
     if isinstance(x, F8Rows):
         _need(not gated, "gated: apply it in quantise_f8")
         L = _f8_lib()
-        _need(x.width == inn, f"x has {x.width} columns, the weight {inn}")
+        if x.width != inn:
+            raise ValueError(f"x has {x.width} columns, the weight {inn}")
         _need(x.q.dtype is torch.float8_e4m3fn and x.q.is_contiguous() and x.scales.is_contiguous() and x.scales.element_size() == 1
               and tuple(x.q.shape[1:]) == (L.bitstack_f8_row_bytes(inn),) and tuple(x.scales.shape) == (L.bitstack_f8_row_scales(inn) // 4, x.q.shape[0], 4),
               "x: as quantise_f8 makes it")
@@ -222,16 +224,17 @@ def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, strea
     args = _args
     with _on(device, stream, (*held, q, scales, offsets, index, y, workspace)) as handle:
         if y is None:
-            y = torch.empty((rows, out), dtype=out_dtype or dtype, device=device)
+            y = q.new_empty((rows, out), dtype=out_dtype or dtype)
             ld_y = out
         else:
-            _need(y.shape == (rows, out) and (out_dtype is None or y.dtype is out_dtype), f"y: [{rows}, {out}] is needed")
+            if y.shape != (rows, out) or (out_dtype is not None and y.dtype is not out_dtype):
+                raise ValueError(f"y: [{rows}, {out}] is needed")
             ld_y = _matrix(y, "y")
         t = _type(y, "y")
         if workspace is None:
             nbytes = L.bitstack_f8_call_workspace_bytes(args.xp, args.wp, rows, t, grouped)
             if nbytes:
-                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+                workspace = q.new_empty(nbytes, dtype=torch.uint8)
         else:
             _need(workspace.is_contiguous(), "workspace: contiguous")
             nbytes = workspace.numel() * workspace.element_size()
@@ -328,7 +331,7 @@ def combine(h, slots, weights, *, y=None, stream=None):
     n, k = slots.shape
     with _on(h.device, stream, (h, slots, weights, y)) as handle:
         if y is None:
-            y = torch.empty((n, h.shape[1]), dtype=h.dtype, device=h.device)
+            y = h.new_empty((n, h.shape[1]))
         else:
             _need(tuple(y.shape) == (n, h.shape[1]) and y.dtype is h.dtype, "y: [tokens, width] of h's type")
         _check(L.bitstack_combine(h.data_ptr(), t, ld, h.shape[0], h.shape[1], slots.data_ptr(), weights.data_ptr(), n, k, y.data_ptr(), _matrix(y, "y"),

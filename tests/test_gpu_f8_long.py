@@ -83,3 +83,13 @@ def test_quantise_past_4_gib():
     r = B.quantise_f8(x)
     v = r.q.view(torch.uint8)
     assert not v[:-2].any() and torch.equal(B.F8Rows(r.q[-2:], r.scales[:, -2:].contiguous(), 512).values(), x[-2:])
+
+
+def test_combine_of_many_tokens():
+    """more tokens than a launch has workgroups"""
+    n, width = 20_000_001, 3
+    h = torch.arange(12, device=DEV).view(4, width).to(F16)
+    slots = (torch.arange(n, device=DEV) % 5 - 1).to(torch.int32).view(n, 1)   # -1: nothing
+    y = B.combine(h, slots, torch.full((n, 1), 2.0, device=DEV))
+    want = torch.cat([torch.zeros((1, width), dtype=F16, device=DEV), 2 * h])
+    assert torch.equal(y[: n // 5 * 5].view(-1, 5, width), want.expand(n // 5, 5, width)) and torch.equal(y[n // 5 * 5 :], want[: n % 5])
