@@ -322,19 +322,18 @@ __global__ __launch_bounds__(256) void k_combine(CombineParams p) {
         if (unsigned(slot) >= unsigned(p.h_rows)) continue;
         const float w = p.weights[size_t(token) * p.top_k + j];
         float v[8];
-        load_elems<T, 8>(static_cast<const E*>(p.h) + size_t(slot) * p.ld_h + col, p.width - col, p.vec, v);
+        load_elems<T, 8>(static_cast<const E*>(p.h) + size_t(slot) * p.ld_h + col, p.width - col, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
     }
     E* const y = static_cast<E*>(p.y) + size_t(token) * p.ld_y + col;
-    if (p.vec && p.width - col >= 8) {
-        typedef E piece __attribute__((ext_vector_type(Elem<T>::kPer16)));
+    if (p.width - col >= 8) {
 #pragma unroll
         for (int i = 0; i < 8 / Elem<T>::kPer16; ++i) {
-            piece u;
+            typename Piece<T>::type u;
 #pragma unroll
             for (int e = 0; e < Elem<T>::kPer16; ++e) u[e] = E(sum[i * Elem<T>::kPer16 + e]);
-            reinterpret_cast<piece*>(y)[i] = u;
+            reinterpret_cast<typename Piece<T>::loose*>(y)[i] = u;
         }
     } else {
         for (int i = 0; i < 8 && col + i < p.width; ++i) y[i] = E(sum[i]);

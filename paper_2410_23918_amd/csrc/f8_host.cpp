@@ -123,8 +123,6 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     p.rows = y_rows;
     p.y_dtype = y_dtype;
     p.ws_f32 = w->scale_type == BITSTACK_S_F32;
-    p.y_vec = ld_y % 4 == 0 && !misaligned(y, 4 * type_size(y_dtype));
-    p.y_vec16 = ld_y * type_size(y_dtype) % 16 == 0 && !misaligned(y, 16);
     const hipError_t e = launch_f8_product(p, plan, st);
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }
@@ -228,8 +226,7 @@ int bitstack_combine(const void* h, int dtype, size_t ld_h, int h_rows, int widt
     const size_t size = type_size(dtype);
     if (misaligned(h, size) || misaligned(y, size) || misaligned(slots, 4) || misaligned(weights, 4)) return BITSTACK_E_ALIGN;
     if ((h_rows > 1 && ld_h < size_t(width)) || (tokens > 1 && ld_y < size_t(width))) return BITSTACK_E_SHAPE;
-    const int vec = !misaligned(h, 16) && !misaligned(y, 16) && ld_h * size % 16 == 0 && ld_y * size % 16 == 0;
-    const CombineParams p{h, y, slots, weights, ld_h, ld_y, h_rows, width, tokens, top_k, vec};
+    const CombineParams p{h, y, slots, weights, ld_h, ld_y, h_rows, width, tokens, top_k};
     const hipError_t e = launch_combine(p, dtype, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }

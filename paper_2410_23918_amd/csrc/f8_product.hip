@@ -43,30 +43,23 @@ __device__ __forceinline__ v4i keep_columns(v4i v, int n) {
 }
 
 // four outputs of a token, rows n .. n + 3
-__device__ __forceinline__ void store4(const F8Params& p, int row, int n, const v4f& v) {
-    if (n >= p.out) return;
-    const size_t at = size_t(row) * p.ldy + n;
-    const bool whole = p.y_vec && n + 4 <= p.out;
-    if (p.y_dtype == BITSTACK_T_F32) {
-        float* const y = static_cast<float*>(p.y) + at;
-        if (whole) *reinterpret_cast<v4f*>(y) = v;
-        else
-            for (int i = 0; i < 4 && n + i < p.out; ++i) y[i] = v[i];
-    } else if (p.y_dtype == BITSTACK_T_F16) {
-        typedef _Float16 v4h __attribute__((ext_vector_type(4)));
-        const v4h h = {_Float16(v[0]), _Float16(v[1]), _Float16(v[2]), _Float16(v[3])};
-        _Float16* const y = static_cast<_Float16*>(p.y) + at;
-        if (whole) *reinterpret_cast<v4h*>(y) = h;
-        else
-            for (int i = 0; i < 4 && n + i < p.out; ++i) y[i] = h[i];
+template <int T>
+__device__ __forceinline__ void store4_as(const F8Params& p, int row, int n, const v4f& v) {
+    typedef typename Elem<T>::type E;
+    typedef E four __attribute__((ext_vector_type(4)));
+    typedef four loose __attribute__((aligned(sizeof(E))));
+    const four o = {E(v[0]), E(v[1]), E(v[2]), E(v[3])};
+    E* const y = static_cast<E*>(p.y) + size_t(row) * p.ldy + n;
+    if (n + 4 <= p.out) {
+        *reinterpret_cast<loose*>(y) = o;
     } else {
-        typedef __bf16 v4b __attribute__((ext_vector_type(4)));
-        const v4b h = {__bf16(v[0]), __bf16(v[1]), __bf16(v[2]), __bf16(v[3])};
-        __bf16* const y = static_cast<__bf16*>(p.y) + at;
-        if (whole) *reinterpret_cast<v4b*>(y) = h;
-        else
-            for (int i = 0; i < 4 && n + i < p.out; ++i) y[i] = h[i];
+        for (int i = 0; i < 4 && n + i < p.out; ++i) y[i] = o[i];
     }
+}
+__device__ __forceinline__ void store4(const F8Params& p, int row, int n, const v4f& v) {
+    if (p.y_dtype == BITSTACK_T_F32) store4_as<BITSTACK_T_F32>(p, row, n, v);
+    else if (p.y_dtype == BITSTACK_T_F16) store4_as<BITSTACK_T_F16>(p, row, n, v);
+    else store4_as<BITSTACK_T_BF16>(p, row, n, v);
 }
 
 template <class E>
@@ -381,8 +374,9 @@ __device__ __forceinline__ void finish_tile(const F8Params& p, unsigned char* sm
         if (n >= p.out) continue;
         const unsigned char* const from = smem + tok * kLd + piece * 16;
         unsigned char* const y = static_cast<unsigned char*>(p.y) + (size_t(row0 + tok) * p.ldy + n) * kSize;
-        if (p.y_vec16 && n + kEach <= p.out) {
-            *reinterpret_cast<v4i*>(y) = *reinterpret_cast<const v4i*>(from);
+        if (n + kEach <= p.out) {
+            typedef v4i loose __attribute__((aligned(2)));   // y lies at any element
+            *reinterpret_cast<loose*>(y) = *reinterpret_cast<const v4i*>(from);
         } else {
             for (int e = 0; e < kEach && n + e < p.out; ++e) {
                 if constexpr (kSize == 4) reinterpret_cast<float*>(y)[e] = reinterpret_cast<const float*>(from)[e];

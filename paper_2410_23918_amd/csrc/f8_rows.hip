@@ -63,7 +63,7 @@ __device__ void make_work_list(const F8WorkList& l) {
 // times over.  Bound by memory: x is read once and q written once, 16 and 8 bytes a lane and word: 2048 x 8192 in fp16 11.8 us, 4.3 TB/s; 2048 gated rows of
 // 2 x 14336 30.3 us, 4.8 TB/s.  The first workgroup makes the work list where there is one: a launch less.
 template <int T, bool GATED, int WORDS>
-__global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, int vec, unsigned char* q,
+__global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, unsigned char* q,
                                                      unsigned* s, int kp, F8WorkList list) {
     if (list.offsets && blockIdx.x == 0) {
         make_work_list(list);
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
     for (int k = 0; k < WORDS; ++k) {   // all requests first
         const int col = (word0 + k) * 512 + lane * 8;
         const typename Elem<T>::type* const from = x + size_t(row) * ld + col;
-        load_elems<T, 8>(from, in - col, vec, v[k]);
-        if constexpr (GATED) load_elems<T, 8>(from + in, in - col, vec, u[k]);
+        load_elems<T, 8>(from, in - col, v[k]);
+        if constexpr (GATED) load_elems<T, 8>(from + in, in - col, u[k]);
     }
 #pragma unroll
     for (int k = 0; k < WORDS; ++k) {
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
 // A workgroup brings a block of 128 rows x 128 columns to 8 bits: sixteen lanes a row, sixteen rows a pass, the values in registers between
 // the maximum and the rounding, so that w is read once.  Bound by memory: 28672 x 8192 in fp16 130 us, 5.4 TB/s.
 template <int T>
-__global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<T>::type* w, size_t ld, int out, int in, int vec,
+__global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<T>::type* w, size_t ld, int out, int in,
                                                             unsigned char* q, size_t ld_q, int q_cols, unsigned char* s, int kb) {
     __shared__ unsigned most[4];
     const int kblock = blockIdx.x % kb, nblock = blockIdx.x / kb;
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int row = nblock * kF8Block + i * 16 + (threadIdx.x >> 4);
-        load_elems<T, 8>(w + size_t(row) * ld + col, row < out ? in - col : 0, vec, v[i]);
+        load_elems<T, 8>(w + size_t(row) * ld + col, row < out ? in - col : 0, v[i]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) m = max(m, f8_magnitude(v[i][k]));
     }
@@ -143,20 +143,16 @@ __global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<
     if (threadIdx.x == 0) s[size_t(nblock) * kb + kblock] = (unsigned char)e;
 }
 
-static bool vector_rows(const void* p, size_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0; }
-
 template <int T>
 static void quantise(const void* x, size_t ld, int rows, int in, bool gated, unsigned char* q, unsigned char* s, const F8WorkList& list, hipStream_t st) {
     typedef typename Elem<T>::type E;
     const int kp = (in + 127) / 128 * 128;
-    // the halves of a gated row begin `in` elements apart
-    const int vec = vector_rows(x, ld, sizeof(E)) && (!gated || size_t(in) * sizeof(E) % 16 == 0);
     unsigned* const words = reinterpret_cast<unsigned*>(s);
     // Gated rows, whose arithmetic hides no latency: four words a wavefront where that leaves enough wavefronts
     const int each = gated && size_t(rows) * ((kp + 2047) / 2048) >= 4096 ? 4 : 1;
     const size_t waves = size_t(rows) * ((kp + 512 * each - 1) / (512 * each));
     const unsigned grid = unsigned((waves + 3) / 4) + (list.offsets ? 1 : 0);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, vec, q, words, kp, list); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, static_cast<const E*>(x), ld, rows, in, q, words, kp, list); };
     if (gated) each == 4 ? go(&k_f8_quantise<T, true, 4>) : go(&k_f8_quantise<T, true, 1>);
     else go(&k_f8_quantise<T, false, 1>);
 }
@@ -175,7 +171,7 @@ static void quantise_weight(const void* w, size_t ld, int out, int in, unsigned 
     const int kb = (in + 127) / 128, nb = (out + 127) / 128;
     const int q_cols = int(ld_q < size_t(kb) * 128 ? ld_q : size_t(kb) * 128);   // written: what lies past `in` as zero
     hipLaunchKernelGGL((k_f8_quantise_weight<T>), dim3(unsigned(size_t(kb) * nb)), dim3(256), 0, st, static_cast<const E*>(w), ld, out, in,
-                       int(vector_rows(w, ld, sizeof(E))), q, ld_q, q_cols, s, kb);
+                       q, ld_q, q_cols, s, kb);
 }
 
 hipError_t launch_f8_quantise_weight(const void* w, int dtype, size_t ld, int out, int in, unsigned char* q, size_t ld_q,
