@@ -4,7 +4,8 @@
 //
 // and the same with the rows of y grouped by expert.  v_mfma_scale_f32_16x16x128_f8f6f4 multiplies one block of 16 rows and 16 tokens and
 // takes powers of two as scales of its operands: those of the activations, and those of weights that hold them so, cost nothing.
-// A weight's fp32 scale is the same for the whole block: the product goes into zeros and is added with it.
+// A weight's fp32 scale is the same for the whole block: its power of two goes to the instruction too, the product goes into zeros and is added
+// times the rest.
 //   That instruction (and the unscaled one for 8 bits) adds eight neighbouring columns at a time, with every product cut to a multiple of
 // 2^-13 of the largest one's power of two; what it adds these sums to is fp32.  (Measured: 2^16 + 2^2 loses its second term within eight columns, 2^16 + 2^3 does
 // not; across them 24 bits are kept.)  Outputs of 16 bits are coarser: 5e-5 of y's norm with a few columns 30 times louder than the rest, 4.9e-4 is
@@ -29,7 +30,6 @@ __device__ __forceinline__ v4f mfma_f8(const v8i& w, const v8i& x, const v4f& c,
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, w_scale, 0, x_scale);
 }
 constexpr int kOne = 127;   // the scale 1
-
 __device__ __forceinline__ v8i join(const v4i& a, const v4i& b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
 // zeroes the bytes of a 16-byte piece from its column `n` on (n may be anything)
@@ -71,8 +71,18 @@ __device__ __forceinline__ v2u pack4(const v4f& v) {
 // How a tile is multiplied: the scales of the weight are powers of two, or fp32 numbers; or the outputs are fp32 (either scales)
 enum F8Mode { kModeE8M0, kModeF32, kModeExact };
 
-__device__ __forceinline__ float scale_of(int byte) {   // 2^(byte - 127), 255: NaN
-    return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : unsigned(byte) << 23);
+// A block's scale of the weight (sw, in bits, the same in all lanes) as factor * 2^(byte - 127), in scalar registers.  An fp32 scale's power of two is taken
+// off it and goes where that of the activations is, so that nothing passes fp32's range, or drops below it, on the way to a y that does not; the
+// factor is in [1, 2) (0, less than 1 for a denormal scale, or no number).
+struct WeightScale {
+    int byte;
+    float factor;
+};
+__device__ __forceinline__ WeightScale weight_scale(int sw, bool sw_f32) {
+    sw = __builtin_amdgcn_readfirstlane(sw);
+    if (!sw_f32) return {sw, sw == 255 ? __uint_as_float(0x7fc00000u) : 1.0f};
+    const int byte = min(max(sw >> 23 & 255, 1), 254);
+    return {byte, __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(__builtin_amdgcn_ldexpf(__int_as_float(sw), kOne - byte))))};
 }
 
 // 32 e4m3 numbers as fp16, exactly
@@ -100,11 +110,14 @@ __device__ __forceinline__ v4f mfma_halves(const Halves& w, const Halves& x) {
 }
 
 // acc += a block's products of FR fragments of the weight and one of the activations, with their scales (xs: of the lane's token; sw: the
-// weight's, in bits).  D's columns are the tokens: a lane's four results have one scale.
+// weight's).  D's columns are the tokens: a lane's four results have one scale.
 template <int FR, int MODE, class Weights>
-__device__ __forceinline__ void multiply(v4f* const (&acc)[FR], const Weights (&w)[FR], const v8i& x, int xs, int sw, bool sw_f32) {
+__device__ __forceinline__ void multiply(v4f* const (&acc)[FR], const Weights (&w)[FR], const v8i& x, int xs, const WeightScale& sw) {
     if constexpr (MODE == kModeExact) {
-        const float f = sw_f32 ? __int_as_float(sw) : scale_of(sw), g = scale_of(xs);
+        // Both powers of two in two halves: a block's sum lies between 2^-18 and 2^25, and neither half takes it out of range where y is not.  One
+        // rounding, that of the sum.
+        const int e = sw.byte + xs - 2 * kOne, half = e >> 1;   // half >= -127, where 0 will do
+        const float f = __builtin_amdgcn_ldexpf(sw.factor, e - half), g = __int_as_float((half + 127) << 23);
         const Halves xh = to_halves(x);
 #pragma unroll
         for (int j = 0; j < FR; ++j) {
@@ -116,11 +129,11 @@ __device__ __forceinline__ void multiply(v4f* const (&acc)[FR], const Weights (&
 #pragma unroll
         for (int j = 0; j < FR; ++j) {
             if constexpr (MODE == kModeF32) {
-                const v4f part = mfma_f8(w[j], x, v4f{0.0f, 0.0f, 0.0f, 0.0f}, kOne, xs);
+                const v4f part = mfma_f8(w[j], x, v4f{0.0f, 0.0f, 0.0f, 0.0f}, sw.byte, xs);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) (*acc[j])[v] = fmaf(part[v], __int_as_float(sw), (*acc[j])[v]);
+                for (int v = 0; v < 4; ++v) (*acc[j])[v] = fmaf(part[v], sw.factor, (*acc[j])[v]);
             } else {
-                *acc[j] = mfma_f8(w[j], x, *acc[j], sw, xs);
+                *acc[j] = mfma_f8(w[j], x, *acc[j], sw.byte, xs);
             }
         }
     }
@@ -129,6 +142,7 @@ __device__ __forceinline__ void multiply(v4f* const (&acc)[FR], const Weights (&
 template <int FR, int FT, int MODE, class After>
 __device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[FR], const v8i (&x)[FT], const int (&xs)[FT], int sw, bool sw_f32, After after) {
     typedef typename std::conditional<MODE == kModeExact, Halves, v8i>::type Weights;
+    const WeightScale scale = weight_scale(sw, sw_f32);
     Weights f[FR];
 #pragma unroll
     for (int j = 0; j < FR; ++j) {
@@ -140,7 +154,7 @@ __device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[
         v4f* to[FR];
 #pragma unroll
         for (int j = 0; j < FR; ++j) to[j] = &acc[j][i];
-        multiply<FR, MODE>(to, f, x[i], xs[i], sw, sw_f32);
+        multiply<FR, MODE>(to, f, x[i], xs[i], scale);
         after(i);
     }
 }
@@ -287,7 +301,9 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
                 if constexpr (kRaw) columns_to_f8<T>(s.raw, x[i], s.xs[i]);
                 else x[i] = join(s.x[i][0], s.x[i][1]);
             }
-            multiply_all<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32, [](int) {});
+            multiply_all<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32, [](int) __attribute__((always_inline)) {
+                if constexpr (MODE == kModeExact && FT == 4) __builtin_amdgcn_sched_barrier(0);   // one fragment's conversions at a time: registers
+            });
         };
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) load(st[d], wave + 8 * d);
