@@ -179,7 +179,8 @@ def _fill_weight(q, scales, grouped):
     _need(len(shape) == (3 if grouped else 2) and (stride[-1] == 1 or shape[-1] == 1), "q: rows of e4m3, [out, in] or [experts, out, in]")
     out, inn = shape[-2], shape[-1]
     e = shape[0] if grouped else 1
-    ld = stride[-2] if out > 1 else -(-inn // 16) * 16
+    # experts of one row each: their distance is the rows'
+    ld = stride[-2] if out > 1 else stride[0] if e > 1 else -(-inn // 16) * 16
     _need(e == 1 or stride[0] == out * ld, "q: the experts' weights have to follow one another")
     want = (-(-out // 128), -(-inn // 128))
     if scales.shape != ((e, *want) if grouped else want) or not scales.is_contiguous():
