@@ -27,6 +27,7 @@ __device__ __forceinline__ void scan_lds(int* v, int n, OP op) {
 // wavefront, whose logits are under way together.  57 tokens, 8 experts: 6.1 us.  16384 tokens, 8 of 128 experts: 13.7 and 8.1 us, of which reading the
 // logits would be 1; 16 wavefronts on every compute unit choose for 64 tokens at a time.
 constexpr int kRouteStep = 64, kRouteChunks = 256;
+__host__ __device__ inline int route_steps(int tokens) { return tokens / kRouteStep + (tokens % kRouteStep ? 1 : 0); }   // any number of tokens
 
 // Orders like the logit; 0: not to be taken (NaN, -infinity)
 __device__ __forceinline__ unsigned route_key(float l) {
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(1024) void k_route_choose(RouteParams p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     RouteLds& s = *reinterpret_cast<RouteLds*>(smem);
     for (int e = threadIdx.x; e < p.experts; e += 1024) s.count[e] = s.base[e] = 0;
-    const int steps = (p.tokens + kRouteStep - 1) / kRouteStep, per_chunk = (steps + p.chunks - 1) / p.chunks;
+    const int steps = route_steps(p.tokens), per_chunk = (steps + p.chunks - 1) / p.chunks;
     for (int step = blockIdx.x * per_chunk; step < min(steps, int(blockIdx.x + 1) * per_chunk); ++step) {
         __syncthreads();
         choose_step<T, NL>(p, s, step * kRouteStep);
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(1024) void k_route_place(RouteParams p) {
     }
     __syncthreads();
     bases(p, s);
-    const int steps = (p.tokens + kRouteStep - 1) / kRouteStep, per_chunk = (steps + p.chunks - 1) / p.chunks;
+    const int steps = route_steps(p.tokens), per_chunk = (steps + p.chunks - 1) / p.chunks;
     for (int step = blockIdx.x * per_chunk; step < min(steps, int(blockIdx.x + 1) * per_chunk); ++step) {
         const int token0 = step * kRouteStep, n = min(kRouteStep, p.tokens - token0) * p.top_k;
         for (int i = threadIdx.x; i < n; i += 1024) s.chosen[i] = short(p.chosen[size_t(token0) * p.top_k + i]);
@@ -302,7 +303,7 @@ static hipError_t route_of(const RouteParams& p, hipStream_t st) {
 
 hipError_t launch_route(RouteParams p, int dtype, void* workspace, hipStream_t st) {
     p.counts = static_cast<int*>(workspace);
-    const int steps = (p.tokens + kRouteStep - 1) / kRouteStep;
+    const int steps = route_steps(p.tokens);
     p.chunks = std::max(1, std::min(steps, kRouteChunks));
     if (dtype == BITSTACK_T_F16) return route_of<BITSTACK_T_F16>(p, st);
     if (dtype == BITSTACK_T_BF16) return route_of<BITSTACK_T_BF16>(p, st);
