@@ -83,9 +83,11 @@ typedef struct bitstack_f8_rows {
 
 /* Workspace of the two calls below (caller-owned, 256-byte aligned, free for other use once the stream has passed the
  * call): the 8-bit form of x_rows rows of `in` columns, the work list of y_rows rows in `experts` groups and partial sums.
- * Enough for any type of x and y and either call; 0 for unsupported sizes. */
+ * Enough for any type of x and y and either call, and for fewer rows: where the partial sums of fewer rows need more (up to some
+ * hundred MB), a call takes fewer slices of the columns than it would with bitstack_f8_call_workspace_bytes, in more time and with its sums
+ * in another order.  0 for unsupported sizes. */
 size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int experts);
-/* The same for one call (grouped: bitstack_f8_grouped_linear; the pointers in x and w are not followed).  0: the call needs none,
+/* What one call takes at most (grouped: bitstack_f8_grouped_linear; the pointers in x and w are not followed).  0: the call needs none,
  * workspace may be NULL (or it will be refused). */
 size_t bitstack_f8_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, int y_rows, int y_dtype,
                                         int grouped);

@@ -116,7 +116,8 @@ struct F8Plan {
     int tiles;                                // of the weight's rows and y's
     size_t part_bytes;                        // partial sums
 };
-F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32);
+// room: bytes for the work list and the partial sums; with less than they need there are fewer slices
+F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32, size_t room = ~size_t(0));
 hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
 void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
 

@@ -31,6 +31,12 @@ Workspace workspace_of(int x_rows, int in, const F8Plan& plan, bool raw, bool gr
     w.total = w.part + align256(plan.part_bytes);
     return w;
 }
+// The least that calls with up to so many rows run in, whichever their kernels: the work list of the smallest tiles, no partial sums
+size_t least_workspace(int x_rows, int in, int y_rows, int experts) {
+    F8Plan plan{};
+    plan.n_tiles = y_rows / 16 + 1 + (y_rows < experts ? y_rows : experts);
+    return workspace_of(x_rows, in, plan, false, true).total;
+}
 
 int check_rows(const bitstack_f8_rows_t& x, int in) {
     if (x.rows < 0) return BITSTACK_E_RANGE;
@@ -74,12 +80,19 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     if (misaligned(w->q, 16) || w->ld % 16 || (w->scale_type == BITSTACK_S_F32 && misaligned(w->scales, 4))) return BITSTACK_E_ALIGN;
     if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
-    const F8Plan plan = f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32);
+    auto plan_in = [&](size_t room) {
+        return f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32, room);
+    };
+    F8Plan plan = plan_in(~size_t(0));
     const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
-    const Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
+    Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {
         if (!workspace) return BITSTACK_E_NULL;
         if (misaligned(workspace, 256)) return BITSTACK_E_ALIGN;
+        if (workspace_bytes < at.total && plan.part_bytes) {   // made for more rows, whose columns need not be sliced: as many slices as fit
+            plan = plan_in(workspace_bytes < at.list ? 0 : workspace_bytes - at.list);
+            at = workspace_of(x->rows, w->in, plan, quantised, offsets != nullptr);
+        }
         if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -164,7 +177,7 @@ int bitstack_f8_quantise_weight(const void* w, int w_dtype, size_t ld, int out, 
 size_t bitstack_f8_workspace_bytes(int x_rows, int in, int y_rows, int out, int experts) {
     if (x_rows < 0 || y_rows < 0 || !columns_ok(in) || out < 1 || out > kMaxOut || experts < 1 || experts > kMaxExperts) return 0;
     if (size_t(x_rows) * bitstack_f8_row_bytes(in) > kMaxRowBytes) return 0;
-    size_t most = 256;
+    size_t most = least_workspace(x_rows, in, y_rows, experts);
     for (int k = 0; k < 8; ++k)
         if (y_rows) {
             const size_t n = workspace_of(x_rows, in, f8_plan(y_rows, out, in, experts, k & 1, k >> 1 & 1, k >> 2), false, true).total;

@@ -891,37 +891,41 @@ static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, 
     return std::max(us, stream) + (slices > 1 ? 4.0 + slices * tiles * k.rows * k.toks * 8 / 6.3e6 : 0.0);
 }
 
-// Kernel and column slices of a product, from sizes alone (the workspace holds the partial sums)
-F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32) {
+// Kernel and column slices of a product, from sizes alone, and from the room for the partial sums where that is too small for the fastest
+F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32, size_t room) {
     const int forced = g_forced.load(), kb = (in + 127) / 128;
-    F8Plan plan{kShapes[0].kernel, 1, 0, 0, 0, 0};
+    auto plan_of = [&](const F8KernelShape& k, int slices) {
+        const int each = (kb + slices - 1) / slices;
+        F8Plan plan{k.kernel, (kb + each - 1) / each, k.toks, 0, 0, 0};   // none of the slices empty
+        // every group's rows, rounded up to tiles, and those of the rows past the last group
+        plan.n_tiles = grouped ? rows / k.toks + 1 + std::min(rows, experts) : (rows + k.toks - 1) / k.toks;
+        const size_t tiles = size_t((out + k.rows - 1) / k.rows) * plan.n_tiles;
+        plan.tiles = int(std::min<size_t>(tiles, 0x7fffffff));
+        if (plan.slices > 1) plan.part_bytes = plan.slices * tiles * (k.rows * k.toks * 4);
+        return plan;
+    };
+    auto fits = [&](const F8Plan& plan) { return plan.slices == 1 || (grouped ? plan.n_tiles * sizeof(F8Tile) + 256 : 0) + plan.part_bytes <= room; };
+    F8Plan plan = plan_of(kShapes[0], 1);
     double best = 1e30;
     for (const F8KernelShape& k : kShapes) {
         if (!forced && rows <= 16 && k.toks > 16) break;   // never faster
         if (exact && k.kernel >= kTile128Wide) continue;   // the operands as fp16 leave no registers for its sums
         // 1851 x 384 x 2048 in fp32: 14.6 us, 128 x 64 16.5; in 16 bits, where that has half the work, it is faster: 1920 x 272 x 1024 9.4, 7.9
         if (!exact && k.kernel == kSlices64) continue;
+        if (forced) {
+            if (k.kernel == forced % 1024) return plan_of(k, k.kernel > kSlices64 ? std::max(1, std::min(forced / 1024, kb)) : 1);
+            continue;
+        }
         for (int slices : {1, 2, 3, 4, 5, 6, 7, 8, 12, 16}) {
-            if (forced ? k.kernel != forced % 1024 || slices > 1 : slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
+            if (slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
             const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact, ws_f32);
             if (us >= best) continue;
+            const F8Plan this_one = plan_of(k, slices);
+            if (!fits(this_one)) continue;
             best = us;
-            plan = {k.kernel, slices, k.toks, 0, 0, 0};
+            plan = this_one;
         }
     }
-    if (forced && forced % 1024 == plan.kernel && plan.kernel > kSlices64) plan.slices = std::max(1, std::min(forced / 1024, kb));
-    const int each = (kb + plan.slices - 1) / plan.slices;
-    plan.slices = (kb + each - 1) / each;   // none of them empty
-    plan.tile_rows = kShapes[0].toks;
-    for (const F8KernelShape& k : kShapes)
-        if (k.kernel == plan.kernel) {
-            plan.tile_rows = k.toks;
-            // every group's rows, rounded up to tiles, and those of the rows past the last group
-            plan.n_tiles = grouped ? rows / k.toks + 1 + std::min(rows, experts) : (rows + k.toks - 1) / k.toks;
-            const size_t tiles = size_t((out + k.rows - 1) / k.rows) * plan.n_tiles;
-            plan.tiles = int(std::min<size_t>(tiles, 0x7fffffff));
-            if (plan.slices > 1) plan.part_bytes = plan.slices * tiles * (k.rows * k.toks * 4);
-        }
     return plan;
 }
 hipError_t launch_f8_product(const F8Params& args, const F8Plan& plan, hipStream_t st) {

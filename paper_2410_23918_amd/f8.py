@@ -251,6 +251,8 @@ def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, strea
 
 
 def f8_workspace_bytes(x_rows: int, inn: int, y_rows: int, out: int, experts: int = 1) -> int:
+    """bitstack_f8_workspace_bytes: of a `workspace` for products with up to so many rows.  One that a call allocates for itself may be larger and then
+    makes it faster."""
     n = int(_f8_lib().bitstack_f8_workspace_bytes(x_rows, inn, y_rows, out, experts))
     if n == 0:
         raise BitStackError(-2, "bitstack_f8_workspace_bytes")
