@@ -36,7 +36,7 @@ enum { BITSTACK_T_F16 = 0, BITSTACK_T_F32 = 1, BITSTACK_T_BF16 = 2, BITSTACK_T_F
 enum { BITSTACK_S_E8M0 = 0, BITSTACK_S_F32 = 1 };
 
 /* Limits: 1 <= in <= 2^20, 1 <= out <= 2^24, up to 1024 experts, top_k up to 32; the rows of x below 2 GiB in 8 bits, the rows
- * of a weight at most 4 MiB apart. */
+ * of a weight at most 4 MiB apart; y of up to 2^23 tiles of 256 x 256 (fp32: 128 x 128), of which a group's last one may be in part empty. */
 
 /* ---- into 8 bits */
 

@@ -118,6 +118,8 @@ struct F8Plan {
 };
 // room: bytes for the work list and the partial sums; with less than they need there are fewer slices
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32, size_t room = ~size_t(0));
+// a launch has fewer than 2^32 threads, 512 to a workgroup
+inline bool f8_launchable(const F8Plan& plan) { return size_t(plan.tiles) * plan.slices <= (size_t(1) << 23) - 8; }
 hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
 void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
 

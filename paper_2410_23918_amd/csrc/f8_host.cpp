@@ -84,6 +84,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
         return f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32, room);
     };
     F8Plan plan = plan_in(~size_t(0));
+    if (!f8_launchable(plan)) return BITSTACK_E_RANGE;   // with any kernel's tiles
     const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
     Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {

@@ -921,7 +921,7 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact,
             const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact, ws_f32);
             if (us >= best) continue;
             const F8Plan this_one = plan_of(k, slices);
-            if (!fits(this_one)) continue;
+            if (!f8_launchable(this_one) || !fits(this_one)) continue;
             best = us;
             plan = this_one;
         }
