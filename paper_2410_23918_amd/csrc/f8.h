@@ -97,8 +97,17 @@ __device__ __forceinline__ unsigned f8_x4(float a, float b, float c, float d) {
 }
 // |v| as an integer that orders like it, NaN and infinity above all others
 __device__ __forceinline__ unsigned f8_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// g / (1 + exp(-g)) u, by the hardware's exp2 and reciprocal (1 ulp each): relative error (3 + |g| / 2) 2^-24
-__device__ __forceinline__ float f8_gate(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
+// g / (1 + exp(-g)) u by the hardware's exp2 and reciprocal (1 ulp each), relative error 8 * 2^-24 (of which they are 4).  -g / ln 2 is rounded, and at 50 that
+// is 50 half steps of the result: what it misses, in units of ln 2, comes after as a factor 1 + d.  Below -64 both terms of the denominator are taken 2^-64 times,
+// so that the product is there as long as fp32, denormals included, holds it (down to gates of -132).
+__device__ __forceinline__ float f8_gate(float g, float u) {
+    constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147182464599609375f, kLn2Rest = -1.904654299957767878e-9f;   // ln 2 = their sum
+    const float p = __builtin_amdgcn_fmed3f(g * -kLog2e, -150.0f, 250.0f);   // beyond, exp2 is 0 or infinite and g may be anything
+    const float d = fmaf(-kLn2Rest, p, fmaf(-kLn2, p, -g));
+    const bool far = g < -64.0f;
+    const float k = far ? 0x1p-64f : 1.0f;
+    return g * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(p - (far ? 64.0f : 0.0f)), 1.0f + d, k)) * u * k;
+}
 
 // The work list of a product grouped by expert: made by the launch that brings the activations to 8 bits, or (rows 0 there) by itself
 struct F8WorkList {
