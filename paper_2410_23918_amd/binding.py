@@ -535,6 +535,9 @@ class PackedStack:
 
         import torch
         from .f8 import quantise_weight_f8
+        # the caller's scratch is kept from reuse until the stream has passed the call
+        if stream is not None and w_dense is not None and stream != torch.cuda.current_stream(w_dense.device):
+            w_dense.record_stream(stream)
         # what is allocated here belongs to the stream that uses it
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
             return quantise_weight_f8(self.restore_weight(n_loaded, w_dense=w_dense, stream=stream), stream=stream)
