@@ -29,7 +29,9 @@ enum {
     BITSTACK_OPT_BATCH_TILES = 8,         /* row tiles per workgroup of the batch kernel: 2 or 4 (64 / 128 rows) */
     BITSTACK_OPT_F8_KERNEL = 10,          /* kernel of the 8-bit products, by its tile (rows of the weight x of y): 16 = 16 x 16,
                                              17 = 64 x 16, 32 = 64 x 32, 64 = 64 x 64, without LDS, 65 = 128 x 64, 128 = 128 x 128, 129 = 256 x 128,
-                                             256 = 256 x 256; + 1024 x the number of column slices (65 and up) */
+                                             256 = 256 x 256; + 1024 x the number of column slices (65 and up); others are
+                                             refused.  64 makes fp32 outputs only, 129 and 256 16-bit ones only: other
+                                             calls fall back */
     BITSTACK_OPT_ROWS_CHUNKS = 9          /* the batch kernel of one row tile per workgroup: 1, 2, 4 or 8 = always (up to 1024 tokens),
                                              with so many column chunks at a time where the stack has 8 / value
                                              blocks or more; 16 = never */

@@ -130,7 +130,7 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact,
 // a launch has fewer than 2^32 threads, 512 to a workgroup
 inline bool f8_launchable(const F8Plan& plan) { return size_t(plan.tiles) * plan.slices <= (size_t(1) << 23) - 8; }
 hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
-void f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size
+bool f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size; false: no such kernel
 
 size_t route_workspace_bytes(int tokens, int experts, int top_k);
 struct RouteParams {

@@ -857,7 +857,17 @@ struct F8KernelShape {
 constexpr F8KernelShape kShapes[] = {{kSlices16, 16, 16}, {kSlices16Wide, 64, 16}, {kSlices32, 64, 32}, {kSlices64, 64, 64}, {kTile64, 128, 64}, {kTile128, 128, 128}, {kTile128Wide, 256, 128}, {kTile256, 256, 256}};
 
 static std::atomic<int> g_forced{0};   // measurement hook: kernel + 1024 * column slices, 0 = the choice below
-void f8_force_kernel(int kernel) { g_forced = kernel; }
+bool f8_force_kernel(int kernel) {
+    bool known = kernel == 0;
+    for (const F8KernelShape& k : kShapes) known |= kernel % 1024 == k.kernel && (kernel < 1024 || k.kernel > kSlices64);
+    if (known) g_forced = kernel;
+    return known;
+}
+static bool makes(const F8KernelShape& k, bool exact) {
+    if (exact) return k.kernel < kTile128Wide;   // the operands as fp16 leave no registers for the larger tiles' sums
+    // 1851 x 384 x 2048 in fp32: 14.6 us, 128 x 64 16.5; in 16 bits, where that has half the work, it is faster: 1920 x 272 x 1024 9.4, 7.9
+    return k.kernel != kSlices64;
+}
 
 // Duration in microseconds.  The constants were fitted to timings of every kernel on 88 products (1 to 3660 rows, 256 to 28672 x 512 to 14336, up to 64
 // experts, all types): what they choose is 1.1 % slower than the fastest, in the mean, 15 % at most.
@@ -905,17 +915,13 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact,
         return plan;
     };
     auto fits = [&](const F8Plan& plan) { return plan.slices == 1 || (grouped ? plan.n_tiles * sizeof(F8Tile) + 256 : 0) + plan.part_bytes <= room; };
+    for (const F8KernelShape& k : kShapes)
+        if (forced && k.kernel == forced % 1024 && makes(k, exact)) return plan_of(k, std::max(1, std::min(forced / 1024, kb)));
     F8Plan plan = plan_of(kShapes[0], 1);
     double best = 1e30;
     for (const F8KernelShape& k : kShapes) {
-        if (!forced && rows <= 16 && k.toks > 16) break;   // never faster
-        if (exact && k.kernel >= kTile128Wide) continue;   // the operands as fp16 leave no registers for its sums
-        // 1851 x 384 x 2048 in fp32: 14.6 us, 128 x 64 16.5; in 16 bits, where that has half the work, it is faster: 1920 x 272 x 1024 9.4, 7.9
-        if (!exact && k.kernel == kSlices64) continue;
-        if (forced) {
-            if (k.kernel == forced % 1024) return plan_of(k, k.kernel > kSlices64 ? std::max(1, std::min(forced / 1024, kb)) : 1);
-            continue;
-        }
+        if (rows <= 16 && k.toks > 16) break;   // never faster
+        if (!makes(k, exact)) continue;
         for (int slices : {1, 2, 3, 4, 5, 6, 7, 8, 12, 16}) {
             if (slices > 1 && (k.kernel <= kSlices64 || slices > kb / 4)) continue;
             const double us = f8_time_us(k, slices, rows, out, kb, experts, grouped, exact, ws_f32);
