@@ -204,13 +204,14 @@ __device__ __forceinline__ bool tile_of(const F8Params& p, int nrt, unsigned tog
 // experts 24.9 us, 4.7 TB/s (16 rows as tokens stay in registers; tiles of 64 x 16, so that a block of the activations is read for 64 rows).  Small weights are bound by
 // the launch and three latencies (first load, LDS, store): 57 tokens through 1056 x 2001 in fp32, 16 x 16 tiles, 5.9 us.  With 32 and 64 tokens each
 // wavefront's operands come from L2 again for every 64 rows.
-//   T: type of the activations.  With one fragment of tokens they may come as they are and are brought to 8 bits on the way (a block of a token lies
-// in four lanes), by every workgroup anew: one launch instead of two.  One token through 1024 x 4096: 7.0 us, 5.5 and 2.4 + a launch for the rows
+//   T: type of the activations.  With one fragment of tokens they may come as they are, in no groups, and are brought to 8 bits on the way (a block of a token
+// lies in four lanes), by every workgroup anew: one launch instead of two.  One token through 1024 x 4096: 7.0 us, 5.5 and 2.4 + a launch for the rows
 // quantised before; 14336 x 4096 16.7, 16.2 and 2.4; 4096 x 14336, where 256 workgroups convert 112 blocks each, 20.4, 14.4 and 2.5.
 template <int FR, int FT, int DEPTH, int MODE, int T>
 __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
     constexpr bool kRaw = T != kRowsF8;
     static_assert(!kRaw || FT == 1, "one fragment of raw tokens");
+    if constexpr (kRaw) p.tiles = nullptr, p.index = nullptr;   // in no groups, rows as they come
     __shared__ v4f red[8 * FR * FT * 64];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
