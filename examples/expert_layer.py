@@ -24,10 +24,13 @@ class ExpertLayer:
     def from_stacks(cls, router, stacks1, stacks2, n_loaded: int, top_k: int):
         """the weights as the first n_loaded blocks of every expert's stacks give them; one fp16 scratch for all"""
         def all_of(stacks):
-            out, inn = stacks[0].out, stacks[0].inn
+            out, inn, e = stacks[0].out, stacks[0].inn, len(stacks)
             scratch = torch.empty((out, inn), dtype=torch.float16, device=router.device)
-            parts = [s.restore_weight_f8(n_loaded, w_dense=scratch) for s in stacks]
-            return torch.stack([q for q, _ in parts]), torch.stack([s for _, s in parts])
+            q = torch.empty((e, out, -(-inn // 128) * 128), dtype=torch.float8_e4m3fn, device=router.device)[:, :, :inn]
+            scales = torch.empty((e, -(-out // 128), -(-inn // 128)), dtype=torch.float8_e8m0fnu, device=router.device)
+            for i, stack in enumerate(stacks):   # each where it will lie among the others
+                stack.restore_weight_f8(n_loaded, w_dense=scratch, out=(q[i], scales[i]))
+            return q, scales
         return cls(router, all_of(stacks1), all_of(stacks2), top_k)
 
     def __call__(self, x):

@@ -528,19 +528,20 @@ class PackedStack:
                "bitstack_restore_weight")
         return w_dense
 
-    def restore_weight_f8(self, n_loaded: int, w_dense=None, stream=None):
+    def restore_weight_f8(self, n_loaded: int, w_dense=None, out=None, stream=None):
         """The loaded prefix in 8 bits, (q, scales) as linear_f8 takes them: bitstack_restore_weight into w_dense (an fp16 scratch
-        [out][in], allocated unless given), then bitstack_f8_quantise_weight."""
+        [out][in], allocated unless given), then bitstack_f8_quantise_weight (into `out` as in quantise_weight_f8)."""
         import contextlib
 
         import torch
         from .f8 import quantise_weight_f8
-        # the caller's scratch is kept from reuse until the stream has passed the call
-        if stream is not None and w_dense is not None and stream != torch.cuda.current_stream(w_dense.device):
-            w_dense.record_stream(stream)
+        # what the caller gives is kept from reuse until the stream has passed the call
+        for t in (w_dense, *(out or ())):
+            if stream is not None and t is not None and stream != torch.cuda.current_stream(t.device):
+                t.record_stream(stream)
         # what is allocated here belongs to the stream that uses it
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            return quantise_weight_f8(self.restore_weight(n_loaded, w_dense=w_dense, stream=stream), stream=stream)
+            return quantise_weight_f8(self.restore_weight(n_loaded, w_dense=w_dense, stream=stream), out=out, stream=stream)
 
     def _y_for(self, x, y, out_dtype):
         import torch

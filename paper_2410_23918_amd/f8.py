@@ -284,21 +284,42 @@ def quantise_f8(x, *, gated: bool = False, stream=None) -> F8Rows:
     return F8Rows(q, s, inn)
 
 
-def quantise_weight_f8(w, *, stream=None):
+def _f8_output(out, shape, device):
+    """(q, scales) that the caller gives to be written, as quantise_weight_f8 makes them or with rows closer together"""
+    q, s = out
+    e, rows, inn = shape
+    q3, s3 = (q, s) if q.dim() == 3 else (q[None], s[None])
+    _need(q.dtype is torch.float8_e4m3fn and tuple(q3.shape) == shape and (q3.stride(2) == 1 or inn == 1), f"out: q, float8_e4m3fn {list(shape[3 - q.dim():])}")
+    _need(s.dtype is torch.float8_e8m0fnu and tuple(s3.shape) == (e, -(-rows // 128), -(-inn // 128)) and s.is_contiguous(), "out: scales, float8_e8m0fnu, one for each 128 x 128 block, contiguous")
+    _same_device(device, q, s)
+    ld = q3.stride(1) if rows > 1 else -(-inn // 16) * 16
+    _need(e == 1 or (q3.stride(0) >= rows * ld and q3.stride(0) % 16 == 0), "out: q, experts a multiple of 16 bytes apart")
+    written = (e - 1) * q3.stride(0) + (rows - 1) * ld + min(ld, -(-inn // 128) * 128)
+    _need(q.storage_offset() + written <= q.untyped_storage().nbytes(), "out: q's last row ends with its last column: it is written up to a multiple of 16")
+    return q3, s3, ld
+
+
+def quantise_weight_f8(w, *, out=None, stream=None):
     """bitstack_f8_quantise_weight for w [out, in] or [experts, out, in] -> (q, scales), q's rows a multiple of 128 bytes apart and zero
-    past `in`."""
+    past `in`; or into `out`, such a pair whose rows may be any multiple of 16 bytes apart (zeroed past `in` up to there or to a multiple of 128)."""
     L = _f8_lib()
     _need(w.dim() in (2, 3), "w: [out, in] or [experts, out, in]")
     t = _type(w, "w")
     each = w if w.dim() == 3 else w[None]
-    e, out, inn = each.shape
-    ld_q = int(L.bitstack_f8_row_bytes(inn))
-    with _on(w.device, stream, (w,)) as handle:
-        q = torch.empty((e, out, ld_q), dtype=torch.float8_e4m3fn, device=w.device)
-        s = torch.empty((e, -(-out // 128), -(-inn // 128)), dtype=torch.float8_e8m0fnu, device=w.device)
+    e, rows, inn = each.shape
+    with _on(w.device, stream, (w, *(out or ()))) as handle:
+        if out is None:
+            ld_q = int(L.bitstack_f8_row_bytes(inn))
+            q = torch.empty((e, rows, ld_q), dtype=torch.float8_e4m3fn, device=w.device)
+            s = torch.empty((e, -(-rows // 128), -(-inn // 128)), dtype=torch.float8_e8m0fnu, device=w.device)
+        else:
+            _need(out[0].dim() == w.dim() and out[1].dim() == w.dim(), "out: q and scales of as many dimensions as w")
+            q, s, ld_q = _f8_output(out, (e, rows, inn), w.device)
         for i in range(e):
-            _check(L.bitstack_f8_quantise_weight(each[i].data_ptr(), t, _matrix(each[i], "w"), out, inn, q[i].data_ptr(), ld_q, s[i].data_ptr(),
+            _check(L.bitstack_f8_quantise_weight(each[i].data_ptr(), t, _matrix(each[i], "w"), rows, inn, q[i].data_ptr(), ld_q, s[i].data_ptr(),
                                                  handle), "bitstack_f8_quantise_weight")
+    if out is not None:
+        return out
     q = q[:, :, :inn]
     return (q, s) if w.dim() == 3 else (q[0], s[0])
 

@@ -32,7 +32,7 @@ def test_scratch_of_the_caller(monkeypatch, stream, kept):
     from paper_2410_23918_amd import f8
     monkeypatch.setattr(torch.cuda, "stream", entered)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1])
-    monkeypatch.setattr(f8, "quantise_weight_f8", lambda w, stream=None: (w, stream))
+    monkeypatch.setattr(f8, "quantise_weight_f8", lambda w, out=None, stream=None: (w, stream))
     monkeypatch.setattr(B.PackedStack, "restore_weight", lambda self, n_loaded, w_dense=None, stream=None: w_dense)
     scratch = Scratch()
     assert B.PackedStack.restore_weight_f8(object.__new__(B.PackedStack), 3, w_dense=scratch, stream=stream) == (scratch, stream)
