@@ -268,9 +268,9 @@ __global__ __launch_bounds__(1024) void k_route_place(RouteParams p) {
     }
 }
 
-size_t route_workspace_bytes(int tokens, int experts, int top_k) {
-    (void)tokens, (void)top_k;
-    return size_t(kRouteChunks) * experts * 4;
+static int route_chunks(int tokens) { return std::max(1, std::min(route_steps(tokens), kRouteChunks)); }
+size_t route_workspace_bytes(int tokens, int experts) {   // the chunks' counts; one chunk has them in LDS
+    return tokens <= kRouteStep ? 1 : size_t(route_chunks(tokens)) * experts * 4;
 }
 
 template <int T, int NL>
@@ -303,8 +303,7 @@ static hipError_t route_of(const RouteParams& p, hipStream_t st) {
 
 hipError_t launch_route(RouteParams p, int dtype, void* workspace, hipStream_t st) {
     p.counts = static_cast<int*>(workspace);
-    const int steps = route_steps(p.tokens);
-    p.chunks = std::max(1, std::min(steps, kRouteChunks));
+    p.chunks = route_chunks(p.tokens);
     if (dtype == BITSTACK_T_F16) return route_of<BITSTACK_T_F16>(p, st);
     if (dtype == BITSTACK_T_BF16) return route_of<BITSTACK_T_BF16>(p, st);
     return route_of<BITSTACK_T_F32>(p, st);

@@ -132,7 +132,7 @@ inline bool f8_launchable(const F8Plan& plan) { return size_t(plan.tiles) * plan
 hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
 bool f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size; false: no such kernel
 
-size_t route_workspace_bytes(int tokens, int experts, int top_k);
+size_t route_workspace_bytes(int tokens, int experts);
 struct RouteParams {
     const void* logits;
     size_t ld;

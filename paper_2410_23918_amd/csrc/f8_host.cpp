@@ -210,7 +210,7 @@ int bitstack_f8_grouped_linear(const bitstack_f8_rows_t* x, const bitstack_f8_we
 
 size_t bitstack_route_workspace_bytes(int tokens, int experts, int top_k) {
     if (tokens < 0 || experts < 1 || experts > kMaxExperts || top_k < 1 || top_k > kMaxTopK || top_k > experts) return 0;
-    return align256(route_workspace_bytes(tokens, experts, top_k));
+    return align256(route_workspace_bytes(tokens, experts));
 }
 
 int bitstack_route(const void* logits, int dtype, size_t ld, int tokens, int experts, int top_k, int renormalise,

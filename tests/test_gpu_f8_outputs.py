@@ -60,3 +60,14 @@ def test_refusals():
     with pytest.raises(B.BitStackError) as e:
         B.quantise_weight_f8(w, out=(odd, s))
     assert e.value.code == -4
+
+
+@pytest.mark.parametrize("tokens", [5, 64, 65, 3000])
+def test_routing_keeps_its_tables_alone(tokens):
+    experts, top_k = 512, 2
+    logits = torch.randn((tokens, experts), device=DEV)
+    B.route(logits, top_k)
+    r = B.route(logits, top_k)
+    held = r.offsets.untyped_storage().nbytes()
+    assert all(t.untyped_storage().data_ptr() == r.offsets.untyped_storage().data_ptr() for t in r)
+    assert held <= 4 * (4 * tokens * top_k + experts + 1) + 512
