@@ -81,8 +81,12 @@ struct WeightScale {
 __device__ __forceinline__ WeightScale weight_scale(int sw, bool sw_f32) {
     sw = __builtin_amdgcn_readfirstlane(sw);
     if (!sw_f32) return {sw, sw == 255 ? __uint_as_float(0x7fc00000u) : 1.0f};
-    const int byte = min(max(sw >> 23 & 255, 1), 254);
-    return {byte, __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(__builtin_amdgcn_ldexpf(__int_as_float(sw), kOne - byte))))};
+    int byte = sw >> 23 & 255, factor = (sw & 0x807fffff) | 0x3f800000;
+    if (__builtin_expect(unsigned(byte - 1) >= 254u, 0)) {   // zero, denormal or no number
+        byte = byte ? 254 : 1;
+        factor = __builtin_amdgcn_readfirstlane(__float_as_int(__builtin_amdgcn_ldexpf(__int_as_float(sw), kOne - byte)));
+    }
+    return {byte, __int_as_float(factor)};
 }
 
 // 32 e4m3 numbers as fp16, exactly
@@ -140,9 +144,8 @@ __device__ __forceinline__ void multiply(v4f* const (&acc)[FR], const Weights (&
 }
 // the same for FT fragments of the activations; after(i) follows those of fragment i
 template <int FR, int FT, int MODE, class After>
-__device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[FR], const v8i (&x)[FT], const int (&xs)[FT], int sw, bool sw_f32, After after) {
+__device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[FR], const v8i (&x)[FT], const int (&xs)[FT], const WeightScale& sw, After after) {
     typedef typename std::conditional<MODE == kModeExact, Halves, v8i>::type Weights;
-    const WeightScale scale = weight_scale(sw, sw_f32);
     Weights f[FR];
 #pragma unroll
     for (int j = 0; j < FR; ++j) {
@@ -154,7 +157,7 @@ __device__ __forceinline__ void multiply_all(v4f (&acc)[FR][FT], const v8i (&w)[
         v4f* to[FR];
 #pragma unroll
         for (int j = 0; j < FR; ++j) to[j] = &acc[j][i];
-        multiply<FR, MODE>(to, f, x[i], xs[i], scale);
+        multiply<FR, MODE>(to, f, x[i], xs[i], sw);
         after(i);
     }
 }
@@ -302,7 +305,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
                 if constexpr (kRaw) columns_to_f8<T>(s.raw, x[i], s.xs[i]);
                 else x[i] = join(s.x[i][0], s.x[i][1]);
             }
-            multiply_all<FR, FT, MODE>(acc, w, x, s.xs, s.sw, s_f32, [](int) __attribute__((always_inline)) {
+            multiply_all<FR, FT, MODE>(acc, w, x, s.xs, weight_scale(s.sw, s_f32), [](int) __attribute__((always_inline)) {
                 if constexpr (MODE == kModeExact && FT == 4) __builtin_amdgcn_sched_barrier(0);   // one fragment's conversions at a time: registers
             });
         };
@@ -503,7 +506,8 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
             asm volatile("v_mov_b32 %0, %1" : "=v"(scales) : "v"(v));   // waited for here, not at every step's use
         };
         v8i w[FR], x[FT];
-        int xs[FT], sw = 0;
+        int xs[FT];
+        WeightScale sw{};
         auto read = [&](int b) __attribute__((always_inline)) {
             if (ragged % 16 && b == p.kb - 1 && !late) {
                 // The last block ends inside a 16-byte piece, and the weight's rows may go on with anything: the wavefronts that read first clear the
@@ -521,12 +525,12 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
 #pragma unroll
             for (int i = 0; i < FT; ++i) x[i] = read_x(i);
             if ((b - first & 63) == 0) load_scales(b);
-            sw = __builtin_amdgcn_readlane(scales, b - first & 63);
+            sw = weight_scale(__builtin_amdgcn_readlane(scales, b - first & 63), s_f32);   // here, where the other side multiplies
             r_src = r_src == (S::kRing - 1) * S::kStep ? 0 : r_src + S::kStep;
         };
         auto products = [&](auto after) __attribute__((always_inline)) {
             __builtin_amdgcn_s_setprio(1);
-            multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, s_f32, after);
+            multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, after);
             __builtin_amdgcn_s_setprio(0);
         };
         // A loop for each side: with branches inside, the compiler moves the products past the barriers.  kAhead: loads that may still be on their way when a
@@ -677,7 +681,8 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
             asm volatile("v_mov_b32 %0, %1" : "=v"(scales) : "v"(v));   // waited for here, not at every step's use
         };
         v8i w[FR], x[FT];
-        int xs[FT], sw = 0;
+        int xs[FT];
+        WeightScale sw{};
         auto read = [&](int b, bool early_wave) __attribute__((always_inline)) {
             if (early_wave && ragged % 16 && b == p.kb - 1) {
                 // the last block ends inside a 16-byte piece: cleared by those that read first, as in k_f8_tile
@@ -694,7 +699,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
 #pragma unroll
             for (int i = 0; i < FT; ++i) x[i] = read_piece(x_src + i * 2048);
             if ((b - first & 63) == 0) load_scales(b);
-            sw = __builtin_amdgcn_readlane(scales, b - first & 63);
+            sw = weight_scale(__builtin_amdgcn_readlane(scales, b - first & 63), MODE == kModeF32);
             w_src = (b - first) & 1 ? w_src - kBigW : w_src + kBigW;
             x_src = x_src == x_wrap ? x_wrap - (early_wave ? 1 : 2) * kBigX : x_src + kBigX;
             s_src = s_src == s_wrap ? s_wrap - 2 * kBigS : s_src + kBigS;
@@ -702,7 +707,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
         auto products = [&](auto after) __attribute__((always_inline)) {
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
-            multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, MODE == kModeF32, [&](int i) __attribute__((always_inline)) {
+            multiply_all<FR, FT, MODE>(acc, w, x, xs, sw, [&](int i) __attribute__((always_inline)) {
                 __builtin_amdgcn_sched_barrier(0);
                 after(i);
                 __builtin_amdgcn_sched_barrier(0);
