@@ -204,8 +204,9 @@ __device__ __forceinline__ bool tile_of(const F8Params& p, int nrt, unsigned tog
 // A tile of 16 FR rows of the weight x 16 FT tokens.  The eight wavefronts of a workgroup take every eighth block of columns each, straight
 // from memory into registers (nothing of a tile is read by two of them), DEPTH blocks ahead; their sums meet in LDS.
 //   Bound by the stream of the weight, of which four wavefronts a SIMD keep 16 to 32 KB in flight on a compute unit: one token through two of eight 14336 x 4096
-// experts 24.9 us, 4.7 TB/s (16 rows as tokens stay in registers; tiles of 64 x 16, so that a block of the activations is read for 64 rows).  Small weights are bound by
-// the launch and three latencies (first load, LDS, store): 57 tokens through 1056 x 2001 in fp32, 16 x 16 tiles, 5.9 us.  With 32 and 64 tokens each
+// experts 26.6 us, 4.4 TB/s, 57 tokens through six of 64 experts of 1024 x 4096 48.6 us, 4.6 TB/s (16 rows as tokens stay in registers; tiles of 64 x 16, so that a
+// block of the activations is read for 64 rows).  Small weights are bound by
+// the launch and three latencies (first load, LDS, store): 57 tokens through 1056 x 2001 in fp32, 16 x 16 tiles, 6.2 us.  With 32 and 64 tokens each
 // wavefront's operands come from L2 again for every 64 rows.
 //   T: type of the activations.  With one fragment of tokens they may come as they are, in no groups, and are brought to 8 bits on the way (a block of a token
 // lies in four lanes), by every workgroup anew: one launch instead of two.  One token through 1024 x 4096: 7.0 us, 5.5 and 2.4 + a launch for the rows
@@ -344,8 +345,7 @@ const_cast<unsigned char*>(static_cast<const unsigned char*>(p.ws)) + s_row * s_
 // outputs of a token.
 //   Bound by LDS and latency: a phase reads 32 to 64 KB of fragments (128 bytes a clock) and multiplies for 128 to 256 clocks; 128 x 64 takes 0.54 us a step alone and
 // 0.9 for two workgroups of a compute unit, 128 x 128 0.78, 256 x 128 1.08; products alone would take 0.12, 0.25 and 0.50.  300 tokens
-// through 4096 x 14336 (256 x 128, five column slices, fp32 scales): 36.6 us, 0.96 PFLOP/s, and 6.8 to join them.  64 experts' 342 rows through 1024 x 4096
-// (128 x 64): 51.8 us, 4.3 TB/s, the stream of the weights.
+// through 4096 x 14336 (256 x 128, five column slices, fp32 scales): 36.9 us, 0.95 PFLOP/s, and 6.6 to join them.
 //   The activations' scales come with the step, four bytes a token (four steps' scales, of which one is used); the weight's, the same for 128
 // rows, are kept one to a lane for 64 steps.
 template <int FR, int FT, int WR, int WT, int MODE>
@@ -578,9 +578,10 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
 // requested in turn: the weight in even phases; the tokens in odd ones, a step earlier, those that the first wavefronts read into the
 // buffer that these have just read, the others' into a ring of three.
 //   Up to 128 tokens the last four wavefronts have none and only load.
-//   28672 x 8192, 2048 tokens: 390 us, 2.47 PFLOP/s, 8192 x 8192, 8192 tokens 415, 2.65; the matrix cores work in 56 % of the clocks (both operands requested in one
-// phase: 37 %, 460 us), of which there are then 2.0 in a nanosecond and not 2.35: power is the bound.  Without the loads it takes 279 us, without the
-// products 290.  fp32 scales of the weight cost 20 % more: four multiply-adds a matrix instruction.
+//   28672 x 8192, 2048 tokens: 390 us, 2.47 PFLOP/s, 8192 x 8192, 8192 tokens 408, 2.69 (replayed in a graph); the matrix cores work in 56 % of the clocks (both
+// operands requested in one phase: 37 %, 460 us), of which there are then 2.1 in a nanosecond and not 2.35: power is the bound.  Without the loads it takes 279 us, without the
+// products 290.  fp32 scales of the weight: 511 us.  They add four multiply-adds to a matrix instruction, whose
+// product goes into zeros.
 constexpr unsigned kBigW = 32768, kBigX = 16384, kBigS = 1024;                                          // bytes of a buffer
 constexpr unsigned kBigEarly = 2 * kBigW, kBigLate = kBigEarly + 2 * kBigX, kBigScales = kBigLate + 3 * kBigX;
 struct F8BigShape {
@@ -871,12 +872,13 @@ bool f8_force_kernel(int kernel) {
 }
 static bool makes(const F8KernelShape& k, bool exact) {
     if (exact) return k.kernel < kTile128Wide;   // the operands as fp16 leave no registers for the larger tiles' sums
-    // 1851 x 384 x 2048 in fp32: 14.6 us, 128 x 64 16.5; in 16 bits, where that has half the work, it is faster: 1920 x 272 x 1024 9.4, 7.9
+    // 1851 x 384 x 2048 in fp32: 14.3 us, 128 x 64 16.2; in 16 bits, where that has half the work, it is faster: 1920 x 272 x 1024 9.4, 7.9
     return k.kernel != kSlices64;
 }
 
 // Duration in microseconds.  The constants were fitted to timings of every kernel on 88 products (1 to 3660 rows, 256 to 28672 x 512 to 14336, up to 64
-// experts, all types): what they choose is 1.1 % slower than the fastest, in the mean, 15 % at most.
+// experts, all types): what they choose is 1.2 to 1.4 % slower than the fastest, in the mean of two runs, 16 % at most
+// (profiles/f8_kernel_choice.txt).
 static double f8_time_us(const F8KernelShape& k, int slices, int rows, int out, int kb, int experts, bool grouped, bool exact, bool ws_f32) {
     // tiles of y's rows that have any: a group fills its last one by half, in the mean
     const int groups = grouped ? std::min(rows, experts) : 1;

@@ -60,8 +60,9 @@ __device__ void make_work_list(const F8WorkList& l) {
 }
 
 // Sixteen lanes bring a block of 128 columns to 8 bits, eight columns each: a wavefront has four blocks of a row, whose scales are one word, WORDS
-// times over.  Bound by memory: x is read once and q written once, 16 and 8 bytes a lane and word: 2048 x 8192 in fp16 11.8 us, 4.3 TB/s; 2048 gated rows of
-// 2 x 14336 30.3 us, 4.8 TB/s.  The first workgroup makes the work list where there is one: a launch less.
+// times over.  Bound by memory: x is read once and q written once, 16 and 8 bytes a lane and word: 2048 x 8192 in fp16, from memory, 12.9 us, 3.9 TB/s.  Gated rows
+// have the gate's instructions beside that (f8_gate: 16 and two of a quarter of the rate): 2048 of 2 x 14336 41.7 us, 3.5 TB/s, 37.2 with six and two.  The first
+// workgroup makes the work list where there is one: a launch less.
 template <int T, bool GATED, int WORDS>
 __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::type* x, size_t ld, int rows, int in, unsigned char* q,
                                                      unsigned* s, int kp, F8WorkList list) {
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(256) void k_f8_quantise(const typename Elem<T>::typ
 }
 
 // A workgroup brings a block of 128 rows x 128 columns to 8 bits: sixteen lanes a row, sixteen rows a pass, the values in registers between
-// the maximum and the rounding, so that w is read once.  Bound by memory: 28672 x 8192 in fp16 130 us, 5.4 TB/s.
+// the maximum and the rounding, so that w is read once.  Bound by memory: 28672 x 8192 in fp16 132 us, 5.4 TB/s.
 template <int T>
 __global__ __launch_bounds__(256) void k_f8_quantise_weight(const typename Elem<T>::type* w, size_t ld, int out, int in,
                                                             unsigned char* q, size_t ld_q, int q_cols, unsigned char* s, int kb) {
