@@ -1,0 +1,47 @@
+// Shared by the layer of experts (expert_layer.hip) and its host code (f8_host.cpp).
+#pragma once
+#include "f8.h"
+
+namespace bitstack {
+
+constexpr int kLayerTokens = 64;   // at most: the tokens of an expert are a 64-bit mask
+
+struct LayerExpert {   // that has tokens
+    int expert, base;   // base: its first row; rows are sorted by expert, then token
+    unsigned long long tokens;
+};
+// Two choices of sizes alone
+struct LayerPlan {
+    int down_rows, tiles_down, splits;   // k_layer_down: rows of W2 in a tile, tiles, parts of the columns
+};
+LayerPlan layer_plan(int tokens, int hidden, int experts, int top_k);
+
+struct LayerParams {
+    const void* x;
+    const void* logits;
+    const unsigned char* w1;   // [experts][2 width] rows of e4m3
+    const unsigned char* s1;
+    const unsigned char* w2;   // [experts][hidden]
+    const unsigned char* s2;
+    const void* residual;      // or null
+    void* y;
+    size_t ld_x, ld_logits, ld_w1, ld_w2, ld_r, ld_y;   // elements, of the weights bytes
+    int dtype, logits_dtype, s1_f32, s2_f32;
+    int tokens, top_k, renormalise, experts, hidden, width;
+    int most;                  // experts that may have tokens
+    // workspace
+    int* count;                // experts that have tokens
+    LayerExpert* list;         // [most]
+    float* row_weight;         // [rows]
+    unsigned char* row_token;  // [rows]
+    unsigned* arrived;         // [tiles_down]
+    unsigned short* h;         // [h_parts][rows][ld_h] bf16, the largest part first
+    float* part;               // [tiles_down][splits][tokens][down_rows]
+    unsigned h_part, ld_h;     // elements
+    unsigned h_bytes;
+    int h_parts;
+    int down_rows, tiles_down, splits;
+};
+hipError_t launch_expert_layer(const LayerParams& p, hipStream_t st);
+
+}  // namespace bitstack

@@ -1,0 +1,774 @@
+// A layer of experts for a few tokens, from the router's logits to the weighted sums, in two kernels:
+//
+//     p[t], e[t] = the top_k choices of token t (as bitstack_route makes them)
+//     (g, u) = W1[e] x[t],   h[t, j] = g / (1 + exp(-g)) u,   y[t] = sum_j p[t, j] W2[e] h[t, j]  (+ residual[t])
+//
+// k_layer_up routes (every workgroup for itself: a launch and a pass over memory less) and writes h; k_layer_down multiplies with W2 and sums.
+//   The weights are e4m3 with a scale for each 128 x 128; the activations are not brought to 8 bits.  A few tokens are bound by the stream of the weights,
+// 3 width x hidden bytes for every expert that has a token, and the matrix cores have time for operands of 16 bits: an e4m3 number is an fp16 and a
+// bf16 number, x of 16 bits is taken as it is, x of 32 bits as the sum of three bf16 numbers (8 bits each, exact), h as the sum of two (16 bits, 2^-17 of a
+// value) for outputs of 16 bits and of three for fp32.  Sums are fp32: a block of 128 columns starts from zero and is added times its scale.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "expert_layer.h"
+#include "kparams.h"
+#include "route.h"
+
+namespace bitstack {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ v4f multiply8(const v8h& w, const v8h& x, const v4f& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x, c, 0, 0, 0); }
+__device__ __forceinline__ v4f multiply8(const v8bf& w, const v8bf& x, const v4f& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0); }
+
+// eight e4m3 numbers as fp16 or bf16, exactly
+__device__ __forceinline__ void widen(int lo, int hi, v8h& to) {
+    const v2h a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true),
+              c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+    to = v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ void widen(int lo, int hi, v8bf& to) {
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    to = v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The upper half of an fp32 number is a bf16 number; what is left over is exact (and 0 for an infinity, which the upper half holds)
+__device__ __forceinline__ float upper(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ float left_over(float v, float up) { return __builtin_isinf(v) ? 0.0f : v - up; }
+__device__ __forceinline__ unsigned short upper16(float v) { return (unsigned short)(__float_as_uint(v) >> 16); }
+
+// A lane's share of a block of columns: 16 from 16 kg on and 16 from 64 + 16 kg on, as four pieces of eight
+__device__ __forceinline__ int piece_column(int c, int kg) { return (c >> 1) * 64 + kg * 16 + (c & 1) * 8; }
+
+// Activations as they come: 32 columns of a token
+template <int T>
+struct RawX {
+    static constexpr int kParts = 1;
+    typedef typename std::conditional<T == BITSTACK_T_F16, v8h, v8bf>::type V;
+    V v[4];
+    __device__ __forceinline__ void load(const typename Elem<T>::type* row, int b, int kg, int in) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)   // always inside the row; what lies past it is put right by end()
+            v[c] = __builtin_bit_cast(V, *reinterpret_cast<const typename Piece<T>::loose*>(row + min(b * 128 + piece_column(c, kg), in - 8)));
+    }
+    __device__ __forceinline__ void end(const typename Elem<T>::type* row, int b, int kg, int in) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int col = b * 128 + piece_column(c, kg);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = col + i < in ? row[min(col + i, in - 1)] : typename Elem<T>::type(0);
+        }
+    }
+    __device__ __forceinline__ V part(int, int c) const { return v[c]; }
+};
+template <>
+struct RawX<BITSTACK_T_F32> {
+    static constexpr int kParts = 3;   // the smallest first
+    typedef v8bf V;
+    v4f v[4][2];
+    __device__ __forceinline__ void load(const float* row, int b, int kg, int in) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float* const from = row + min(b * 128 + piece_column(c, kg), in - 8);
+            v[c][0] = *reinterpret_cast<const Piece<BITSTACK_T_F32>::loose*>(from);
+            v[c][1] = *reinterpret_cast<const Piece<BITSTACK_T_F32>::loose*>(from + 4);
+        }
+    }
+    __device__ __forceinline__ void end(const float* row, int b, int kg, int in) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int col = b * 128 + piece_column(c, kg);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i >> 2][i & 3] = col + i < in ? row[min(col + i, in - 1)] : 0.0f;
+        }
+    }
+    __device__ __forceinline__ v8bf part(int q, int c) const {
+        v4u o;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            unsigned bits[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float a = v[c][d >> 1][(d & 1) * 2 + e];
+                if (q < 2) a = left_over(a, upper(a));
+                if (q < 1) a = left_over(a, upper(a));
+                bits[e] = __float_as_uint(a);
+            }
+            o[d] = bits[0] >> 16 | (bits[1] & 0xffff0000u);
+        }
+        return __builtin_bit_cast(v8bf, o);
+    }
+};
+
+// a scale of the weight as it lies in memory
+template <bool S_F32>
+__device__ __forceinline__ float scale_value(int raw) {
+    if constexpr (S_F32) return __int_as_float(raw);
+    else return raw == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(raw ? unsigned(raw) << 23 : 0x00400000u);
+}
+template <bool S_F32>
+__device__ __forceinline__ int load_scale(__amdgpu_buffer_rsrc_t s, unsigned at) {
+    if constexpr (S_F32) return __builtin_amdgcn_raw_buffer_load_b32(s, int(at * 4u), 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b8(s, int(at), 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, unsigned bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(bytes), 0x00020000);
+}
+
+// zeroes the bytes of a 16-byte piece from its column `n` on
+__device__ __forceinline__ v4i cut_columns(v4i v, int n) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const int k = n - 4 * d;
+        v[d] &= k >= 4 ? -1 : k <= 0 ? 0 : (1 << (8 * k)) - 1;
+    }
+    return v;
+}
+
+// FR fragments of 16 rows of the weight, a block of columns of them
+template <int FR>
+struct RawW {
+    v4i v[FR][2];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t w, const unsigned (&row)[FR], int b, int kg, int in) {
+#pragma unroll
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)   // always inside the row
+                v[j][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(w, int(row[j] + unsigned(min(b * 128 + h * 64 + kg * 16, (in - 1) & ~15))), 0, 0));
+    }
+    __device__ __forceinline__ void end(int b, int kg, int in) {   // the rows may go on with anything
+#pragma unroll
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[j][h] = cut_columns(v[j][h], in - (b * 128 + h * 64 + kg * 16));
+    }
+    template <class V>
+    __device__ __forceinline__ void widened(int j, V (&to)[4]) const {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) widen(v[j][c >> 1][(c & 1) * 2], v[j][c >> 1][(c & 1) * 2 + 1], to[c]);
+    }
+};
+
+// ---- routing, by every workgroup: who goes where, in LDS
+struct LayerLds {
+    unsigned long long* mask;   // [experts] the tokens of an expert
+    LayerExpert* list;          // [most] the experts that have any
+    int* base;                  // [experts] an expert's first row
+    int* count;                 // experts with tokens
+    float* weight;              // [rows] by row: rows sorted by expert, then token
+    unsigned char* token;       // [rows]
+    float* chosen_weight;       // [rows] by (token, j)
+    short* chosen;              // [rows]
+};
+__host__ __device__ inline unsigned layer_lds_bytes(int experts, int rows, int most) {
+    return unsigned(16 + 16 * most + 12 * experts + 11 * rows + 15) & ~15u;   // a multiple of 16
+}
+__device__ __forceinline__ LayerLds layer_lds(unsigned char* at, int experts, int rows, int most) {
+    LayerLds l;
+    l.count = reinterpret_cast<int*>(at);
+    at += 16;
+    l.list = reinterpret_cast<LayerExpert*>(at);
+    at += 16 * most;
+    l.mask = reinterpret_cast<unsigned long long*>(at);
+    at += 8 * experts;
+    l.base = reinterpret_cast<int*>(at);
+    at += 4 * experts;
+    l.weight = reinterpret_cast<float*>(at);
+    at += 4 * rows;
+    l.chosen_weight = reinterpret_cast<float*>(at);
+    at += 4 * rows;
+    l.chosen = reinterpret_cast<short*>(at);
+    at += 2 * rows;
+    l.token = at;
+    return l;
+}
+
+template <int NL>
+__device__ void layer_choose(const LayerParams& p, const LayerLds& l, int wave, int lane) {
+    for (int t = wave; t < p.tokens; t += 8) {
+        unsigned key[NL];
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int e = min(i * 64 + lane, p.experts - 1);
+            const size_t at = size_t(t) * p.ld_logits + e;
+            float v;
+            if (p.logits_dtype == BITSTACK_T_F32) v = static_cast<const float*>(p.logits)[at];
+            else if (p.logits_dtype == BITSTACK_T_F16) v = float(static_cast<const _Float16*>(p.logits)[at]);
+            else v = float(static_cast<const __bf16*>(p.logits)[at]);
+            key[i] = i * 64 + lane < p.experts ? route_key(v) : 0;
+        }
+        int expert;
+        float weight;
+        choose<NL>(p.top_k, p.renormalise != 0, key, lane, expert, weight);
+        if (lane < p.top_k) {
+            l.chosen[t * p.top_k + lane] = short(expert);
+            l.chosen_weight[t * p.top_k + lane] = weight;
+            if (expert >= 0) atomicOr(reinterpret_cast<unsigned*>(&l.mask[expert]) + (t >> 5), 1u << (t & 31));   // bits: the order does not matter
+        }
+    }
+}
+
+__device__ __forceinline__ void layer_route(const LayerParams& p, const LayerLds& l) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int e = tid; e < p.experts; e += 512) l.mask[e] = 0;
+    __syncthreads();
+    if (p.experts <= 64) layer_choose<1>(p, l, wave, lane);
+    else if (p.experts <= 128) layer_choose<2>(p, l, wave, lane);
+    else if (p.experts <= 256) layer_choose<4>(p, l, wave, lane);
+    else layer_choose<16>(p, l, wave, lane);
+    __syncthreads();
+    if (wave == 0) {   // experts with tokens and their first rows, 64 at a time; both sums in one word (fewer than 2^12 rows)
+        int before = 0;
+        for (int e0 = 0; e0 < p.experts; e0 += 64) {
+            const int e = e0 + lane;
+            const unsigned long long m = e < p.experts ? l.mask[e] : 0;
+            const int mine = (m ? 1 << 16 : 0) + __popcll(m);
+            int sum = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(sum, d);
+                if (lane >= d) sum += other;
+            }
+            const int at = before + sum - mine;
+            if (m) l.list[at >> 16] = LayerExpert{e, at & 0xffff, m};
+            if (e < p.experts) l.base[e] = at & 0xffff;
+            before += __shfl(sum, 63);
+        }
+        if (lane == 0) *l.count = before >> 16;
+    }
+    __syncthreads();
+    for (int i = tid; i < p.tokens * p.top_k; i += 512) {
+        const int e = l.chosen[i], t = i / p.top_k;
+        if (e < 0) continue;
+        const int row = l.base[e] + __popcll(l.mask[e] & ((1ull << t) - 1));
+        l.weight[row] = l.chosen_weight[i];
+        l.token[row] = (unsigned char)t;
+    }
+    __syncthreads();
+}
+
+// an expert's entry, in scalar registers
+struct Active {
+    int expert, base, rows;
+};
+__device__ __forceinline__ Active active_of(const LayerExpert* list, int a) {
+    const LayerExpert e = list[a];
+    return {__builtin_amdgcn_readfirstlane(e.expert), __builtin_amdgcn_readfirstlane(e.base), __builtin_amdgcn_readfirstlane(__popcll(e.tokens))};
+}
+
+// ---- h.  A unit: 8 FR of an expert's gates and the values next to them (FR = 1: both in one fragment of 16 rows) for all its tokens, NF fragments of 16 at
+// most; its eight wavefronts take every eighth block of columns each and meet in LDS.  A workgroup has a run of units and requests DEPTH blocks ahead, over
+// the ends of units.
+//   ODD: width is no multiple of 4, so that a lane's four rows may have two scales.
+template <int T, int FR, int NF, int DEPTH, bool S_F32, bool ODD>
+__global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
+    typedef typename Elem<T>::type E;
+    typedef typename RawX<T>::V V;
+    static_assert(!ODD || FR == 1, "one fragment");
+    constexpr int kBufs = FR * NF > 4 ? 1 : 2, kRed = 8 * FR * NF * 256;   // floats
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    float* const red = reinterpret_cast<float*>(smem);
+    const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rows = p.tokens * p.top_k;
+    const LayerLds l = layer_lds(smem + kBufs * kRed * 4, p.experts, rows, p.most);
+    layer_route(p, l);
+    const int actives = __builtin_amdgcn_readfirstlane(*l.count);
+    if (blockIdx.x == 0) {   // for the other kernel
+        if (tid == 0) *p.count = actives;
+        for (int a = tid; a < actives; a += 512) p.list[a] = l.list[a];
+        for (int i = tid; i < rows; i += 512) {
+            p.row_weight[i] = l.weight[i];
+            p.row_token[i] = l.token[i];
+        }
+        for (int i = tid; i < p.tiles_down; i += 512) p.arrived[i] = 0;
+    }
+    const int kb = (p.hidden + 127) / 128, steps = (kb + 7) / 8, tiles = (p.width + 8 * FR - 1) / (8 * FR);
+    const long long units = (long long)actives * tiles;
+    const int u0 = int(units * blockIdx.x / gridDim.x), u1 = int(units * (blockIdx.x + 1) / gridDim.x);
+    if (u0 >= u1) return;
+    const bool ragged = p.hidden % 128 != 0;
+    const unsigned w_extent = unsigned(size_t(2 * p.width - 1) * p.ld_w1 + (p.hidden + 15) / 16 * 16);
+    const int s_rows = (2 * p.width + 127) / 128;
+
+    // where the loads are
+    struct Place {
+        Active a;
+        int ai, tile, step;
+    };
+    Place at = {active_of(l.list, u0 / tiles), u0 / tiles, u0 % tiles, 0};
+    int left = u1 - u0;
+    unsigned w_row[FR], s_row[FR], s_row2 = 0;
+    const unsigned char* w_base;
+    const unsigned char* s_base;
+    const E* x_row[NF];
+    auto token_row = [&](const Active& a, int f) {   // of the f-th fragment's token ln
+        const int r = a.base + min(16 * f + ln, a.rows - 1);
+        return static_cast<const E*>(p.x) + size_t(l.token[r]) * p.ld_x;
+    };
+    auto enter = [&]() __attribute__((always_inline)) {
+        const int n0 = at.tile * 8 * FR;
+        w_base = p.w1 + size_t(at.a.expert) * (2 * p.width) * p.ld_w1;
+        s_base = p.s1 + size_t(at.a.expert) * s_rows * kb * (S_F32 ? 4 : 1);
+#pragma unroll
+        for (int j = 0; j < FR; ++j) {
+            // the weight's row that this lane loads, and the first of the four whose sums it gets
+            const int n = FR == 1 ? n0 + (ln & 7) : n0 + 16 * (j >> 1) + ln, m = FR == 1 ? n0 + 4 * (kg & 1) : n0 + 16 * (j >> 1) + 4 * kg;
+            const bool value = FR == 1 ? ln >= 8 : j & 1, value_sum = FR == 1 ? kg >= 2 : j & 1;
+            w_row[j] = unsigned((value ? p.width : 0) + min(n, p.width - 1)) * unsigned(p.ld_w1);
+            const int first = (value_sum ? p.width : 0) + min(m, p.width - 1);
+            s_row[j] = unsigned(first >> 7) * unsigned(kb);
+            if constexpr (ODD) s_row2 = unsigned(min(first + 3, 2 * p.width - 1) >> 7) * unsigned(kb);
+        }
+    };
+    struct Stage {
+        RawW<FR> w;
+        RawX<T> x;
+        int s[FR], s2;
+    };
+    Stage st[DEPTH];
+    auto load = [&](Stage& s) __attribute__((always_inline)) {
+        const int b = min(wave + 8 * at.step, kb - 1);
+        const bool live = left > 0 && wave + 8 * at.step < kb;   // past the last block nothing is read and zeros arrive
+        s.w.load(buffer_of(w_base, live ? w_extent : 0), w_row, b, kg, p.hidden);
+        s.x.load(x_row[0], b, kg, p.hidden);
+        const __amdgpu_buffer_rsrc_t sr = buffer_of(s_base, live ? unsigned(s_rows) * unsigned(kb) * (S_F32 ? 4u : 1u) : 0);
+#pragma unroll
+        for (int j = 0; j < FR; ++j) s.s[j] = load_scale<S_F32>(sr, s_row[j] + unsigned(b));
+        if constexpr (ODD) s.s2 = load_scale<S_F32>(sr, s_row2 + unsigned(b));
+        if (++at.step == steps) {
+            at.step = 0;
+            if (--left > 0) {
+                if (++at.tile == tiles) {
+                    at.tile = 0;
+                    at.a = active_of(l.list, ++at.ai);
+                    x_row[0] = token_row(at.a, 0);
+                }
+                enter();
+            }
+        }
+    };
+    x_row[0] = token_row(at.a, 0);
+    Place now = at;   // where the products are
+    const E* x_now = x_row[0];
+    int nf = (now.a.rows + 15) / 16;
+#pragma unroll
+    for (int f = 1; f < NF; ++f) x_row[f] = token_row(now.a, f);
+    enter();
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(st[d]);
+    v4f acc[FR][NF];
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) acc[j][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    clear();
+    auto products = [&](Stage& s) __attribute__((always_inline)) {
+        const int b = wave + 8 * now.step;
+        if (b >= kb) return;
+        const bool end = ragged && b == kb - 1;
+        if (end) {
+            s.w.end(b, kg, p.hidden);
+            s.x.end(x_now, b, kg, p.hidden);
+        }
+        V w[FR][4];
+        float scale[FR][4];
+#pragma unroll
+        for (int j = 0; j < FR; ++j) {
+            s.w.widened(j, w[j]);
+            const float first = scale_value<S_F32>(s.s[j]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) scale[j][v] = first;
+            if constexpr (ODD) {
+                const int row = (kg >= 2 ? p.width : 0) + min(now.tile * 8 + 4 * (kg & 1), p.width - 1);
+#pragma unroll
+                for (int v = 1; v < 4; ++v)
+                    if ((row + v) >> 7 != row >> 7) scale[j][v] = scale_value<S_F32>(s.s2);
+            }
+        }
+        auto multiply = [&](const RawX<T>& x, int f) __attribute__((always_inline)) {
+            v4f part[FR];
+#pragma unroll
+            for (int j = 0; j < FR; ++j) part[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int q = 0; q < RawX<T>::kParts; ++q)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const V xv = x.part(q, c);
+#pragma unroll
+                    for (int j = 0; j < FR; ++j) part[j] = multiply8(w[j][c], xv, part[j]);
+                }
+#pragma unroll
+            for (int j = 0; j < FR; ++j)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[j][v], scale[j][v], acc[j][f][v]);
+        };
+        multiply(s.x, 0);
+#pragma unroll
+        for (int f = 1; f < NF; ++f) {
+            if (f < nf) {
+                RawX<T> x;
+                x.load(x_row[f], b, kg, p.hidden);
+                if (end) x.end(x_row[f], b, kg, p.hidden);
+                multiply(x, f);
+            }
+        }
+    };
+    int buf = 0;
+    auto finish = [&]() __attribute__((always_inline)) {   // a unit's sums
+        float* const r = red + buf * kRed;
+#pragma unroll
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+                if (f < nf) *reinterpret_cast<v4f*>(r + ((wave * FR + j) * NF + f) * 256 + lane * 4) = acc[j][f];
+        lds_barrier();
+        constexpr int kEach = FR == 1 ? 128 : FR / 2 * 256;   // outputs of a fragment of tokens
+        const int padded = (p.width + 7) & ~7, n0 = now.tile * 8 * FR;
+        for (int o = tid; o < kEach * nf; o += 512) {
+            const int f = o / kEach, k = o % kEach, jj = FR == 1 ? 0 : k / 256, kk = FR == 1 ? k : k % 256;
+            const int rank = 16 * f + (kk >> 2 & 15), n = n0 + 16 * jj + 4 * (kk >> 6) + (kk & 3);
+            const float* const g = r + (2 * jj * NF + f) * 256 + kk;
+            const float* const u = FR == 1 ? g + 128 : g + NF * 256;
+            float gate = g[0], value = u[0];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) {
+                gate += g[w * FR * NF * 256];
+                value += u[w * FR * NF * 256];
+            }
+            if (rank >= now.a.rows || n >= padded) continue;
+            const float h = n < p.width ? f8_gate(gate, value) : 0.0f;
+            unsigned short* const to = p.h + size_t(now.a.base + rank) * p.ld_h + n;
+            to[0] = upper16(h);
+            const float rest = left_over(h, upper(h));
+            if (p.h_parts == 2) {
+                to[p.h_part] = __builtin_bit_cast(unsigned short, __bf16(rest));
+            } else {
+                to[p.h_part] = upper16(rest);
+                to[2 * p.h_part] = upper16(left_over(rest, upper(rest)));
+            }
+        }
+        if (kBufs == 2) buf ^= 1;
+        else lds_barrier();
+        clear();
+    };
+    const int total = (u1 - u0) * steps;
+    for (int i = 0; i < total; i += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            if (i + d >= total) break;
+            products(st[d]);
+            load(st[d]);
+            if (++now.step == steps) {
+                finish();
+                now.step = 0;
+                if (++now.tile == tiles && i + d + 1 < total) {
+                    now.tile = 0;
+                    now.a = active_of(l.list, ++now.ai);
+                    nf = (now.a.rows + 15) / 16;
+                    x_now = token_row(now.a, 0);
+#pragma unroll
+                    for (int f = 1; f < NF; ++f) x_row[f] = token_row(now.a, f);
+                }
+            }
+        }
+    }
+}
+
+// ---- y.  A workgroup has 16 FR rows of W2 and a part of the (expert, block of columns) pairs; its eight wavefronts take every eighth of these each.  At an
+// expert's end a wavefront adds its sums, times the tokens' weights, to its own tokens' sums in LDS; these meet there, and the parts in memory, where
+// the last workgroup to arrive adds them up: in order, so that the result does not depend on what arrives when.
+template <int FR, int NF, int PARTS, int DEPTH, bool S_F32>
+__global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rows = p.tokens * p.top_k;
+    constexpr int kN = 16 * FR, kLd = kN + 4;   // floats from token to token
+    float* const sums = reinterpret_cast<float*>(smem) + wave * p.tokens * kLd;
+    unsigned char* at = smem + 8 * p.tokens * kLd * 4;
+    LayerExpert* const list = reinterpret_cast<LayerExpert*>(at);
+    at += 16 * p.most;
+    float* const row_weight = reinterpret_cast<float*>(at);
+    at += 4 * rows;
+    int& last_here = *reinterpret_cast<int*>(at);
+    unsigned char* const row_token = at + 16;
+    const int actives = __builtin_amdgcn_readfirstlane(*p.count);
+    for (int a = tid; a < actives; a += 512) list[a] = p.list[a];
+    for (int i = tid; i < rows; i += 512) {
+        row_weight[i] = p.row_weight[i];
+        row_token[i] = p.row_token[i];
+    }
+    for (int i = lane; i < p.tokens * kLd; i += 64) sums[i] = 0.0f;
+    __syncthreads();
+    const int tile = blockIdx.x / p.splits, split = blockIdx.x % p.splits, n0 = tile * kN;
+    const int kb = (p.width + 127) / 128;
+    const int i0 = int((long long)actives * kb * split / p.splits), i1 = int((long long)actives * kb * (split + 1) / p.splits);
+    const int mine = i1 - i0 > wave ? (i1 - i0 - wave + 7) / 8 : 0;   // pairs of this wavefront
+    if (mine > 0) {
+        const bool ragged = p.width % 128 != 0;
+        const int padded = (p.width + 7) & ~7, s_rows = (p.hidden + 127) / 128;
+        const int w_rows = min(kN, p.hidden - n0);
+        const unsigned w_extent = unsigned((w_rows - 1) * p.ld_w2 + (p.width + 15) / 16 * 16);
+        unsigned w_row[FR];
+#pragma unroll
+        for (int j = 0; j < FR; ++j) w_row[j] = unsigned(min(16 * j + ln, w_rows - 1)) * unsigned(p.ld_w2);
+        const __amdgpu_buffer_rsrc_t hr = buffer_of(p.h, p.h_bytes);
+        struct Place {
+            Active a;
+            int ai, b;
+        };
+        auto place = [&](int i) { return Place{active_of(list, i / kb), i / kb, i % kb}; };
+        Place from = place(i0 + wave);
+        int left = mine;
+        auto h_row = [&](const Active& a, int f) { return unsigned(a.base + min(16 * f + ln, a.rows - 1)) * unsigned(p.ld_h); };   // in elements
+        const unsigned char* w_base;
+        const unsigned char* s_base;
+        unsigned h_from;
+        auto enter = [&]() __attribute__((always_inline)) {
+            w_base = p.w2 + (size_t(from.a.expert) * p.hidden + n0) * p.ld_w2;
+            s_base = p.s2 + (size_t(from.a.expert) * s_rows + n0 / 128) * kb * (S_F32 ? 4 : 1);
+            h_from = h_row(from.a, 0);
+        };
+        enter();
+        struct H {
+            v8bf v[PARTS][4];   // the smallest first
+        };
+        auto load_h = [&](H& h, unsigned row, int b, bool live) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int col = b * 128 + piece_column(c, kg);
+                const unsigned none = live && col < padded ? 0u : 0x80000000u;   // zeros arrive
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q)
+                    h.v[q][c] = __builtin_bit_cast(v8bf, __builtin_amdgcn_raw_buffer_load_b128(hr, int(((row + unsigned(col) + unsigned(PARTS - 1 - q) * p.h_part) * 2u) | none), 0, 0));
+            }
+        };
+        struct Stage {
+            RawW<FR> w;
+            H h;
+            int s;
+        };
+        Stage st[DEPTH];
+        auto load = [&](Stage& s) __attribute__((always_inline)) {
+            const bool live = left > 0;
+            s.w.load(buffer_of(w_base, live ? w_extent : 0), w_row, from.b, kg, p.width);
+            load_h(s.h, h_from, from.b, live);
+            s.s = load_scale<S_F32>(buffer_of(s_base, live ? unsigned(kb) * (S_F32 ? 4u : 1u) : 0), unsigned(from.b));
+            if (--left > 0) {
+                from.b += 8;
+                if (from.b >= kb) {
+                    do {
+                        from.b -= kb;
+                        ++from.ai;
+                    } while (from.b >= kb);
+                    from.a = active_of(list, from.ai);
+                    enter();
+                }
+            }
+        };
+        Place now = from;
+        int nf = (now.a.rows + 15) / 16;
+        v4f acc[FR][NF];
+        auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < FR; ++j)
+#pragma unroll
+                for (int f = 0; f < NF; ++f) acc[j][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        };
+        clear();
+        auto products = [&](Stage& s) __attribute__((always_inline)) {
+            if (ragged && now.b == kb - 1) s.w.end(now.b, kg, p.width);
+            v8bf w[FR][4];
+#pragma unroll
+            for (int j = 0; j < FR; ++j) s.w.widened(j, w[j]);
+            const float scale = scale_value<S_F32>(s.s);
+            auto multiply = [&](const H& h, int f) __attribute__((always_inline)) {
+                v4f part[FR];
+#pragma unroll
+                for (int j = 0; j < FR; ++j) part[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int j = 0; j < FR; ++j) part[j] = multiply8(w[j][c], h.v[q][c], part[j]);
+#pragma unroll
+                for (int j = 0; j < FR; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[j][v], scale, acc[j][f][v]);
+            };
+            multiply(s.h, 0);
+#pragma unroll
+            for (int f = 1; f < NF; ++f) {
+                if (f < nf) {
+                    H h;
+                    load_h(h, h_row(now.a, f), now.b, true);
+                    multiply(h, f);
+                }
+            }
+        };
+        auto finish = [&]() __attribute__((always_inline)) {   // an expert's sums
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                if (16 * f + ln < now.a.rows) {
+                    const int r = now.a.base + 16 * f + ln;
+                    const float weight = row_weight[r];
+                    float* const to = sums + row_token[r] * kLd + 4 * kg;
+#pragma unroll
+                    for (int j = 0; j < FR; ++j) {
+                        v4f v = *reinterpret_cast<v4f*>(to + 16 * j);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = fmaf(weight, acc[j][f][k], v[k]);
+                        *reinterpret_cast<v4f*>(to + 16 * j) = v;
+                    }
+                }
+            }
+            clear();
+        };
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) load(st[d]);
+        for (int i = 0; i < mine; i += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                if (i + d >= mine) break;
+                products(st[d]);
+                load(st[d]);
+                now.b += 8;
+                if (now.b >= kb) {
+                    finish();
+                    if (i + d + 1 < mine) {
+                        do {
+                            now.b -= kb;
+                            ++now.ai;
+                        } while (now.b >= kb);
+                        now.a = active_of(list, now.ai);
+                        nf = (now.a.rows + 15) / 16;
+                    }
+                } else if (i + d + 1 == mine) {
+                    finish();
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const float* const all = reinterpret_cast<const float*>(smem);
+    auto own = [&](int t, int n) {   // the eight wavefronts' sums
+        float v = all[t * kLd + n];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) v += all[(w * p.tokens + t) * kLd + n];
+        return v;
+    };
+    const int outputs = p.tokens * kN;
+    if (p.splits > 1) {
+        float* const part = p.part + (size_t(tile) * p.splits + split) * outputs;
+        for (int o = tid; o < outputs; o += 512) part[o] = own(o / kN, o % kN);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        __syncthreads();
+        if (tid == 0) last_here = __hip_atomic_fetch_add(&p.arrived[tile], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == unsigned(p.splits - 1);
+        __syncthreads();
+        if (!last_here) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    }
+    for (int o = tid; o < outputs; o += 512) {
+        const int t = o / kN, n = n0 + o % kN;
+        if (n >= p.hidden) continue;
+        float v;
+        if (p.splits > 1) {
+            const float* const part = p.part + size_t(tile) * p.splits * outputs + o;
+            v = part[0];
+            for (int s = 1; s < p.splits; ++s) v += part[size_t(s) * outputs];
+        } else {
+            v = own(t, o % kN);
+        }
+        const size_t r = size_t(t) * p.ld_r + n, to = size_t(t) * p.ld_y + n;
+        auto put = [&](auto* y, const auto* residual) {
+            if (residual) v += float(residual[r]);
+            y[to] = typename std::remove_reference<decltype(*y)>::type(v);
+        };
+        if (p.dtype == BITSTACK_T_F32) put(static_cast<float*>(p.y), static_cast<const float*>(p.residual));
+        else if (p.dtype == BITSTACK_T_F16) put(static_cast<_Float16*>(p.y), static_cast<const _Float16*>(p.residual));
+        else put(static_cast<__bf16*>(p.y), static_cast<const __bf16*>(p.residual));
+    }
+}
+
+constexpr int kLayerGroups = 256;   // workgroups of k_layer_up: one on each compute unit
+
+template <class K>
+static hipError_t go(K kernel, std::atomic<int>& allowed, unsigned grid, unsigned lds, const LayerParams& p, hipStream_t st) {
+    if (int(lds) > allowed && lds > 65536) {   // (doing it twice is harmless)
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 163840);
+        if (e != hipSuccess) return e;
+        allowed = 163840;
+    }
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(512), lds, st, p);
+    return hipGetLastError();
+}
+
+template <int T, int FR, int NF, int DEPTH, bool S_F32, bool ODD>
+static hipError_t up_as(const LayerParams& p, hipStream_t st) {
+    static std::atomic<int> allowed{0};
+    constexpr unsigned kRed = (FR * NF > 4 ? 1 : 2) * 8 * FR * NF * 1024;
+    return go(&k_layer_up<T, FR, NF, DEPTH, S_F32, ODD>, allowed, kLayerGroups, kRed + layer_lds_bytes(p.experts, p.tokens * p.top_k, p.most), p, st);
+}
+template <int T, bool S_F32>
+static hipError_t up(const LayerParams& p, hipStream_t st) {
+    constexpr int kMore = T == BITSTACK_T_F32 ? 1 : 2;
+    if (p.width % 4 != 0) return up_as<T, 1, 4, kMore, S_F32, true>(p, st);
+    if (p.tokens <= 16) return up_as<T, 2, 1, 2 * kMore, S_F32, false>(p, st);
+    if (p.tokens <= 32) return up_as<T, 2, 2, kMore, S_F32, false>(p, st);
+    return up_as<T, 2, 4, kMore, S_F32, false>(p, st);
+}
+static unsigned down_lds_bytes(int rows, int tokens, int top_k, int most) { return unsigned(8 * tokens * (rows + 4) * 4 + 16 * most + 5 * tokens * top_k + 16); }
+template <int FR, int NF, int PARTS, int DEPTH, bool S_F32>
+static hipError_t down_as(const LayerParams& p, hipStream_t st) {
+    static std::atomic<int> allowed{0};
+    return go(&k_layer_down<FR, NF, PARTS, DEPTH, S_F32>, allowed, unsigned(p.tiles_down * p.splits), down_lds_bytes(16 * FR, p.tokens, p.top_k, p.most), p, st);
+}
+template <int PARTS, bool S_F32>
+static hipError_t down(const LayerParams& p, hipStream_t st) {
+    if (p.down_rows == 16) return down_as<1, 1, PARTS, 3, S_F32>(p, st);
+    if (p.down_rows == 32) return down_as<2, 4, PARTS, 1, S_F32>(p, st);
+    if (p.tokens <= 16) return down_as<4, 1, PARTS, 2, S_F32>(p, st);
+    return down_as<4, 4, PARTS, 1, S_F32>(p, st);
+}
+
+LayerPlan layer_plan(int tokens, int hidden, int experts, int top_k) {
+    LayerPlan plan;
+    const int most = std::min(experts, tokens * top_k);
+    plan.down_rows = tokens * top_k <= 4 * most && tokens <= 16 ? 16 : 64;
+    if (down_lds_bytes(plan.down_rows, tokens, top_k, most) > 163840) plan.down_rows = 32;   // 64 tokens with many choices of many experts
+    plan.tiles_down = (hidden + plan.down_rows - 1) / plan.down_rows;
+    // parts of the columns: the fewest of up to 16 with which the last round of workgroups is filled best
+    plan.splits = 1;
+    double best = 0.0;
+    for (int s = 1; s <= 16; ++s) {
+        const int groups = plan.tiles_down * s;
+        const double filled = double(groups) / ((groups + 255) / 256 * 256);
+        if (filled > best + 0.05) {
+            best = filled;
+            plan.splits = s;
+        }
+    }
+    return plan;
+}
+
+hipError_t launch_expert_layer(const LayerParams& p, hipStream_t st) {
+    hipError_t e;
+    if (p.dtype == BITSTACK_T_F16) e = p.s1_f32 ? up<BITSTACK_T_F16, true>(p, st) : up<BITSTACK_T_F16, false>(p, st);
+    else if (p.dtype == BITSTACK_T_BF16) e = p.s1_f32 ? up<BITSTACK_T_BF16, true>(p, st) : up<BITSTACK_T_BF16, false>(p, st);
+    else e = p.s1_f32 ? up<BITSTACK_T_F32, true>(p, st) : up<BITSTACK_T_F32, false>(p, st);
+    if (e != hipSuccess) return e;
+    if (p.h_parts == 2) return p.s2_f32 ? down<2, true>(p, st) : down<2, false>(p, st);
+    return p.s2_f32 ? down<3, true>(p, st) : down<3, false>(p, st);
+}
+
+}  // namespace bitstack

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include "../../include/bitstack_f8.h"
+#include "expert_layer.h"
 #include "f8.h"
 #include "layout.h"
 
@@ -141,6 +142,35 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }
 
+// The workspace of a layer of experts
+struct LayerWorkspace {
+    size_t list, row_weight, row_token, arrived, h, part, total;
+};
+unsigned h_columns(int width) { return unsigned(width + 63) / 64 * 64; }
+LayerWorkspace layer_workspace(int tokens, int hidden, int width, int experts, int top_k, int h_parts) {
+    const LayerPlan plan = layer_plan(tokens, hidden, experts, top_k);
+    const size_t rows = size_t(tokens) * top_k;
+    LayerWorkspace w;
+    w.list = 256;
+    w.row_weight = w.list + align256((rows < size_t(experts) ? rows : size_t(experts)) * sizeof(LayerExpert));
+    w.row_token = w.row_weight + align256(rows * 4);
+    w.arrived = w.row_token + align256(rows);
+    w.h = w.arrived + align256(size_t(plan.tiles_down) * 4);
+    w.part = w.h + align256(size_t(h_parts) * rows * h_columns(width) * 2);
+    w.total = w.part + (plan.splits > 1 ? align256(size_t(plan.tiles_down) * plan.splits * tokens * plan.down_rows * 4) : 0);
+    return w;
+}
+bool layer_sizes_ok(int hidden, int width, int experts, int top_k) {
+    return hidden >= 8 && columns_ok(hidden) && columns_ok(width) && experts >= 1 && experts <= kMaxExperts && top_k >= 1 && top_k <= kMaxTopK && top_k <= experts;
+}
+int check_weight(const bitstack_f8_weight_t& w) {
+    if (w.scale_type != BITSTACK_S_E8M0 && w.scale_type != BITSTACK_S_F32) return BITSTACK_E_ARG;
+    if (!w.q || !w.scales) return BITSTACK_E_NULL;
+    if (misaligned(w.q, 16) || w.ld % 16 || (w.scale_type == BITSTACK_S_F32 && misaligned(w.scales, 4))) return BITSTACK_E_ALIGN;
+    if (w.ld < size_t(w.in) || w.ld > kMaxLd) return BITSTACK_E_SHAPE;
+    return BITSTACK_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -242,6 +272,86 @@ int bitstack_combine(const void* h, int dtype, size_t ld_h, int h_rows, int widt
     if ((h_rows > 1 && ld_h < size_t(width)) || (tokens > 1 && ld_y < size_t(width))) return BITSTACK_E_SHAPE;
     const CombineParams p{h, y, slots, weights, ld_h, ld_y, h_rows, width, tokens, top_k};
     const hipError_t e = launch_combine(p, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? BITSTACK_OK : hip_error(e);
+}
+
+size_t bitstack_f8_expert_layer_workspace_bytes(int tokens, int hidden, int width, int experts, int top_k) {
+    if (tokens < 0 || tokens > kLayerTokens || !layer_sizes_ok(hidden, width, experts, top_k)) return 0;
+    size_t most = 256;
+    for (int t = 1; t <= tokens; ++t) {
+        const size_t n = layer_workspace(t, hidden, width, experts, top_k, 3).total;
+        most = n > most ? n : most;
+    }
+    return most;
+}
+
+int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* logits, int logits_dtype, size_t ld_logits, int tokens, int top_k,
+                             int renormalise, const bitstack_f8_weight_t* w1, const bitstack_f8_weight_t* w2, const void* residual,
+                             size_t ld_residual, void* y, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+    if (!w1 || !w2) return BITSTACK_E_NULL;
+    if (tokens < 0 || tokens > kLayerTokens) return BITSTACK_E_RANGE;
+    const int hidden = w1->in, width = w2->in, experts = w1->experts;
+    if (!layer_sizes_ok(hidden, width, experts, top_k) || w2->experts != experts || w1->out != 2 * width || w2->out != hidden) return BITSTACK_E_SHAPE;
+    if (!real_type(dtype) || !real_type(logits_dtype) || (renormalise != 0 && renormalise != 1)) return BITSTACK_E_ARG;
+    int rc = check_weight(*w1);
+    if (rc == BITSTACK_OK) rc = check_weight(*w2);
+    if (rc) return rc;
+    if (tokens == 0) return BITSTACK_OK;
+    if (!x || !logits || !y || !workspace) return BITSTACK_E_NULL;
+    const size_t size = type_size(dtype);
+    if (misaligned(x, size) || misaligned(y, size) || misaligned(residual, size) || misaligned(logits, type_size(logits_dtype)) || misaligned(workspace, 256))
+        return BITSTACK_E_ALIGN;
+    if (tokens > 1 && (ld_x < size_t(hidden) || ld_y < size_t(hidden) || (residual && ld_residual < size_t(hidden)) || ld_logits < size_t(experts)))
+        return BITSTACK_E_SHAPE;
+    const int h_parts = dtype == BITSTACK_T_F32 ? 3 : 2;
+    const size_t rows = size_t(tokens) * top_k, ld_h = h_columns(width), h_bytes = h_parts * rows * ld_h * 2;
+    // reached by 32-bit offsets (h by 31-bit ones)
+    if (size_t(w1->out - 1) * w1->ld + (size_t(hidden) + 15) / 16 * 16 > 0xffffffffu || h_bytes > kMaxRowBytes) return BITSTACK_E_RANGE;
+    const LayerWorkspace at = layer_workspace(tokens, hidden, width, experts, top_k, h_parts);
+    if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
+    const LayerPlan plan = layer_plan(tokens, hidden, experts, top_k);
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    LayerParams p{};
+    p.x = x;
+    p.logits = logits;
+    p.w1 = static_cast<const unsigned char*>(w1->q);
+    p.s1 = static_cast<const unsigned char*>(w1->scales);
+    p.w2 = static_cast<const unsigned char*>(w2->q);
+    p.s2 = static_cast<const unsigned char*>(w2->scales);
+    p.residual = residual;
+    p.y = y;
+    p.ld_x = ld_x;
+    p.ld_logits = ld_logits;
+    p.ld_w1 = w1->ld;
+    p.ld_w2 = w2->ld;
+    p.ld_r = ld_residual;
+    p.ld_y = ld_y;
+    p.dtype = dtype;
+    p.logits_dtype = logits_dtype;
+    p.s1_f32 = w1->scale_type == BITSTACK_S_F32;
+    p.s2_f32 = w2->scale_type == BITSTACK_S_F32;
+    p.tokens = tokens;
+    p.top_k = top_k;
+    p.renormalise = renormalise;
+    p.experts = experts;
+    p.hidden = hidden;
+    p.width = width;
+    p.most = int(rows < size_t(experts) ? rows : size_t(experts));
+    p.count = reinterpret_cast<int*>(ws);
+    p.list = reinterpret_cast<LayerExpert*>(ws + at.list);
+    p.row_weight = reinterpret_cast<float*>(ws + at.row_weight);
+    p.row_token = ws + at.row_token;
+    p.arrived = reinterpret_cast<unsigned*>(ws + at.arrived);
+    p.h = reinterpret_cast<unsigned short*>(ws + at.h);
+    p.part = reinterpret_cast<float*>(ws + at.part);
+    p.ld_h = unsigned(ld_h);
+    p.h_part = unsigned(rows * ld_h);
+    p.h_bytes = unsigned(h_bytes);
+    p.h_parts = h_parts;
+    p.down_rows = plan.down_rows;
+    p.tiles_down = plan.tiles_down;
+    p.splits = plan.splits;
+    const hipError_t e = launch_expert_layer(p, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }
 

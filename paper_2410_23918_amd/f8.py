@@ -36,8 +36,8 @@ class _Args(threading.local):
     """argument blocks of one thread, filled anew for every call"""
 
     def __init__(self):
-        self.w, self.x = _Weight(), _Rows()
-        self.wp, self.xp = C.byref(self.w), C.byref(self.x)
+        self.w, self.w2, self.x = _Weight(), _Weight(), _Rows()
+        self.wp, self.w2p, self.xp = C.byref(self.w), C.byref(self.w2), C.byref(self.x)
 
 
 _args = _Args()
@@ -60,6 +60,8 @@ def _f8_lib():
             ("bitstack_route_workspace_bytes", sz, [i32] * 3),
             ("bitstack_route", i32, [vp, i32, sz, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
             ("bitstack_combine", i32, [vp, i32, sz, i32, i32, vp, vp, i32, i32, vp, sz, vp]),
+            ("bitstack_f8_expert_layer_workspace_bytes", sz, [i32] * 5),
+            ("bitstack_f8_expert_layer", i32, [vp, i32, sz, vp, i32, sz, i32, i32, i32, vp, vp, vp, sz, vp, sz, vp, sz, vp]),
         ):
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
@@ -169,7 +171,7 @@ def _matrix(t: torch.Tensor, what: str):
     return stride[0] if shape[0] > 1 else shape[1]
 
 
-def _fill_weight(q, scales, grouped):
+def _fill_weight(q, scales, grouped, w=None):
     if q.dtype is not torch.float8_e4m3fn:
         raise ValueError(f"q: float8_e4m3fn, not {q.dtype}")
     kind = _SCALES.get(scales.dtype)
@@ -185,7 +187,7 @@ def _fill_weight(q, scales, grouped):
     want = (-(-out // 128), -(-inn // 128))
     if scales.shape != ((e, *want) if grouped else want) or not scales.is_contiguous():
         raise ValueError(f"scales: one for each 128 x 128 block of q, {want}, contiguous")
-    w = _args.w
+    w = w or _args.w
     w.q, w.ld, w.scales, w.scale_type, w.out, w.inn, w.experts = q.data_ptr(), ld, scales.data_ptr(), kind, out, inn, e
     return out, inn, e
 
@@ -364,4 +366,48 @@ def combine(h, slots, weights, *, y=None, stream=None):
             _need(tuple(y.shape) == (n, h.shape[1]) and y.dtype is h.dtype, "y: [tokens, width] of h's type")
         _check(L.bitstack_combine(h.data_ptr(), t, ld, h.shape[0], h.shape[1], slots.data_ptr(), weights.data_ptr(), n, k, y.data_ptr(), _matrix(y, "y"),
                                   handle), "bitstack_combine")
+    return y
+
+
+def expert_layer_workspace_bytes(tokens: int, hidden: int, width: int, experts: int, top_k: int) -> int:
+    """bitstack_f8_expert_layer_workspace_bytes: of a `workspace` for expert_layer_f8 with up to so many tokens."""
+    n = int(_f8_lib().bitstack_f8_expert_layer_workspace_bytes(tokens, hidden, width, experts, top_k))
+    if n == 0:
+        raise BitStackError(-3 if not 0 <= tokens <= 64 else -2, "bitstack_f8_expert_layer_workspace_bytes")
+    return n
+
+
+def expert_layer_f8(x, logits, w1, w2, top_k: int, *, renormalise: bool = True, residual=None, y=None, workspace=None, stream=None):
+    """bitstack_f8_expert_layer: route, both products of every token's experts and the weighted sums (+ residual), for up to 64 tokens.  x [tokens, hidden];
+    logits [tokens, experts]; w1 and w2 pairs (q, scales), q [experts, 2 width, hidden] (gates above values) and [experts, hidden, width].
+    y has the type of x.  Activations are not brought to 8 bits.  workspace: a uint8 tensor of expert_layer_workspace_bytes, else one is allocated."""
+    L = _f8_lib()
+    args = _args
+    out1, hidden, experts = _fill_weight(*w1, True)
+    out2, width, experts2 = _fill_weight(*w2, True, args.w2)
+    t, ld_x, tl, ld_l = _type(x, "x"), _matrix(x, "x"), _type(logits, "logits"), _matrix(logits, "logits")
+    n = x.shape[0]
+    if x.shape[1] != hidden or out2 != hidden or out1 != 2 * width or experts != experts2 or logits.shape != (n, experts):
+        raise ValueError(f"w1 [experts, 2 width, hidden], w2 [experts, hidden, width], x [tokens, hidden] and logits [tokens, experts] are needed, not {list(w1[0].shape)}, "
+                         f"{list(w2[0].shape)}, {list(x.shape)} and {list(logits.shape)}")
+    device = x.device
+    _same_device(device, logits, *w1, *w2, residual, y, workspace)
+    ld_r = 0
+    if residual is not None:
+        _need(residual.shape == x.shape and residual.dtype is x.dtype, "residual: [tokens, hidden] of x's type")
+        ld_r = _matrix(residual, "residual")
+    with _on(device, stream, (x, logits, *w1, *w2, residual, y, workspace)) as handle:
+        if y is None:
+            y = x.new_empty((n, hidden))
+        else:
+            _need(y.shape == x.shape and y.dtype is x.dtype, "y: [tokens, hidden] of x's type")
+        if workspace is None:
+            nbytes = L.bitstack_f8_expert_layer_workspace_bytes(n, hidden, width, experts, top_k)
+            workspace = x.new_empty(nbytes, dtype=torch.uint8)
+        else:
+            _need(workspace.is_contiguous(), "workspace: contiguous")
+            nbytes = workspace.numel() * workspace.element_size()
+        _check(L.bitstack_f8_expert_layer(x.data_ptr(), t, ld_x, logits.data_ptr(), tl, ld_l, n, top_k, renormalise, args.wp, args.w2p,
+                                          None if residual is None else residual.data_ptr(), ld_r, y.data_ptr(), _matrix(y, "y"), workspace.data_ptr(), nbytes, handle),
+               "bitstack_f8_expert_layer")
     return y
