@@ -32,6 +32,8 @@ extern "C" {
 /* Element types of x, w, y, h and logits (the first two are BITSTACK_Y_F16 and BITSTACK_Y_F32).  BITSTACK_T_F8, for x
  * only: rows that bitstack_f8_quantise has written. */
 enum { BITSTACK_T_F16 = 0, BITSTACK_T_F32 = 1, BITSTACK_T_BF16 = 2, BITSTACK_T_F8 = 3 };
+/* what follows a product (bitstack_f8_epilogue_t) */
+enum { BITSTACK_ACT_NONE = 0, BITSTACK_ACT_RELU = 1, BITSTACK_ACT_GELU = 2, BITSTACK_ACT_GELU_TANH = 3, BITSTACK_ACT_SILU = 4, BITSTACK_ACT_SILU_GATED = 5 };
 /* types of a weight's scales */
 enum { BITSTACK_S_E8M0 = 0, BITSTACK_S_F32 = 1 };
 
@@ -96,6 +98,27 @@ size_t bitstack_f8_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitst
  * host structs, read during the call.  rows may be 0. */
 int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, void* y, int y_dtype, size_t ld_y,
                        void* workspace, size_t workspace_bytes, bitstack_stream_t stream);
+
+/* The same with what follows a product in a decoder, on the fp32 sums a[t][o], rounded once:
+ *     y = act(a + bias) + residual,                                      columns of y: out
+ *     SILU_GATED: y = g / (1 + exp(-g)) u + residual, (g, u) = a + bias in halves, columns of y: out / 2   (w's rows are gates above values, out is even)
+ * RELU: max(v, 0).  GELU: v (1 + erf(v / sqrt 2)) / 2.  GELU_TANH: v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2.  SILU: v / (1 + exp(-v)).
+ *   bias: [out] of bias_dtype (not F8), or NULL.  residual: [rows][columns of y] of y_dtype, ld_residual elements from row to row, or NULL; it may be y, but
+ *   must not overlap it otherwise.  All NULL and NONE: bitstack_f8_linear.
+ * Gates and values are written half as wide and never as they are.  Where out / 2 is a multiple of 128 (a block's scale is then that of gates or of values alone; the
+ * weight below 4 GiB) they meet inside the product; otherwise the sums of all rows go through the workspace, in more time. */
+typedef struct bitstack_f8_epilogue {
+    const void* bias;
+    int bias_dtype;
+    int activation;       /* BITSTACK_ACT_* */
+    const void* residual;
+    size_t ld_residual;
+} bitstack_f8_epilogue_t;
+/* As bitstack_f8_workspace_bytes (up to so many rows, any types), and as bitstack_f8_call_workspace_bytes (one call). */
+size_t bitstack_f8_epilogue_workspace_bytes(int rows, int in, int out, int activation);
+size_t bitstack_f8_epilogue_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, int y_dtype);
+int bitstack_f8_linear_epilogue(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, void* y, int y_dtype,
+                                size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream);
 
 /* Grouped by expert: rows [offsets[e], offsets[e+1]) of y are the products with expert e's weight,
  *     y[r] = w[e] x8[index[r]]        (x8[r] where index is NULL; y_rows <= x->rows then)

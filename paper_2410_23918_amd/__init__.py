@@ -32,7 +32,7 @@ from .binding import (  # noqa: F401
     unpack_image_host,
 )
 
-_F8 = ("F8Rows", "Routing", "combine", "expert_layer_f8", "expert_layer_workspace_bytes", "f8_workspace_bytes", "grouped_linear_f8", "linear_f8", "quantise_f8", "quantise_weight_f8", "route")
+_F8 = ("F8Rows", "Routing", "combine", "expert_layer_f8", "expert_layer_workspace_bytes", "f8_epilogue_workspace_bytes", "f8_workspace_bytes", "grouped_linear_f8", "linear_f8", "quantise_f8", "quantise_weight_f8", "route")
 
 
 def __getattr__(name):

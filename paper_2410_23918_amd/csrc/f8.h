@@ -34,7 +34,15 @@ struct F8Params {
     int slices, slice_blocks;  // of the columns; blocks in one
     int n_tiles;               // tiles of rows (an upper bound where they are grouped)
     int y_dtype, ws_f32;       // ws_f32: fp32 scales
+    // what follows the product, where anything does (epi)
+    int epi, act;              // F8Epi, BITSTACK_ACT_*
+    int cols;                  // of y: out, or half of it
+    int bias_dtype, parts_only;   // parts_only: no tile is finished by itself
+    const void* bias;          // [out] or null
+    const void* residual;      // [rows][cols] of y_dtype, or null
+    size_t ld_r;
 };
+enum F8Epi { kEpiNone, kEpiPlain, kEpiGated };
 
 // float of an element, and back
 template <int T>
@@ -127,9 +135,13 @@ struct F8Plan {
 };
 // room: bytes for the work list and the partial sums; with less than they need there are fewer slices
 F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32, size_t room = ~size_t(0));
+// The same for a product of one group all of whose sums are left as partial ones
+F8Plan f8_plan_parts(int rows, int out, int in, bool exact, bool ws_f32, size_t room = ~size_t(0));
 // a launch has fewer than 2^32 threads, 512 to a workgroup
 inline bool f8_launchable(const F8Plan& plan) { return size_t(plan.tiles) * plan.slices <= (size_t(1) << 23) - 8; }
 hipError_t launch_f8_product(const F8Params& p, const F8Plan& plan, hipStream_t st);
+hipError_t launch_f8_epilogue(const F8Params& p, const F8Plan& plan, hipStream_t st);   // its kernels with an epilogue
+hipError_t launch_f8_gated(const F8Params& p, const F8Plan& plan, hipStream_t st);
 bool f8_force_kernel(int kernel);   // measurement hook, 0: the choice by size; false: no such kernel
 
 size_t route_workspace_bytes(int tokens, int experts);

@@ -1,0 +1,118 @@
+// What follows a product: y = act(a + bias) + residual, or, where the rows of the weight are gates above values,
+//     y = g / (1 + exp(-g)) u + residual,   (g, u) = the halves of a + bias,
+// on the fp32 sums a, rounded once to the type of y.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "f8.h"
+
+namespace bitstack {
+
+// N consecutive elements as floats, at any element's address; those at or past `n` zero
+template <int T, int N>
+__device__ __forceinline__ void load_few(const void* from, size_t at, int n, float (&v)[N]) {
+    typedef typename Elem<T>::type E;
+    typedef E some __attribute__((ext_vector_type(N)));
+    typedef some loose __attribute__((aligned(sizeof(E))));
+    const E* const p = static_cast<const E*>(from) + at;
+    if (n >= N) {
+        const some u = *reinterpret_cast<const loose*>(p);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = float(u[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = e < n ? float(p[e]) : 0.0f;
+    }
+}
+template <int N>
+__device__ __forceinline__ void load_as(int dtype, const void* from, size_t at, int n, float (&v)[N]) {
+    if (dtype == BITSTACK_T_F32) load_few<BITSTACK_T_F32, N>(from, at, n, v);
+    else if (dtype == BITSTACK_T_F16) load_few<BITSTACK_T_F16, N>(from, at, n, v);
+    else load_few<BITSTACK_T_BF16, N>(from, at, n, v);
+}
+
+template <int N>
+__device__ __forceinline__ void add_bias(const F8Params& p, int n, int at, float (&a)[N]) {   // columns n .. of y, rows at .. of the weight
+    if (!p.bias) return;
+    float b[N];
+    load_as<N>(p.bias_dtype, p.bias, size_t(at), p.cols - n, b);
+#pragma unroll
+    for (int e = 0; e < N; ++e) a[e] += b[e];
+}
+template <int N>
+__device__ __forceinline__ void add_residual(const F8Params& p, int row, int n, float (&a)[N]) {
+    if (!p.residual) return;
+    float r[N];
+    load_as<N>(p.y_dtype, p.residual, size_t(row) * p.ld_r + n, p.cols - n, r);
+#pragma unroll
+    for (int e = 0; e < N; ++e) a[e] += r[e];
+}
+
+// v Phi(v), Phi(v) = erfc(-v / sqrt 2) / 2: no digits are lost where Phi is small
+__device__ __forceinline__ float gelu(float v) { return v < -40.0f ? 0.0f : 0.5f * v * erfcf(v * -0.70710678118654752440f); }
+// v / (1 + exp(-c v)), c = 2 sqrt(2 / pi) (1 + 0.044715 v^2), as the gate of c v times 1 / c; beyond 16 the quotient is 1 or 0 in fp32
+__device__ __forceinline__ float gelu_tanh(float v) {
+    const float c = fmaf(v * v, 0.07135481282553484f, 1.5957691216057308f);
+    const float y = f8_gate(c * v, __builtin_amdgcn_rcpf(c));
+    return v > 16.0f ? v : v < -16.0f ? 0.0f : y;
+}
+
+// a: sums of columns n .. n + N - 1 of a row of y (n < cols), in place
+template <int N>
+__device__ __forceinline__ void epilogue(const F8Params& p, int row, int n, float (&a)[N]) {
+    add_bias<N>(p, n, n, a);
+    auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) a[e] = f(a[e]);
+    };
+    if (p.act == BITSTACK_ACT_RELU) each([](float v) { return v < 0.0f ? 0.0f : v; });
+    else if (p.act == BITSTACK_ACT_GELU) each([](float v) { return gelu(v); });
+    else if (p.act == BITSTACK_ACT_GELU_TANH) each([](float v) { return gelu_tanh(v); });
+    else if (p.act == BITSTACK_ACT_SILU) each([](float v) { return f8_gate(v, 1.0f); });
+    add_residual<N>(p, row, n, a);
+}
+template <int N>
+__device__ __forceinline__ void epilogue_gated(const F8Params& p, int row, int n, float (&a)[N], float (&u)[N]) {
+    add_bias<N>(p, n, n, a);
+    add_bias<N>(p, n, p.cols + n, u);
+#pragma unroll
+    for (int e = 0; e < N; ++e) a[e] = f8_gate(a[e], u[e]);
+    add_residual<N>(p, row, n, a);
+}
+__device__ __forceinline__ v4f epilogue4(const F8Params& p, int row, int n, const v4f& v) {
+    float a[4] = {v[0], v[1], v[2], v[3]};
+    epilogue<4>(p, row, n, a);
+    return v4f{a[0], a[1], a[2], a[3]};
+}
+__device__ __forceinline__ v4f epilogue4_gated(const F8Params& p, int row, int n, const v4f& g, const v4f& v) {
+    float a[4] = {g[0], g[1], g[2], g[3]}, u[4] = {v[0], v[1], v[2], v[3]};
+    epilogue_gated<4>(p, row, n, a, u);
+    return v4f{a[0], a[1], a[2], a[3]};
+}
+
+template <int T>
+__device__ __forceinline__ void store8_as(const F8Params& p, int row, int n, const float (&a)[8]) {
+    typedef typename Elem<T>::type E;
+    constexpr int K = Elem<T>::kPer16;
+    E* const y = static_cast<E*>(p.y) + size_t(row) * p.ldy + n;
+    if (n + 8 <= p.cols) {
+#pragma unroll
+        for (int i = 0; i < 8 / K; ++i) {
+            typename Piece<T>::type u;
+#pragma unroll
+            for (int e = 0; e < K; ++e) u[e] = E(a[i * K + e]);
+            reinterpret_cast<typename Piece<T>::loose*>(y)[i] = u;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (n + e < p.cols) y[e] = E(a[e]);
+    }
+}
+__device__ __forceinline__ void store8(const F8Params& p, int row, int n, const float (&a)[8]) {
+    if (p.y_dtype == BITSTACK_T_F32) store8_as<BITSTACK_T_F32>(p, row, n, a);
+    else if (p.y_dtype == BITSTACK_T_F16) store8_as<BITSTACK_T_F16>(p, row, n, a);
+    else store8_as<BITSTACK_T_BF16>(p, row, n, a);
+}
+
+}  // namespace bitstack

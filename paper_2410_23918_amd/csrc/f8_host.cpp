@@ -72,17 +72,39 @@ bool raw_rows(const bitstack_f8_rows_t& x, const bitstack_f8_weight_t& w, int y_
     return !misaligned(x.x, 16) && (x.rows == 1 || (x.ld % 8 == 0 && x.ld <= kMaxRowBytes / 2)) && (size_t(x.rows - 1) * x.ld + w.in) * 2 <= kMaxRowBytes;
 }
 
-int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, void* y,
-            int y_dtype, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
-    const int rc = check_call(x, w, y_rows, y_dtype);
+// What follows the product.  Gates and values whose rows do not share their blocks of 128 are joined from partial sums of all rows.
+bool is_gated(const bitstack_f8_epilogue_t* e) { return e && e->activation == BITSTACK_ACT_SILU_GATED; }
+bool any_epilogue(const bitstack_f8_epilogue_t* e) { return e && (e->bias || e->residual || e->activation != BITSTACK_ACT_NONE); }
+bool parts_only(const bitstack_f8_epilogue_t* e, int out) { return is_gated(e) && out / 2 % kF8Block != 0; }
+F8Plan plan_of(const bitstack_f8_epilogue_t* e, int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32, size_t room = ~size_t(0)) {
+    return parts_only(e, out) ? f8_plan_parts(rows, out, in, exact, ws_f32, room) : f8_plan(rows, out, in, experts, grouped, exact, ws_f32, room);
+}
+int check_epilogue(const bitstack_f8_epilogue_t& e, const bitstack_f8_weight_t& w, int rows, int y_dtype) {
+    if (e.activation < BITSTACK_ACT_NONE || e.activation > BITSTACK_ACT_SILU_GATED) return BITSTACK_E_ARG;
+    if (e.bias && !real_type(e.bias_dtype)) return BITSTACK_E_ARG;
+    const bool gated = is_gated(&e);
+    if (gated && w.out % 2 != 0) return BITSTACK_E_SHAPE;
+    // gates and values are reached from one descriptor, by 31-bit offsets
+    if (gated && !parts_only(&e, w.out) && (size_t(w.out / 2) + 256) * w.ld > kMaxRowBytes) return BITSTACK_E_RANGE;
+    if (e.bias && misaligned(e.bias, type_size(e.bias_dtype))) return BITSTACK_E_ALIGN;
+    if (misaligned(e.residual, type_size(y_dtype))) return BITSTACK_E_ALIGN;
+    if (e.residual && rows > 1 && e.ld_residual < size_t(gated ? w.out / 2 : w.out)) return BITSTACK_E_SHAPE;
+    return BITSTACK_OK;
+}
+
+int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, const bitstack_f8_epilogue_t* epi,
+            void* y, int y_dtype, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+    int rc = check_call(x, w, y_rows, y_dtype);
+    if (rc == BITSTACK_OK && epi) rc = check_epilogue(*epi, *w, y_rows, y_dtype);
     if (rc) return rc;
+    const int cols = is_gated(epi) ? w->out / 2 : w->out;
     if (y_rows == 0) return BITSTACK_OK;
     if (!w->q || !w->scales || !y) return BITSTACK_E_NULL;
     if (misaligned(w->q, 16) || w->ld % 16 || (w->scale_type == BITSTACK_S_F32 && misaligned(w->scales, 4))) return BITSTACK_E_ALIGN;
-    if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(w->out))) return BITSTACK_E_SHAPE;
+    if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(cols))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
     auto plan_in = [&](size_t room) {
-        return f8_plan(y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32, room);
+        return plan_of(epi, y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32, room);
     };
     F8Plan plan = plan_in(~size_t(0));
     if (!f8_launchable(plan)) return BITSTACK_E_RANGE;   // with any kernel's tiles
@@ -138,6 +160,16 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     p.rows = y_rows;
     p.y_dtype = y_dtype;
     p.ws_f32 = w->scale_type == BITSTACK_S_F32;
+    if (any_epilogue(epi)) {
+        p.epi = is_gated(epi) ? kEpiGated : kEpiPlain;
+        p.act = epi->activation;
+        p.cols = cols;
+        p.bias = epi->bias;
+        p.bias_dtype = epi->bias_dtype;
+        p.residual = epi->residual;
+        p.ld_r = epi->ld_residual;
+        p.parts_only = parts_only(epi, w->out);
+    }
     const hipError_t e = launch_f8_product(p, plan, st);
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
 }
@@ -227,7 +259,7 @@ int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* 
                        void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
     if (!x || !w) return BITSTACK_E_NULL;
     if (w->experts != 1) return BITSTACK_E_SHAPE;
-    return product(x, w, nullptr, nullptr, x->rows, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
+    return product(x, w, nullptr, nullptr, x->rows, nullptr, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
 }
 
 int bitstack_f8_grouped_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets,
@@ -235,7 +267,32 @@ int bitstack_f8_grouped_linear(const bitstack_f8_rows_t* x, const bitstack_f8_we
                                size_t workspace_bytes, bitstack_stream_t stream) {
     if (!x || !w || !offsets || (!index && y_rows > 0 && y_rows > x->rows)) return !x || !w || !offsets ? BITSTACK_E_NULL : BITSTACK_E_RANGE;
     if (misaligned(offsets, 4) || misaligned(index, 4)) return BITSTACK_E_ALIGN;
-    return product(x, w, offsets, index, y_rows, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
+    return product(x, w, offsets, index, y_rows, nullptr, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
+}
+
+size_t bitstack_f8_epilogue_workspace_bytes(int rows, int in, int out, int activation) {
+    if (activation < BITSTACK_ACT_NONE || activation > BITSTACK_ACT_SILU_GATED || (activation == BITSTACK_ACT_SILU_GATED && out % 2 != 0)) return 0;
+    size_t most = bitstack_f8_workspace_bytes(rows, in, rows, out, 1);
+    const bitstack_f8_epilogue_t e = {nullptr, 0, activation, nullptr, 0};
+    if (!most || !rows || !parts_only(&e, out)) return most;
+    for (int k = 0; k < 4; ++k) {
+        const size_t n = workspace_of(rows, in, f8_plan_parts(rows, out, in, k & 1, k >> 1), false, false).total;
+        most = n > most ? n : most;
+    }
+    return most;
+}
+
+size_t bitstack_f8_epilogue_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, int y_dtype) {
+    if (!x || !w || w->experts != 1 || check_call(x, w, x->rows, y_dtype) || (epilogue && check_epilogue(*epilogue, *w, x->rows, y_dtype)) || x->rows == 0) return 0;
+    const F8Plan plan = plan_of(epilogue, x->rows, w->out, w->in, 1, false, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32);
+    return workspace_of(x->rows, w->in, plan, x->dtype == BITSTACK_T_F8 || raw_rows(*x, *w, x->rows, plan, false), false).total;
+}
+
+int bitstack_f8_linear_epilogue(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, void* y, int y_dtype,
+                                size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
+    if (!x || !w || !epilogue) return BITSTACK_E_NULL;
+    if (w->experts != 1) return BITSTACK_E_SHAPE;
+    return product(x, w, nullptr, nullptr, x->rows, epilogue, y, y_dtype, ld_y, workspace, workspace_bytes, stream);
 }
 
 size_t bitstack_route_workspace_bytes(int tokens, int experts, int top_k) {

@@ -20,6 +20,7 @@ T_F16, T_F32, T_BF16, T_F8 = 0, 1, 2, 3
 S_E8M0, S_F32 = 0, 1
 _TYPES = {torch.float16: T_F16, torch.float32: T_F32, torch.bfloat16: T_BF16}
 _SCALES = {torch.float8_e8m0fnu: S_E8M0, torch.float32: S_F32}
+_ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4, "silu_gated": 5}
 _lib = None
 
 
@@ -32,12 +33,16 @@ class _Rows(C.Structure):
     _fields_ = [("x", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_size_t), ("dtype", C.c_int), ("rows", C.c_int), ("gated", C.c_int)]
 
 
+class _Epilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("bias_dtype", C.c_int), ("activation", C.c_int), ("residual", C.c_void_p), ("ld_residual", C.c_size_t)]
+
+
 class _Args(threading.local):
     """argument blocks of one thread, filled anew for every call"""
 
     def __init__(self):
-        self.w, self.w2, self.x = _Weight(), _Weight(), _Rows()
-        self.wp, self.w2p, self.xp = C.byref(self.w), C.byref(self.w2), C.byref(self.x)
+        self.w, self.w2, self.x, self.e = _Weight(), _Weight(), _Rows(), _Epilogue()
+        self.wp, self.w2p, self.xp, self.ep = C.byref(self.w), C.byref(self.w2), C.byref(self.x), C.byref(self.e)
 
 
 _args = _Args()
@@ -57,6 +62,9 @@ def _f8_lib():
             ("bitstack_f8_call_workspace_bytes", sz, [vp, vp, i32, i32, i32]),
             ("bitstack_f8_linear", i32, [vp, vp, vp, i32, sz, vp, sz, vp]),
             ("bitstack_f8_grouped_linear", i32, [vp, vp, vp, vp, i32, vp, i32, sz, vp, sz, vp]),
+            ("bitstack_f8_epilogue_workspace_bytes", sz, [i32] * 4),
+            ("bitstack_f8_epilogue_call_workspace_bytes", sz, [vp, vp, vp, i32]),
+            ("bitstack_f8_linear_epilogue", i32, [vp, vp, vp, vp, i32, sz, vp, sz, vp]),
             ("bitstack_route_workspace_bytes", sz, [i32] * 3),
             ("bitstack_route", i32, [vp, i32, sz, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
             ("bitstack_combine", i32, [vp, i32, sz, i32, i32, vp, vp, i32, i32, vp, sz, vp]),
@@ -252,6 +260,46 @@ def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, strea
     return y
 
 
+def _linear_with(x, q, scales, gated, bias, activation, residual, y, out_dtype, workspace, stream):
+    L = _f8_lib()
+    act = _ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation: one of {list(_ACTIVATIONS)}, not {activation!r}")
+    out, inn, _ = _fill_weight(q, scales, False)
+    rows, dtype, held = _fill_rows(x, inn, gated)
+    device = q.device
+    _same_device(device, scales, bias, residual, y, workspace, *held)
+    if act == 5:
+        _need(out % 2 == 0, "silu_gated: gates above values are needed, an even number of rows")
+        out //= 2
+    dtype = out_dtype or (dtype if y is None else y.dtype)
+    args = _args
+    e = args.e
+    e.bias, e.bias_dtype, e.activation, e.residual, e.ld_residual = None, 0, act, None, 0
+    if bias is not None:
+        _need(bias.dim() == 1 and bias.shape[0] == q.shape[0] and bias.is_contiguous(), "bias: one for each row of q, contiguous")
+        e.bias, e.bias_dtype = bias.data_ptr(), _type(bias, "bias")
+    if residual is not None:
+        _need(residual.shape == (rows, out) and residual.dtype is dtype, f"residual: [{rows}, {out}] of y's type")
+        e.residual, e.ld_residual = residual.data_ptr(), _matrix(residual, "residual")
+    with _on(device, stream, (*held, q, scales, bias, residual, y, workspace)) as handle:
+        if y is None:
+            y = q.new_empty((rows, out), dtype=dtype)
+        else:
+            _need(y.shape == (rows, out) and y.dtype is dtype, f"y: [{rows}, {out}] is needed")
+        t = _type(y, "y")
+        if workspace is None:
+            nbytes = L.bitstack_f8_epilogue_call_workspace_bytes(args.xp, args.wp, args.ep, t)
+            if nbytes:
+                workspace = q.new_empty(nbytes, dtype=torch.uint8)
+        else:
+            _need(workspace.is_contiguous(), "workspace: contiguous")
+            nbytes = workspace.numel() * workspace.element_size()
+        _check(L.bitstack_f8_linear_epilogue(args.xp, args.wp, args.ep, y.data_ptr(), t, _matrix(y, "y"), None if workspace is None else workspace.data_ptr(), nbytes, handle),
+               "bitstack_f8_linear_epilogue")
+    return y
+
+
 def f8_workspace_bytes(x_rows: int, inn: int, y_rows: int, out: int, experts: int = 1) -> int:
     """bitstack_f8_workspace_bytes: of a `workspace` for products with up to so many rows.  One that a call allocates for itself may be larger and then
     makes it faster."""
@@ -261,10 +309,23 @@ def f8_workspace_bytes(x_rows: int, inn: int, y_rows: int, out: int, experts: in
     return n
 
 
-def linear_f8(x, q, scales, *, gated: bool = False, y=None, out_dtype=None, workspace=None, stream=None):
+def f8_epilogue_workspace_bytes(rows: int, inn: int, out: int, activation=None) -> int:
+    """bitstack_f8_epilogue_workspace_bytes: of a `workspace` for linear_f8 with bias, activation or residual and up to so many rows (out: rows of q)."""
+    n = int(_f8_lib().bitstack_f8_epilogue_workspace_bytes(rows, inn, out, _ACTIVATIONS.get(activation, -1)))
+    if n == 0:
+        raise BitStackError(-2, "bitstack_f8_epilogue_workspace_bytes")
+    return n
+
+
+def linear_f8(x, q, scales, *, gated: bool = False, bias=None, activation=None, residual=None, y=None, out_dtype=None, workspace=None, stream=None):
     """bitstack_f8_linear: y = x8 w^T.  x [tokens, in] (gated: [tokens, 2 in], gate and value side by side) or an F8Rows; q [out, in] and its
-    scales.  y has the type of x (fp16 for F8Rows) unless given.  workspace: a uint8 tensor of f8_workspace_bytes, else one is allocated."""
-    return _product(x, q, scales, None, None, gated, y, out_dtype, workspace, stream, False)
+    scales.  y has the type of x (fp16 for F8Rows) unless given.  workspace: a uint8 tensor of f8_workspace_bytes, else one is allocated.
+    bitstack_f8_linear_epilogue, with any of these: y = act(x8 w^T + bias) + residual.  bias [out]; activation "relu", "gelu" (by erf), "gelu_tanh", "silu", or
+    "silu_gated", where q's rows are gates above values and y is [tokens, out / 2]; residual of y's shape and type (y itself if it is given).  workspace:
+    f8_epilogue_workspace_bytes."""
+    if bias is None and activation is None and residual is None:
+        return _product(x, q, scales, None, None, gated, y, out_dtype, workspace, stream, False)
+    return _linear_with(x, q, scales, gated, bias, activation, residual, y, out_dtype, workspace, stream)
 
 
 def grouped_linear_f8(x, q, scales, offsets, rows=None, *, gated: bool = False, y=None, out_dtype=None, workspace=None, stream=None):
