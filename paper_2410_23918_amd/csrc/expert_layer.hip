@@ -669,23 +669,31 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
     };
     const int outputs = p.tokens * kN;
     if (p.splits > 1) {
+        // Write-through stores, complete before the counter says so, and loads that pass the caches which other XCDs' stores do not reach: no cache is written
+        // back or emptied as a whole.
         float* const part = p.part + (size_t(tile) * p.splits + split) * outputs;
-        for (int o = tid; o < outputs; o += 512) part[o] = own(o / kN, o % kN);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        for (int o = tid; o < outputs; o += 512) __hip_atomic_store(&part[o], own(o / kN, o % kN), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (tid == 0) last_here = __hip_atomic_fetch_add(&p.arrived[tile], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == unsigned(p.splits - 1);
+        if (tid == 0) last_here = __hip_atomic_fetch_add(&p.arrived[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == unsigned(p.splits - 1);
         __syncthreads();
         if (!last_here) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     }
     for (int o = tid; o < outputs; o += 512) {
         const int t = o / kN, n = n0 + o % kN;
         if (n >= p.hidden) continue;
         float v;
         if (p.splits > 1) {
-            const float* const part = p.part + size_t(tile) * p.splits * outputs + o;
-            v = part[0];
-            for (int s = 1; s < p.splits; ++s) v += part[size_t(s) * outputs];
+            constexpr int kAgentScope = 16;
+            const __amdgpu_buffer_rsrc_t part = buffer_of(p.part + size_t(tile) * p.splits * outputs, unsigned(p.splits) * unsigned(outputs) * 4u);
+            v = 0.0f;
+            for (int s = 0; s < p.splits; s += 4) {   // past the last one zeros arrive
+                float few[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) few[k] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(part, int(unsigned((s + k) * outputs + o) * 4u), 0, kAgentScope));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v += few[k];
+            }
         } else {
             v = own(t, o % kN);
         }
