@@ -7,14 +7,17 @@ namespace bitstack {
 constexpr int kLayerTokens = 64;   // at most: the tokens of an expert are a 64-bit mask
 
 struct LayerExpert {   // that has tokens
-    int expert, base;   // base: its first row; rows are sorted by expert, then token
+    int expert, base;   // base: their first row; rows are sorted by expert, then token
     unsigned long long tokens;
 };
-// Two choices of sizes alone
+// Choices by sizes alone
 struct LayerPlan {
+    int fragments;   // of 16 tokens in a unit of work; an expert with more tokens has several
+    int most;        // entries of the list of experts, at most
+    int up_rows;     // k_layer_up: gates of a unit
     int down_rows, tiles_down, splits;   // k_layer_down: rows of W2 in a tile, tiles, parts of the columns
 };
-LayerPlan layer_plan(int tokens, int hidden, int experts, int top_k);
+LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32);   // f32: x
 
 struct LayerParams {
     const void* x;
@@ -28,9 +31,9 @@ struct LayerParams {
     size_t ld_x, ld_logits, ld_w1, ld_w2, ld_r, ld_y;   // elements, of the weights bytes
     int dtype, logits_dtype, s1_f32, s2_f32;
     int tokens, top_k, renormalise, experts, hidden, width;
-    int most;                  // experts that may have tokens
+    int fragments, most, up_rows;   // LayerPlan
     // workspace
-    int* count;                // experts that have tokens
+    int* count;                // entries of list
     LayerExpert* list;         // [most]
     float* row_weight;         // [rows]
     unsigned char* row_token;  // [rows]

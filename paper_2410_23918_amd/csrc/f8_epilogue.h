@@ -31,6 +31,31 @@ __device__ __forceinline__ void load_as(int dtype, const void* from, size_t at, 
     else load_few<BITSTACK_T_BF16, N>(from, at, n, v);
 }
 
+// and back; those at or past `n` are not stored
+template <int T, int N>
+__device__ __forceinline__ void store_few(void* to, size_t at, int n, const float (&v)[N]) {
+    typedef typename Elem<T>::type E;
+    typedef E some __attribute__((ext_vector_type(N)));
+    typedef some loose __attribute__((aligned(sizeof(E))));
+    E* const p = static_cast<E*>(to) + at;
+    if (n >= N) {
+        some u;
+#pragma unroll
+        for (int e = 0; e < N; ++e) u[e] = E(v[e]);
+        *reinterpret_cast<loose*>(p) = u;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < n) p[e] = E(v[e]);
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_as(int dtype, void* to, size_t at, int n, const float (&v)[N]) {
+    if (dtype == BITSTACK_T_F32) store_few<BITSTACK_T_F32, N>(to, at, n, v);
+    else if (dtype == BITSTACK_T_F16) store_few<BITSTACK_T_F16, N>(to, at, n, v);
+    else store_few<BITSTACK_T_BF16, N>(to, at, n, v);
+}
+
 template <int N>
 __device__ __forceinline__ void add_bias(const F8Params& p, int n, int at, float (&a)[N]) {   // columns n .. of y, rows at .. of the weight
     if (!p.bias) return;
@@ -88,31 +113,6 @@ __device__ __forceinline__ v4f epilogue4_gated(const F8Params& p, int row, int n
     float a[4] = {g[0], g[1], g[2], g[3]}, u[4] = {v[0], v[1], v[2], v[3]};
     epilogue_gated<4>(p, row, n, a, u);
     return v4f{a[0], a[1], a[2], a[3]};
-}
-
-template <int T>
-__device__ __forceinline__ void store8_as(const F8Params& p, int row, int n, const float (&a)[8]) {
-    typedef typename Elem<T>::type E;
-    constexpr int K = Elem<T>::kPer16;
-    E* const y = static_cast<E*>(p.y) + size_t(row) * p.ldy + n;
-    if (n + 8 <= p.cols) {
-#pragma unroll
-        for (int i = 0; i < 8 / K; ++i) {
-            typename Piece<T>::type u;
-#pragma unroll
-            for (int e = 0; e < K; ++e) u[e] = E(a[i * K + e]);
-            reinterpret_cast<typename Piece<T>::loose*>(y)[i] = u;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (n + e < p.cols) y[e] = E(a[e]);
-    }
-}
-__device__ __forceinline__ void store8(const F8Params& p, int row, int n, const float (&a)[8]) {
-    if (p.y_dtype == BITSTACK_T_F32) store8_as<BITSTACK_T_F32>(p, row, n, a);
-    else if (p.y_dtype == BITSTACK_T_F16) store8_as<BITSTACK_T_F16>(p, row, n, a);
-    else store8_as<BITSTACK_T_BF16>(p, row, n, a);
 }
 
 }  // namespace bitstack

@@ -497,7 +497,7 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
             }
             if constexpr (kGated) epilogue_gated<8>(p, row0 + tok, n, a, u);
             else epilogue<8>(p, row0 + tok, n, a);
-            store8(p, row0 + tok, n, a);
+            store_as<8>(p.y_dtype, p.y, size_t(row0 + tok) * p.ldy + n, p.cols - n, a);
         }
     }
 }

@@ -33,13 +33,13 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __int_as_float(wave_all(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
 }
 
-// The j-th lane ends with the j-th choice (-1: none) and its weight.
+// The j-th lane ends with the j-th choice (-1: none) and its key; first: the largest key.
 template <int NL>
-__device__ __forceinline__ void choose(int top_k, bool renormalise, const unsigned (&key)[NL], int lane, int& expert, float& weight) {
+__device__ __forceinline__ void choose_experts(int top_k, const unsigned (&key)[NL], int lane, int& expert, unsigned& mine, unsigned& first) {
     unsigned left[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) left[i] = key[i];
-    unsigned mine = 0, first = 0;
+    mine = first = 0;
     expert = -1;
     for (int j = 0; j < top_k; ++j) {
         unsigned best = 0;
@@ -62,6 +62,10 @@ __device__ __forceinline__ void choose(int top_k, bool renormalise, const unsign
         for (int i = 0; i < NL; ++i)
             if (i * 64 + lane == e) left[i] = 0;
     }
+}
+// and the j-th choice's weight
+template <int NL>
+__device__ __forceinline__ float choice_weight(bool renormalise, const unsigned (&key)[NL], unsigned mine, unsigned first) {
     const float most = route_value(first);
     const float share = mine ? expf(route_value(mine) - most) : 0.0f;
     float total;
@@ -73,7 +77,23 @@ __device__ __forceinline__ void choose(int top_k, bool renormalise, const unsign
         for (int i = 0; i < NL; ++i) sum += key[i] ? expf(route_value(key[i]) - most) : 0.0f;
         total = wave_sum(sum);
     }
-    weight = mine ? share / total : 0.0f;
+    return mine ? share / total : 0.0f;
+}
+template <int NL>
+__device__ __forceinline__ void choose(int top_k, bool renormalise, const unsigned (&key)[NL], int lane, int& expert, float& weight) {
+    unsigned mine, first;
+    choose_experts<NL>(top_k, key, lane, expert, mine, first);
+    weight = choice_weight<NL>(renormalise, key, mine, first);
+}
+// Sums of the lanes up to each one
+__device__ __forceinline__ int wave_scan(int v) {
+    v += from_before<0x111, 0xf>(v);
+    v += from_before<0x112, 0xf>(v);
+    v += from_before<0x114, 0xf>(v);
+    v += from_before<0x118, 0xf>(v);
+    v += from_before<0x142, 0xa>(v);
+    v += from_before<0x143, 0xc>(v);
+    return v;
 }
 
 }  // namespace bitstack
