@@ -14,10 +14,9 @@ struct LayerExpert {   // that has tokens
 struct LayerPlan {
     int fragments;   // of 16 tokens in a unit of work; an expert with more tokens has several
     int most;        // entries of the list of experts, at most
-    int up_rows;     // k_layer_up: gates of a unit
     int down_rows, tiles_down, splits;   // k_layer_down: rows of W2 in a tile, tiles, parts of the columns
 };
-LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32);   // f32: x
+LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k);
 
 struct LayerParams {
     const void* x;
@@ -31,7 +30,7 @@ struct LayerParams {
     size_t ld_x, ld_logits, ld_w1, ld_w2, ld_r, ld_y;   // elements, of the weights bytes
     int dtype, logits_dtype, s1_f32, s2_f32;
     int tokens, top_k, renormalise, experts, hidden, width;
-    int fragments, most, up_rows;   // LayerPlan
+    int fragments, most;   // LayerPlan
     // workspace
     int* count;                // entries of list
     LayerExpert* list;         // [most]

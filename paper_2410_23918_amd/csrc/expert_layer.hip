@@ -79,6 +79,7 @@ struct RawX {
             v[c] = __builtin_bit_cast(V, *reinterpret_cast<const typename Piece<T>::loose*>(row + min(b * 128 + piece_column(c, kg), in - 8)));
     }
     __device__ __forceinline__ void end(int b, int kg, int in) {
+        asm volatile("" : "+v"(kg));   // nothing of this is made ahead and kept in registers
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const v4u u = __builtin_bit_cast(v4u, v[c]);
@@ -103,6 +104,7 @@ struct RawX<BITSTACK_T_F32> {
         }
     }
     __device__ __forceinline__ void end(int b, int kg, int in) {
+        asm volatile("" : "+v"(kg));
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             float d[8];
@@ -129,6 +131,25 @@ struct RawX<BITSTACK_T_F32> {
         }
         return __builtin_bit_cast(v8bf, o);
     }
+};
+
+// The same kept for many products: fp32 numbers in their parts, so that they are taken apart once
+template <int T>
+struct KeptX {
+    RawX<T> x;
+    __device__ __forceinline__ void keep(const RawX<T>& from) { x = from; }
+    __device__ __forceinline__ typename RawX<T>::V part(int q, int c) const { return x.part(q, c); }
+};
+template <>
+struct KeptX<BITSTACK_T_F32> {
+    v8bf p[3][4];
+    __device__ __forceinline__ void keep(const RawX<BITSTACK_T_F32>& from) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) p[q][c] = from.part(q, c);
+    }
+    __device__ __forceinline__ v8bf part(int q, int c) const { return p[q][c]; }
 };
 
 // a scale of the weight as it lies in memory
@@ -168,6 +189,7 @@ struct RawW {
                 v[j][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(w, int(row[j] + unsigned(min(b * 128 + h * 64 + kg * 16, (in - 1) & ~15))), 0, 0));
     }
     __device__ __forceinline__ void end(int b, int kg, int in) {   // the rows may go on with anything
+        asm volatile("" : "+v"(kg));   // nothing of this is made ahead and kept in registers
 #pragma unroll
         for (int j = 0; j < FR; ++j)
 #pragma unroll
@@ -363,16 +385,21 @@ __device__ __forceinline__ Active active_of(const LayerExpert* list, int a) {
 }
 
 // ---- h.  A unit: 8 FR of an expert's gates and the values next to them (FR = 1: both in one fragment of 16 rows) for all its tokens, NF fragments of 16 at
-// most; its eight wavefronts take every eighth block of columns each and meet in LDS.  A workgroup has a run of units and requests DEPTH blocks ahead, over
+// most; its eight wavefronts take every eighth block of columns each and meet in LDS.  A workgroup has a run of units and requests the weight DEPTH blocks ahead, over
 // the ends of units.
+//   KEEP > 0: a wavefront has at most KEEP blocks of columns and keeps its tokens' share of them in registers for as long as the units are the same expert's; a
+// compute unit's registers hold 16 tokens of 6144 or 32 of 4096.  Read anew for every unit they come from beyond L2, which the stream of the weight has gone through since
+// the last unit, and take as much of what the memory gives as a weight of as many rows: 64 tokens through two of eight experts, 28672 x 4096, 328 us, without
+// the tokens' loads 183.  KEEP = 0: they are (FR = 4, so that there are more rows to each load).
 //   ODD: width is no multiple of 4, so that a lane's four rows may have two scales.
-template <int T, int FR, int NF, int DEPTH, bool S_F32, bool ODD>
+template <int T, int FR, int NF, int DEPTH, int KEEP, bool S_F32, bool ODD>
 __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
     typedef typename Elem<T>::type E;
     typedef typename RawX<T>::V V;
     static_assert(!ODD || FR == 1, "one fragment");
+    static_assert(KEEP % DEPTH == 0, "a block's stage is the same in every unit");
     constexpr int kBufs = FR * NF > 4 ? 1 : 2, kRed = 8 * FR * NF * 256;   // floats
-    constexpr int kAhead = T == BITSTACK_T_F32 ? 1 : NF < 2 ? NF : 2;   // fragments of tokens that are requested ahead (registers); others when they are multiplied
+    constexpr int kAhead = KEEP ? 0 : T == BITSTACK_T_F32 ? 1 : NF < 2 ? NF : 2;   // fragments of tokens that are requested ahead (registers); others when they are multiplied
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float* const red = reinterpret_cast<float*>(smem);
     const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, kg = lane >> 4;
@@ -390,7 +417,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
         }
         for (int i = tid; i < p.tiles_down; i += 512) p.arrived[i] = 0;
     }
-    const int kb = (p.hidden + 127) / 128, steps = (kb + 7) / 8, tiles = (p.width + 8 * FR - 1) / (8 * FR);
+    const int kb = (p.hidden + 127) / 128, steps = KEEP ? KEEP : (kb + 7) / 8, tiles = (p.width + 8 * FR - 1) / (8 * FR);
     const long long units = (long long)actives * tiles;
     const int u0 = int(units * blockIdx.x / gridDim.x), u1 = int(units * (blockIdx.x + 1) / gridDim.x);
     if (u0 >= u1) return;
@@ -408,8 +435,8 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
     unsigned w_row[FR], s_row[FR], s_row2 = 0;
     const unsigned char* w_base;
     const unsigned char* s_base;
-    const E* x_row[kAhead];   // of the loads
-    const E* x_late[NF];      // of the products
+    const E* x_row[kAhead + 1];   // of the loads
+    const E* x_late[NF];          // of the products
     auto token_row = [&](const Active& a, int f) {   // of the f-th fragment's token ln
         const int r = a.base + min(16 * f + ln, a.rows - 1);
         return static_cast<const E*>(p.x) + size_t(l.token[r]) * p.ld_x;
@@ -431,7 +458,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
     };
     struct Stage {
         RawW<FR> w;
-        RawX<T> x[kAhead];
+        RawX<T> x[kAhead + 1];
         int s[FR], s2;
     };
     Stage st[DEPTH];
@@ -479,7 +506,22 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
             for (int f = 0; f < NF; ++f) acc[j][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     };
     clear();
-    auto products = [&](Stage& s) __attribute__((always_inline)) {
+    KeptX<T> kept[KEEP + 1][NF];
+    auto keep = [&]() __attribute__((always_inline)) {   // the tokens of the unit that comes
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+            const int b = min(wave + 8 * k, kb - 1);
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                RawX<T> x;
+                x.load(x_late[f], b, kg, p.hidden);
+                if (ragged && b == kb - 1) x.end(b, kg, p.hidden);
+                kept[k][f].keep(x);
+                if constexpr (T == BITSTACK_T_F32) __builtin_amdgcn_sched_barrier(0);   // registers
+            }
+        }
+    };
+    auto products = [&](Stage& s, const KeptX<T> (&own)[NF]) __attribute__((always_inline)) {
         const int b = wave + 8 * now.step;
         if (b >= kb) return;
         const bool end = ragged && b == kb - 1;
@@ -488,11 +530,9 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
 #pragma unroll
             for (int f = 0; f < kAhead; ++f) s.x[f].end(b, kg, p.hidden);
         }
-        V w[FR][4];
         float scale[FR][4];
 #pragma unroll
         for (int j = 0; j < FR; ++j) {
-            s.w.widened(j, w[j]);
             const float first = scale_value<S_F32>(s.s[j]);
 #pragma unroll
             for (int v = 0; v < 4; ++v) scale[j][v] = first;
@@ -503,33 +543,52 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
                     if ((row + v) >> 7 != row >> 7) scale[j][v] = scale_value<S_F32>(s.s2);
             }
         }
-        auto multiply = [&](const RawX<T>& x, int f) __attribute__((always_inline)) {
-            v4f part[FR];
-#pragma unroll
-            for (int j = 0; j < FR; ++j) part[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        // The products of one fragment of rows and one of tokens
+        auto multiply = [&](const V (&w)[4], int j, const auto& x, int f) __attribute__((always_inline)) {
+            v4f part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int q = 0; q < RawX<T>::kParts; ++q)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const V xv = x.part(q, c);
+                for (int c = 0; c < 4; ++c) part = multiply8(w[c], x.part(q, c), part);
 #pragma unroll
-                    for (int j = 0; j < FR; ++j) part[j] = multiply8(w[j][c], xv, part[j]);
-                }
+            for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[v], scale[j][v], acc[j][f][v]);
+        };
+        if constexpr (KEEP > 0) {   // a fragment of rows at a time: registers
 #pragma unroll
-            for (int j = 0; j < FR; ++j)
+            for (int j = 0; j < FR; ++j) {
+                V w[4];
+                s.w.widened(j, w);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[j][v], scale[j][v], acc[j][f][v]);
+                for (int f = 0; f < NF; ++f)
+                    if (f < nf) multiply(w, j, own[f], f);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
+        V w[FR][4];
+#pragma unroll
+        for (int j = 0; j < FR; ++j) s.w.widened(j, w[j]);
+        auto multiply_rows = [&](const RawX<T>& x, int f) __attribute__((always_inline)) {
+            if constexpr (RawX<T>::kParts > 1) {   // taken apart once for all rows
+                KeptX<T> parts;
+                parts.keep(x);
+#pragma unroll
+                for (int j = 0; j < FR; ++j) multiply(w[j], j, parts, f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < FR; ++j) multiply(w[j], j, x, f);
+            }
         };
 #pragma unroll
         for (int f = 0; f < kAhead; ++f)
-            if (f < nf) multiply(s.x[f], f);
+            if (f < nf) multiply_rows(s.x[f], f);
 #pragma unroll
         for (int f = kAhead; f < NF; ++f) {
             if (f < nf) {
                 RawX<T> x;
                 x.load(x_late[f], b, kg, p.hidden);
                 if (end) x.end(b, kg, p.hidden);
-                multiply(x, f);
+                multiply_rows(x, f);
             }
         }
     };
@@ -571,20 +630,40 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
         else lds_barrier();
         clear();
     };
-    const int total = (u1 - u0) * steps;
-    for (int i = 0; i < total; i += DEPTH) {
+    auto next_expert = [&]() __attribute__((always_inline)) {
+        now.tile = 0;
+        now.a = active_of(l.list, ++now.ai);
+        enter_late();
+    };
+    if constexpr (KEEP > 0) {
+        for (int u = u0; u < u1;) {
+            keep();
+            for (const int end = min(u1, u + tiles - now.tile); u < end; ++u, ++now.tile) {
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            if (i + d >= total) break;
-            products(st[d]);
-            load(st[d]);
-            if (++now.step == steps) {
+                for (int k = 0; k < KEEP; ++k) {
+                    __builtin_amdgcn_sched_barrier(0);   // a block's products at a time: registers
+                    products(st[k % DEPTH], kept[k]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    load(st[k % DEPTH]);
+                    ++now.step;
+                }
                 finish();
                 now.step = 0;
-                if (++now.tile == tiles && i + d + 1 < total) {
-                    now.tile = 0;
-                    now.a = active_of(l.list, ++now.ai);
-                    enter_late();
+            }
+            if (u < u1) next_expert();
+        }
+    } else {
+        const int total = (u1 - u0) * steps;
+        for (int i = 0; i < total; i += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                if (i + d >= total) break;
+                products(st[d], kept[0]);
+                load(st[d]);
+                if (++now.step == steps) {
+                    finish();
+                    now.step = 0;
+                    if (++now.tile == tiles && i + d + 1 < total) next_expert();
                 }
             }
         }
@@ -863,21 +942,26 @@ static hipError_t go(K kernel, std::atomic<int>& allowed, unsigned grid, unsigne
     return hipGetLastError();
 }
 
-template <int T, int FR, int NF, int DEPTH, bool S_F32, bool ODD>
+template <int T, int FR, int NF, int DEPTH, int KEEP, bool S_F32, bool ODD = false>
 static hipError_t up_as(const LayerParams& p, hipStream_t st) {
     static std::atomic<int> allowed{0};
     constexpr unsigned kRed = (FR * NF > 4 ? 1 : 2) * 8 * FR * NF * 1024;
-    return go(&k_layer_up<T, FR, NF, DEPTH, S_F32, ODD>, allowed, kLayerGroups, kRed + layer_lds_bytes(p.experts, p.tokens * p.top_k, p.most), p, st);
+    return go(&k_layer_up<T, FR, NF, DEPTH, KEEP, S_F32, ODD>, allowed, kLayerGroups, kRed + layer_lds_bytes(p.experts, p.tokens * p.top_k, p.most), p, st);
 }
 template <int T, bool S_F32>
 static hipError_t up(const LayerParams& p, hipStream_t st) {
-    constexpr int kMore = T == BITSTACK_T_F32 ? 1 : 2;
-    if (p.width % 4 != 0) return p.fragments == 1 ? up_as<T, 1, 1, 2 * kMore, S_F32, true>(p, st) : up_as<T, 1, 4, 1, S_F32, true>(p, st);
-    if (p.up_rows == 8 && p.fragments == 1) return up_as<T, 1, 1, 3 * kMore, S_F32, false>(p, st);
-    if (p.up_rows != 16) return hipErrorInvalidValue;
-    if (p.fragments == 1) return up_as<T, 2, 1, 2 * kMore, S_F32, false>(p, st);
-    if (p.fragments == 2) return up_as<T, 2, 2, 1 + kMore, S_F32, false>(p, st);
-    return up_as<T, 2, 4, kMore, S_F32, false>(p, st);
+    constexpr bool kF32 = T == BITSTACK_T_F32;
+    const int steps = ((p.hidden + 127) / 128 + 7) / 8;   // blocks of columns of a wavefront
+    if (p.width % 4 != 0) return p.fragments == 1 ? up_as<T, 1, 1, kF32 ? 2 : 4, 0, S_F32, true>(p, st) : up_as<T, 1, 4, 1, 0, S_F32, true>(p, st);
+    if constexpr (kF32) {
+        if (p.fragments == 1) return steps <= 2 ? up_as<T, 2, 1, 2, 2, S_F32>(p, st) : up_as<T, 4, 1, 2, 0, S_F32>(p, st);
+        if (p.fragments == 2) return up_as<T, 4, 2, 1, 0, S_F32>(p, st);
+        return up_as<T, 2, 4, 1, 0, S_F32>(p, st);
+    } else {
+        if (p.fragments == 1) return steps <= 4 ? up_as<T, 2, 1, 4, 4, S_F32>(p, st) : steps <= 6 ? up_as<T, 2, 1, 2, 6, S_F32>(p, st) : up_as<T, 4, 1, 3, 0, S_F32>(p, st);
+        if (p.fragments == 2) return steps <= 4 ? up_as<T, 2, 2, 2, 4, S_F32>(p, st) : up_as<T, 4, 2, 2, 0, S_F32>(p, st);
+        return up_as<T, 2, 4, 2, 0, S_F32>(p, st);
+    }
 }
 static unsigned down_lds_bytes(int rows, int tokens, int top_k, int most) { return unsigned(8 * tokens * (rows + 4) * 4 + 16 * most + 5 * tokens * top_k + 16); }
 template <int FR, int NF, int PARTS, bool PACK, int DEPTH, bool S_F32>
@@ -902,7 +986,7 @@ static hipError_t down(const LayerParams& p, hipStream_t st) {
 }
 
 static std::atomic<int> g_force[4];
-LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32) {
+LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k) {
     LayerPlan plan;
     const int rows = tokens * top_k;
     const double each = double(rows) / experts;   // tokens of an expert, in the mean
@@ -911,16 +995,7 @@ LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, 
     const int cap = 16 * plan.fragments;
     plan.most = std::min(experts, rows) + (tokens > cap ? rows / cap : 0);
     const double actives = experts * (1.0 - std::pow(1.0 - double(top_k) / experts, tokens));
-    plan.up_rows = 16;
-    if (plan.fragments == 1 && !f32) {   // rounds of units, the last one in part empty
-        auto filled = [&](int n) {
-            const double units = actives * ((width + n - 1) / n) / kLayerGroups;
-            return units / std::ceil(units);
-        };
-        if (filled(8) > 1.1 * filled(16)) plan.up_rows = 8;
-    }
     plan.down_rows = tokens <= 8 ? 32 : 64;
-    if (g_force[0]) plan.up_rows = g_force[0];
     if (g_force[1]) plan.down_rows = g_force[1];
     if (g_force[3]) plan.fragments = g_force[3], plan.most = std::min(experts, rows) + (tokens > 16 * g_force[3] ? rows / (16 * g_force[3]) : 0);
     if (down_lds_bytes(plan.down_rows, tokens, top_k, plan.most) > 163840) plan.down_rows = 32;   // 64 tokens with many choices of many experts

@@ -180,7 +180,7 @@ struct LayerWorkspace {
 };
 unsigned h_columns(int width) { return unsigned(width + 63) / 64 * 64; }
 LayerWorkspace layer_workspace(int tokens, int hidden, int width, int experts, int top_k, int h_parts) {
-    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
+    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k);
     const size_t rows = size_t(tokens) * top_k;
     LayerWorkspace w;
     w.list = 256;
@@ -366,7 +366,7 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     if (size_t(w1->out - 1) * w1->ld + (size_t(hidden) + 15) / 16 * 16 > 0xffffffffu || h_bytes > kMaxRowBytes) return BITSTACK_E_RANGE;
     const LayerWorkspace at = layer_workspace(tokens, hidden, width, experts, top_k, h_parts);
     if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
-    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
+    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k);
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     LayerParams p{};
     p.x = x;
@@ -395,7 +395,6 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     p.width = width;
     p.fragments = plan.fragments;
     p.most = plan.most;
-    p.up_rows = plan.up_rows;
     p.count = reinterpret_cast<int*>(ws);
     p.list = reinterpret_cast<LayerExpert*>(ws + at.list);
     p.row_weight = reinterpret_cast<float*>(ws + at.row_weight);
