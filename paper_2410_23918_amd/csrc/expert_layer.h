@@ -16,7 +16,7 @@ struct LayerPlan {
     int most;        // entries of the list of experts, at most
     int down_rows, tiles_down, splits;   // k_layer_down: rows of W2 in a tile, tiles, parts of the columns
 };
-LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k);
+LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32);   // f32: x
 
 struct LayerParams {
     const void* x;
@@ -37,9 +37,8 @@ struct LayerParams {
     float* row_weight;         // [rows]
     unsigned char* row_token;  // [rows]
     unsigned* arrived;         // [tiles_down]
-    unsigned short* h;         // [h_parts][rows][ld_h] bf16, the largest part first
+    unsigned short* h;         // [blocks of 128 columns][rows][h_parts][128] bf16, the largest part first: what a product of 16 rows reads lies together
     float* part;               // [tiles_down][splits][tokens][down_rows]
-    unsigned h_part, ld_h;     // elements
     unsigned h_bytes;
     int h_parts;
     int down_rows, tiles_down, splits;

@@ -156,7 +156,7 @@ struct KeptX<BITSTACK_T_F32> {
 template <bool S_F32>
 __device__ __forceinline__ float scale_value(int raw) {
     if constexpr (S_F32) return __int_as_float(raw);
-    else return raw == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(raw ? unsigned(raw) << 23 : 0x00400000u);
+    else return raw == 255 ? __uint_as_float(0x7fc00000u) : __builtin_amdgcn_ldexpf(1.0f, raw - 127);
 }
 template <bool S_F32>
 __device__ __forceinline__ int load_scale(__amdgpu_buffer_rsrc_t s, unsigned at) {
@@ -616,14 +616,14 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
             }
             if (rank >= now.a.rows || n >= padded) continue;
             const float h = n < p.width ? f8_gate(gate, value) : 0.0f;
-            unsigned short* const to = p.h + size_t(now.a.base + rank) * p.ld_h + n;
+            unsigned short* const to = p.h + (size_t(n >> 7) * rows + now.a.base + rank) * p.h_parts * 128 + (n & 127);
             to[0] = upper16(h);
             const float rest = left_over(h, upper(h));
             if (p.h_parts == 2) {
-                to[p.h_part] = __builtin_bit_cast(unsigned short, __bf16(rest));
+                to[128] = __builtin_bit_cast(unsigned short, __bf16(rest));
             } else {
-                to[p.h_part] = upper16(rest);
-                to[2 * p.h_part] = upper16(left_over(rest, upper(rest)));
+                to[128] = upper16(rest);
+                to[256] = upper16(left_over(rest, upper(rest)));
             }
         }
         if (kBufs == 2) buf ^= 1;
@@ -657,14 +657,15 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
         for (int i = 0; i < total; i += DEPTH) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
-                if (i + d >= total) break;
-                products(st[d], kept[0]);
-                load(st[d]);
-                if (++now.step == steps) {
-                    finish();
-                    now.step = 0;
-                    if (++now.tile == tiles && i + d + 1 < total) next_expert();
+                if (i + d < total) {   // (the loads are in no branch: the compiler would wait for all of them where its ways meet)
+                    products(st[d], kept[0]);
+                    if (++now.step == steps) {
+                        finish();
+                        now.step = 0;
+                        if (++now.tile == tiles && i + d + 1 < total) next_expert();
+                    }
                 }
+                load(st[d]);
             }
         }
     }
@@ -678,6 +679,9 @@ template <int FR, int NF, int PARTS, bool PACK, int DEPTH, bool S_F32>
 __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
     static_assert(!PACK || NF == 1, "one fragment");
     constexpr int kLoads = PACK ? 1 : PARTS, kPack = PACK ? 16 / PARTS : 16;   // tokens of a fragment
+    // One fragment of h is requested with the weight.  Of several the first kNext are requested after the products before (they come from L2), the others when they are
+    // multiplied: registers
+    constexpr int kNext = NF == 1 ? 0 : PARTS > 2 ? 1 : 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -721,8 +725,8 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
         int left = mine;
         const int pack_part = min(ln / kPack, PARTS - 1);   // smallest first
         auto h_row = [&](const Active& a, int f) {   // in elements
-            const unsigned r = unsigned(a.base + min(16 * f + ln % kPack, a.rows - 1)) * p.ld_h;
-            return PACK ? r + unsigned(PARTS - 1 - pack_part) * p.h_part : r;
+            const unsigned r = unsigned(a.base + min(16 * f + ln % kPack, a.rows - 1)) * (PARTS * 128);
+            return PACK ? r + unsigned(PARTS - 1 - pack_part) * 128 : r;
         };
         const unsigned char* w_base;
         const unsigned char* s_base;
@@ -737,25 +741,25 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
             v8bf v[kLoads][4];   // the smallest first
         };
         auto load_h = [&](H& h, unsigned row, int b, bool live) __attribute__((always_inline)) {
+            const unsigned from = row + unsigned(b) * unsigned(rows) * (PARTS * 128);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const int col = b * 128 + piece_column(c, kg);
-                const unsigned none = live && col < padded ? 0u : 0x80000000u;   // zeros arrive
+                const unsigned none = live && b * 128 + piece_column(c, kg) < padded ? 0u : 0x80000000u;   // zeros arrive
 #pragma unroll
                 for (int q = 0; q < kLoads; ++q)
-                    h.v[q][c] = __builtin_bit_cast(v8bf, __builtin_amdgcn_raw_buffer_load_b128(hr, int(((row + unsigned(col) + unsigned(kLoads - 1 - q) * p.h_part) * 2u) | none), 0, 0));
+                    h.v[q][c] = __builtin_bit_cast(v8bf, __builtin_amdgcn_raw_buffer_load_b128(hr, int(((from + unsigned(piece_column(c, kg) + (kLoads - 1 - q) * 128)) * 2u) | none), 0, 0));
             }
         };
         struct Stage {
             RawW<FR> w;
-            H h;
+            H h;   // NF = 1
             int s;
         };
         Stage st[DEPTH];
         auto load = [&](Stage& s) __attribute__((always_inline)) {
             const bool live = left > 0;
             s.w.load(buffer_of(w_base, live ? w_extent : 0), w_row, from.b, kg, p.width);
-            load_h(s.h, h_from, from.b, live);
+            if constexpr (NF == 1) load_h(s.h, h_from, from.b, live);
             s.s = load_scale<S_F32>(buffer_of(s_base, live ? unsigned(kb) * (S_F32 ? 4u : 1u) : 0), unsigned(from.b));
             if (--left > 0) {
                 from.b += 8;
@@ -779,49 +783,85 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
                 for (int f = 0; f < NF; ++f) acc[j][f] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         };
         clear();
+        H next[kNext + 1];
+        auto load_next = [&](bool live) __attribute__((always_inline)) {
+#pragma unroll
+            for (int f = 0; f < kNext; ++f) load_h(next[f], h_row(now.a, f), now.b, live);
+        };
         auto products = [&](Stage& s) __attribute__((always_inline)) {
             if (ragged && now.b == kb - 1) s.w.end(now.b, kg, p.width);
-            // Of several fragments of tokens each turns the weight into bf16 anew, a fragment of rows at a time: registers
-            v8bf w[NF == 1 ? FR : 1][4];
-            if constexpr (NF == 1) {
-#pragma unroll
-                for (int j = 0; j < FR; ++j) s.w.widened(j, w[j]);
-            }
             const float scale = scale_value<S_F32>(s.s);
-            auto multiply = [&](const H& h, int f) __attribute__((always_inline)) {
+            auto add = [&](const v4f& part, int j, int f) __attribute__((always_inline)) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[v], scale, acc[j][f][v]);
+            };
+            constexpr v4f kNone = {0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (NF == 1) {
+                v8bf w[FR][4];
                 v4f part[FR];
 #pragma unroll
-                for (int j = 0; j < FR; ++j) part[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-                if constexpr (NF == 1) {
+                for (int j = 0; j < FR; ++j) {
+                    s.w.widened(j, w[j]);
+                    part[j] = kNone;
+                }
 #pragma unroll
-                    for (int q = 0; q < kLoads; ++q)
+                for (int q = 0; q < kLoads; ++q)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c)
 #pragma unroll
-                            for (int j = 0; j < FR; ++j) part[j] = multiply8(w[j][c], h.v[q][c], part[j]);
-                } else {
+                        for (int j = 0; j < FR; ++j) part[j] = multiply8(w[j][c], s.h.v[q][c], part[j]);
 #pragma unroll
-                    for (int j = 0; j < FR; ++j) {
-                        s.w.widened(j, w[0]);
+                for (int j = 0; j < FR; ++j) add(part[j], j, 0);
+            } else if constexpr (kNext == NF) {
+                static_assert(NF == 2, "two fragments");
+                const bool two = nf == 2;
+#pragma unroll
+                for (int j = 0; j < FR; ++j) {   // a fragment of rows at a time: registers
+                    v8bf w[4];
+                    s.w.widened(j, w);
+                    v4f part[2] = {kNone, kNone};
+                    if (two) {
 #pragma unroll
                         for (int q = 0; q < kLoads; ++q)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) part[j] = multiply8(w[0][c], h.v[q][c], part[j]);
-                        __builtin_amdgcn_sched_barrier(0);
+                            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                                for (int f = 0; f < 2; ++f) part[f] = multiply8(w[c], next[f].v[q][c], part[f]);
+                        add(part[1], j, 1);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < kLoads; ++q)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) part[0] = multiply8(w[c], next[0].v[q][c], part[0]);
                     }
+                    add(part[0], j, 0);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+            } else {
 #pragma unroll
-                for (int j = 0; j < FR; ++j)
+                for (int f = 0; f < NF; ++f) {
+                    if (f >= nf) break;
+                    auto multiply = [&](const H& h) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[j][v], scale, acc[j][f][v]);
-            };
-            multiply(s.h, 0);
+                        for (int j = 0; j < FR; ++j) {
+                            v8bf w[4];
+                            s.w.widened(j, w);
+                            v4f part = kNone;
 #pragma unroll
-            for (int f = 1; f < NF; ++f) {
-                if (f < nf) {
-                    H h;
-                    load_h(h, h_row(now.a, f), now.b, true);
-                    multiply(h, f);
+                            for (int q = 0; q < kLoads; ++q)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) part = multiply8(w[c], h.v[q][c], part);
+                            add(part, j, f);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    };
+                    if (f < kNext) {
+                        multiply(next[f]);
+                    } else {
+                        H h;
+                        load_h(h, h_row(now.a, f), now.b, true);
+                        multiply(h);
+                    }
                 }
             }
         };
@@ -855,17 +895,19 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
             clear();
         };
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) load(st[d]);
+        for (int d = 0; d < DEPTH; ++d) {
+            load(st[d]);
+            if (d == 0) load_next(true);
+        }
         for (int i = 0; i < mine; i += DEPTH) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
-                if (i + d >= mine) break;
-                products(st[d]);
-                load(st[d]);
-                now.b += 8;
-                if (now.b >= kb) {
-                    finish();
-                    if (i + d + 1 < mine) {
+                if (i + d < mine) {   // (the loads are in no branch: the compiler would wait for all of them where its ways meet)
+                    products(st[d]);
+                    now.b += 8;
+                    const bool more = i + d + 1 < mine;
+                    if (now.b >= kb || !more) finish();
+                    if (now.b >= kb && more) {
                         do {
                             now.b -= kb;
                             ++now.ai;
@@ -873,9 +915,9 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
                         now.a = active_of(list, now.ai);
                         nf = (now.a.rows + 15) / 16;
                     }
-                } else if (i + d + 1 == mine) {
-                    finish();
                 }
+                if constexpr (NF > 1) load_next(i + d + 1 < mine);   // before the weight: loads are waited for in their order
+                load(st[d]);
             }
         }
     }
@@ -952,15 +994,13 @@ template <int T, bool S_F32>
 static hipError_t up(const LayerParams& p, hipStream_t st) {
     constexpr bool kF32 = T == BITSTACK_T_F32;
     const int steps = ((p.hidden + 127) / 128 + 7) / 8;   // blocks of columns of a wavefront
-    if (p.width % 4 != 0) return p.fragments == 1 ? up_as<T, 1, 1, kF32 ? 2 : 4, 0, S_F32, true>(p, st) : up_as<T, 1, 4, 1, 0, S_F32, true>(p, st);
+    if (p.width % 4 != 0) return p.fragments == 1 ? up_as<T, 1, 1, kF32 ? 2 : 4, 0, S_F32, true>(p, st) : up_as<T, 1, 2, 2, 0, S_F32, true>(p, st);
     if constexpr (kF32) {
         if (p.fragments == 1) return steps <= 2 ? up_as<T, 2, 1, 2, 2, S_F32>(p, st) : up_as<T, 4, 1, 2, 0, S_F32>(p, st);
-        if (p.fragments == 2) return up_as<T, 4, 2, 1, 0, S_F32>(p, st);
-        return up_as<T, 2, 4, 1, 0, S_F32>(p, st);
+        return up_as<T, 4, 2, 1, 0, S_F32>(p, st);
     } else {
-        if (p.fragments == 1) return steps <= 4 ? up_as<T, 2, 1, 4, 4, S_F32>(p, st) : steps <= 6 ? up_as<T, 2, 1, 2, 6, S_F32>(p, st) : up_as<T, 4, 1, 3, 0, S_F32>(p, st);
-        if (p.fragments == 2) return steps <= 4 ? up_as<T, 2, 2, 2, 4, S_F32>(p, st) : up_as<T, 4, 2, 2, 0, S_F32>(p, st);
-        return up_as<T, 2, 4, 2, 0, S_F32>(p, st);
+        if (p.fragments == 1) return steps <= 2 ? up_as<T, 4, 1, 2, 2, S_F32>(p, st) : steps <= 4 ? up_as<T, 2, 1, 4, 4, S_F32>(p, st) : steps <= 6 ? up_as<T, 2, 1, 2, 6, S_F32>(p, st) : up_as<T, 4, 1, 3, 0, S_F32>(p, st);
+        return steps <= 2 ? up_as<T, 4, 2, 2, 2, S_F32>(p, st) : steps <= 4 ? up_as<T, 2, 2, 2, 4, S_F32>(p, st) : up_as<T, 4, 2, 2, 0, S_F32>(p, st);
     }
 }
 static unsigned down_lds_bytes(int rows, int tokens, int top_k, int most) { return unsigned(8 * tokens * (rows + 4) * 4 + 16 * most + 5 * tokens * top_k + 16); }
@@ -972,30 +1012,22 @@ static hipError_t down_as(const LayerParams& p, hipStream_t st) {
 template <int PARTS, bool S_F32>
 static hipError_t down(const LayerParams& p, hipStream_t st) {
     constexpr int kMore = PARTS == 2 ? 2 : 1;
-    if (p.down_rows == 32) {
-        if (p.tokens <= 16 / PARTS) return down_as<2, 1, PARTS, true, 4, S_F32>(p, st);
-        if (p.fragments == 1) return down_as<2, 1, PARTS, false, 1 + kMore, S_F32>(p, st);
-        if (p.fragments == 2) return down_as<2, 2, PARTS, false, 1 + kMore, S_F32>(p, st);
-        return down_as<2, 4, PARTS, false, kMore, S_F32>(p, st);
-    }
-    if (p.down_rows != 64) return hipErrorInvalidValue;
+    if (p.down_rows == 32) return p.fragments == 1 ? down_as<2, 1, PARTS, false, 2, S_F32>(p, st) : down_as<2, 2, PARTS, false, 2, S_F32>(p, st);
     if (p.tokens <= 16 / PARTS) return down_as<4, 1, PARTS, true, 3, S_F32>(p, st);
     if (p.fragments == 1) return down_as<4, 1, PARTS, false, kMore, S_F32>(p, st);
-    if (p.fragments == 2) return down_as<4, 2, PARTS, false, 1, S_F32>(p, st);
-    return down_as<4, 4, PARTS, false, 1, S_F32>(p, st);
+    return down_as<4, 2, PARTS, false, kMore, S_F32>(p, st);
 }
 
 static std::atomic<int> g_force[4];
-LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k) {
+LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32) {
     LayerPlan plan;
     const int rows = tokens * top_k;
     const double each = double(rows) / experts;   // tokens of an expert, in the mean
-    plan.fragments = tokens <= 16 || each <= 6 ? 1 : tokens <= 32 || each <= 16 ? 2 : 4;
-    if (width % 4 != 0 && plan.fragments == 2) plan.fragments = 4;
+    plan.fragments = tokens <= 16 || each <= (f32 ? 16 : 8) ? 1 : 2;
     const int cap = 16 * plan.fragments;
     plan.most = std::min(experts, rows) + (tokens > cap ? rows / cap : 0);
     const double actives = experts * (1.0 - std::pow(1.0 - double(top_k) / experts, tokens));
-    plan.down_rows = tokens <= 8 ? 32 : 64;
+    plan.down_rows = 64;
     if (g_force[1]) plan.down_rows = g_force[1];
     if (g_force[3]) plan.fragments = g_force[3], plan.most = std::min(experts, rows) + (tokens > 16 * g_force[3] ? rows / (16 * g_force[3]) : 0);
     if (down_lds_bytes(plan.down_rows, tokens, top_k, plan.most) > 163840) plan.down_rows = 32;   // 64 tokens with many choices of many experts

@@ -178,9 +178,9 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
 struct LayerWorkspace {
     size_t list, row_weight, row_token, arrived, h, part, total;
 };
-unsigned h_columns(int width) { return unsigned(width + 63) / 64 * 64; }
+size_t h_columns(int width) { return (size_t(width) + 127) / 128 * 128; }
 LayerWorkspace layer_workspace(int tokens, int hidden, int width, int experts, int top_k, int h_parts) {
-    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k);
+    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
     const size_t rows = size_t(tokens) * top_k;
     LayerWorkspace w;
     w.list = 256;
@@ -335,10 +335,11 @@ int bitstack_combine(const void* h, int dtype, size_t ld_h, int h_rows, int widt
 size_t bitstack_f8_expert_layer_workspace_bytes(int tokens, int hidden, int width, int experts, int top_k) {
     if (tokens < 0 || tokens > kLayerTokens || !layer_sizes_ok(hidden, width, experts, top_k)) return 0;
     size_t most = 256;
-    for (int t = 1; t <= tokens; ++t) {
-        const size_t n = layer_workspace(t, hidden, width, experts, top_k, 3).total;
-        most = n > most ? n : most;
-    }
+    for (int t = 1; t <= tokens; ++t)
+        for (int parts = 2; parts <= 3; ++parts) {
+            const size_t n = layer_workspace(t, hidden, width, experts, top_k, parts).total;
+            most = n > most ? n : most;
+        }
     return most;
 }
 
@@ -361,12 +362,12 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     if (tokens > 1 && (ld_x < size_t(hidden) || ld_y < size_t(hidden) || (residual && ld_residual < size_t(hidden)) || ld_logits < size_t(experts)))
         return BITSTACK_E_SHAPE;
     const int h_parts = dtype == BITSTACK_T_F32 ? 3 : 2;
-    const size_t rows = size_t(tokens) * top_k, ld_h = h_columns(width), h_bytes = h_parts * rows * ld_h * 2;
+    const size_t rows = size_t(tokens) * top_k, h_bytes = h_parts * rows * h_columns(width) * 2;
     // reached by 32-bit offsets (h by 31-bit ones)
     if (size_t(w1->out - 1) * w1->ld + (size_t(hidden) + 15) / 16 * 16 > 0xffffffffu || h_bytes > kMaxRowBytes) return BITSTACK_E_RANGE;
     const LayerWorkspace at = layer_workspace(tokens, hidden, width, experts, top_k, h_parts);
     if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
-    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k);
+    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     LayerParams p{};
     p.x = x;
@@ -402,8 +403,6 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     p.arrived = reinterpret_cast<unsigned*>(ws + at.arrived);
     p.h = reinterpret_cast<unsigned short*>(ws + at.h);
     p.part = reinterpret_cast<float*>(ws + at.part);
-    p.ld_h = unsigned(ld_h);
-    p.h_part = unsigned(rows * ld_h);
     p.h_bytes = unsigned(h_bytes);
     p.h_parts = h_parts;
     p.down_rows = plan.down_rows;
