@@ -14,6 +14,7 @@ struct LayerExpert {   // that has tokens
 struct LayerPlan {
     int fragments;   // of 16 tokens in a unit of work; an expert with more tokens has several
     int most;        // entries of the list of experts, at most
+    int pack;        // k_layer_down: the parts of h are columns of one fragment
     int down_rows, tiles_down, splits;   // k_layer_down: rows of W2 in a tile, tiles, parts of the columns
 };
 LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32);   // f32: x
@@ -30,14 +31,14 @@ struct LayerParams {
     size_t ld_x, ld_logits, ld_w1, ld_w2, ld_r, ld_y;   // elements, of the weights bytes
     int dtype, logits_dtype, s1_f32, s2_f32;
     int tokens, top_k, renormalise, experts, hidden, width;
-    int fragments, most;   // LayerPlan
+    int fragments, most, pack;   // LayerPlan
     // workspace
     int* count;                // entries of list
     LayerExpert* list;         // [most]
     float* row_weight;         // [rows]
     unsigned char* row_token;  // [rows]
     unsigned* arrived;         // [tiles_down]
-    unsigned short* h;         // [blocks of 128 columns][rows][h_parts][128] bf16, the largest part first: what a product of 16 rows reads lies together
+    unsigned short* h;         // bf16 parts of h, in the order in which k_layer_down loads them
     float* part;               // [tiles_down][splits][tokens][down_rows]
     unsigned h_bytes;
     int h_parts;

@@ -616,14 +616,18 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
             }
             if (rank >= now.a.rows || n >= padded) continue;
             const float h = n < p.width ? f8_gate(gate, value) : 0.0f;
-            unsigned short* const to = p.h + (size_t(n >> 7) * rows + now.a.base + rank) * p.h_parts * 128 + (n & 127);
-            to[0] = upper16(h);
+            // where k_layer_down's lanes load it: see there
+            const int column = n & 127, piece = (column >> 6) * 2 + (column >> 3 & 1), lane_of = (column >> 4 & 3) * 16 + rank - 16 * f, parts = p.h_parts;
+            const int kb_down = (p.width + 127) / 128, per_part = p.pack ? 128 : 2048;
+            unsigned short* const to = p.h + (p.pack ? (size_t(n >> 7) * rows + now.a.base + rank) * (parts * 128) + column
+                                                     : ((size_t(now.ai) * NF + f) * kb_down + (n >> 7)) * (parts * 2048) + piece * 512 + lane_of * 8 + (column & 7));
             const float rest = left_over(h, upper(h));
-            if (p.h_parts == 2) {
-                to[128] = __builtin_bit_cast(unsigned short, __bf16(rest));
+            to[(parts - 1) * per_part] = upper16(h);   // the largest last
+            if (parts == 2) {
+                to[0] = __builtin_bit_cast(unsigned short, __bf16(rest));
             } else {
-                to[128] = upper16(rest);
-                to[256] = upper16(left_over(rest, upper(rest)));
+                to[per_part] = upper16(rest);
+                to[0] = upper16(left_over(rest, upper(rest)));
             }
         }
         if (kBufs == 2) buf ^= 1;
@@ -723,31 +727,37 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
         auto place = [&](int i) { return Place{active_of(list, i / kb), i / kb, i % kb}; };
         Place from = place(i0 + wave);
         int left = mine;
-        const int pack_part = min(ln / kPack, PARTS - 1);   // smallest first
-        auto h_row = [&](const Active& a, int f) {   // in elements
-            const unsigned r = unsigned(a.base + min(16 * f + ln % kPack, a.rows - 1)) * (PARTS * 128);
-            return PACK ? r + unsigned(PARTS - 1 - pack_part) * 128 : r;
+        // h lies as the lanes load it, 1024 bytes in a row to an instruction (a lane's 16 bytes of a row of its own would be a lookup of its own in L1, of which
+        // there is one a clock): [entry of the list][fragment of tokens][block][part, the smallest first][piece][lane][8].  Few tokens, which would leave most of that
+        // empty: [block][row][part][128].
+        auto h_lane = [&](const Active& a, int f) {   // a lane's place, in elements; no token: nothing is read
+            const int r = PACK ? ln % kPack : 16 * f + ln;
+            const bool there = r < a.rows && (!PACK || ln < PARTS * kPack);
+            return !there ? 0x40000000u : PACK ? unsigned((a.base + r) * PARTS + ln / kPack) * 128u + unsigned(kg) * 16u : unsigned(lane) * 8u;
         };
+        constexpr unsigned kFragment = unsigned(PARTS) * 2048;
+        auto h_at = [&](int ai, int f) { return PACK ? 0u : unsigned((ai * NF + f) * kb) * kFragment; };
+        const unsigned h_block = PACK ? unsigned(rows) * (PARTS * 128) : kFragment;
         const unsigned char* w_base;
         const unsigned char* s_base;
         unsigned h_from;
         auto enter = [&]() __attribute__((always_inline)) {
             w_base = p.w2 + (size_t(from.a.expert) * p.hidden + n0) * p.ld_w2;
             s_base = p.s2 + (size_t(from.a.expert) * s_rows + n0 / 128) * kb * (S_F32 ? 4 : 1);
-            h_from = h_row(from.a, 0);
+            h_from = h_lane(from.a, 0);
         };
         enter();
         struct H {
             v8bf v[kLoads][4];   // the smallest first
         };
-        auto load_h = [&](H& h, unsigned row, int b, bool live) __attribute__((always_inline)) {
-            const unsigned from = row + unsigned(b) * unsigned(rows) * (PARTS * 128);
+        auto load_h = [&](H& h, unsigned lane_at, unsigned fragment, int b, bool live) __attribute__((always_inline)) {
+            const unsigned from = fragment + unsigned(b) * h_block;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const unsigned none = live && b * 128 + piece_column(c, kg) < padded ? 0u : 0x80000000u;   // zeros arrive
 #pragma unroll
                 for (int q = 0; q < kLoads; ++q)
-                    h.v[q][c] = __builtin_bit_cast(v8bf, __builtin_amdgcn_raw_buffer_load_b128(hr, int(((from + unsigned(piece_column(c, kg) + (kLoads - 1 - q) * 128)) * 2u) | none), 0, 0));
+                    h.v[q][c] = __builtin_bit_cast(v8bf, __builtin_amdgcn_raw_buffer_load_b128(hr, int((lane_at * 2u) | none), int((from + unsigned(PACK ? piece_column(c, 0) : (q * 4 + c) * 512)) * 2u), 0));
             }
         };
         struct Stage {
@@ -759,7 +769,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
         auto load = [&](Stage& s) __attribute__((always_inline)) {
             const bool live = left > 0;
             s.w.load(buffer_of(w_base, live ? w_extent : 0), w_row, from.b, kg, p.width);
-            if constexpr (NF == 1) load_h(s.h, h_from, from.b, live);
+            if constexpr (NF == 1) load_h(s.h, h_from, h_at(from.ai, 0), from.b, live);
             s.s = load_scale<S_F32>(buffer_of(s_base, live ? unsigned(kb) * (S_F32 ? 4u : 1u) : 0), unsigned(from.b));
             if (--left > 0) {
                 from.b += 8;
@@ -786,7 +796,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
         H next[kNext + 1];
         auto load_next = [&](bool live) __attribute__((always_inline)) {
 #pragma unroll
-            for (int f = 0; f < kNext; ++f) load_h(next[f], h_row(now.a, f), now.b, live);
+            for (int f = 0; f < kNext; ++f) load_h(next[f], h_lane(now.a, f), h_at(now.ai, f), now.b, live);
         };
         auto products = [&](Stage& s) __attribute__((always_inline)) {
             if (ragged && now.b == kb - 1) s.w.end(now.b, kg, p.width);
@@ -859,7 +869,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
                         multiply(next[f]);
                     } else {
                         H h;
-                        load_h(h, h_row(now.a, f), now.b, true);
+                        load_h(h, h_lane(now.a, f), h_at(now.ai, f), now.b, true);
                         multiply(h);
                     }
                 }
@@ -1013,7 +1023,7 @@ template <int PARTS, bool S_F32>
 static hipError_t down(const LayerParams& p, hipStream_t st) {
     constexpr int kMore = PARTS == 2 ? 2 : 1;
     if (p.down_rows == 32) return p.fragments == 1 ? down_as<2, 1, PARTS, false, 2, S_F32>(p, st) : down_as<2, 2, PARTS, false, 2, S_F32>(p, st);
-    if (p.tokens <= 16 / PARTS) return down_as<4, 1, PARTS, true, 3, S_F32>(p, st);
+    if (p.pack) return down_as<4, 1, PARTS, true, 3, S_F32>(p, st);
     if (p.fragments == 1) return down_as<4, 1, PARTS, false, kMore, S_F32>(p, st);
     return down_as<4, 2, PARTS, false, kMore, S_F32>(p, st);
 }
@@ -1031,6 +1041,7 @@ LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, 
     if (g_force[1]) plan.down_rows = g_force[1];
     if (g_force[3]) plan.fragments = g_force[3], plan.most = std::min(experts, rows) + (tokens > 16 * g_force[3] ? rows / (16 * g_force[3]) : 0);
     if (down_lds_bytes(plan.down_rows, tokens, top_k, plan.most) > 163840) plan.down_rows = 32;   // 64 tokens with many choices of many experts
+    plan.pack = tokens <= 16 / (f32 ? 3 : 2);
     plan.tiles_down = (hidden + plan.down_rows - 1) / plan.down_rows;
     // Parts of the columns: a workgroup of each compute unit takes a part of 2.5 us and the bytes at 25 a nanosecond (more than an equal share of what the memory gives)
     plan.splits = 1;

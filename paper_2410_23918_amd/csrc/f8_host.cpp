@@ -178,7 +178,10 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
 struct LayerWorkspace {
     size_t list, row_weight, row_token, arrived, h, part, total;
 };
-size_t h_columns(int width) { return (size_t(width) + 127) / 128 * 128; }
+// bytes of h: the rows, or fragments of 16 tokens of every entry of the list; whole blocks of columns
+size_t h_bytes_of(const LayerPlan& plan, size_t rows, int width, int h_parts) {
+    return (plan.pack ? rows : size_t(plan.most) * plan.fragments * 16) * ((size_t(width) + 127) / 128) * h_parts * 256;
+}
 LayerWorkspace layer_workspace(int tokens, int hidden, int width, int experts, int top_k, int h_parts) {
     const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
     const size_t rows = size_t(tokens) * top_k;
@@ -188,7 +191,7 @@ LayerWorkspace layer_workspace(int tokens, int hidden, int width, int experts, i
     w.row_token = w.row_weight + align256(rows * 4);
     w.arrived = w.row_token + align256(rows);
     w.h = w.arrived + align256(size_t(plan.tiles_down) * 4);
-    w.part = w.h + align256(size_t(h_parts) * rows * h_columns(width) * 2);
+    w.part = w.h + align256(h_bytes_of(plan, rows, width, h_parts));
     w.total = w.part + (plan.splits > 1 ? align256(size_t(plan.tiles_down) * plan.splits * tokens * plan.down_rows * 4) : 0);
     return w;
 }
@@ -362,12 +365,12 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     if (tokens > 1 && (ld_x < size_t(hidden) || ld_y < size_t(hidden) || (residual && ld_residual < size_t(hidden)) || ld_logits < size_t(experts)))
         return BITSTACK_E_SHAPE;
     const int h_parts = dtype == BITSTACK_T_F32 ? 3 : 2;
-    const size_t rows = size_t(tokens) * top_k, h_bytes = h_parts * rows * h_columns(width) * 2;
+    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
+    const size_t rows = size_t(tokens) * top_k, h_bytes = h_bytes_of(plan, rows, width, h_parts);
     // reached by 32-bit offsets (h by 31-bit ones)
     if (size_t(w1->out - 1) * w1->ld + (size_t(hidden) + 15) / 16 * 16 > 0xffffffffu || h_bytes > kMaxRowBytes) return BITSTACK_E_RANGE;
     const LayerWorkspace at = layer_workspace(tokens, hidden, width, experts, top_k, h_parts);
     if (workspace_bytes < at.total) return BITSTACK_E_BUFSIZE;
-    const LayerPlan plan = layer_plan(tokens, hidden, width, experts, top_k, h_parts == 3);
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     LayerParams p{};
     p.x = x;
@@ -396,6 +399,7 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     p.width = width;
     p.fragments = plan.fragments;
     p.most = plan.most;
+    p.pack = plan.pack;
     p.count = reinterpret_cast<int*>(ws);
     p.list = reinterpret_cast<LayerExpert*>(ws + at.list);
     p.row_weight = reinterpret_cast<float*>(ws + at.row_weight);
