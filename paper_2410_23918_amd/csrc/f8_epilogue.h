@@ -75,25 +75,29 @@ __device__ __forceinline__ void add_residual(const F8Params& p, int row, int n, 
 
 // v Phi(v), Phi(v) = erfc(-v / sqrt 2) / 2: no digits are lost where Phi is small
 __device__ __forceinline__ float gelu(float v) { return v < -40.0f ? 0.0f : 0.5f * v * erfcf(v * -0.70710678118654752440f); }
-// v / (1 + exp(-c v)), c = 2 sqrt(2 / pi) (1 + 0.044715 v^2), as the gate of c v times 1 / c; beyond 16 the quotient is 1 or 0 in fp32
+// v / (1 + exp(-2 sqrt(2 / pi) (v + 0.044715 v^3))): seven instructions, the exponent's rounding, 2^-22 of it, counts where the value is small
 __device__ __forceinline__ float gelu_tanh(float v) {
-    const float c = fmaf(v * v, 0.07135481282553484f, 1.5957691216057308f);
-    const float y = f8_gate(c * v, __builtin_amdgcn_rcpf(c));
-    return v > 16.0f ? v : v < -16.0f ? 0.0f : y;
+    constexpr float kA = -2.3022081986f, kB = -0.1029432397f;   // -2 sqrt(2 / pi) / ln 2, and times 0.044715
+    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * fmaf(v * v, kB, kA)));
+}
+
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&a)[N]) {
+    auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) a[e] = f(a[e]);
+    };
+    if (act == BITSTACK_ACT_RELU) each([](float v) { return v < 0.0f ? 0.0f : v; });
+    else if (act == BITSTACK_ACT_GELU) each([](float v) { return gelu(v); });
+    else if (act == BITSTACK_ACT_GELU_TANH) each([](float v) { return gelu_tanh(v); });
+    else if (act == BITSTACK_ACT_SILU) each([](float v) { return f8_gate(v, 1.0f); });
 }
 
 // a: sums of columns n .. n + N - 1 of a row of y (n < cols), in place
 template <int N>
 __device__ __forceinline__ void epilogue(const F8Params& p, int row, int n, float (&a)[N]) {
     add_bias<N>(p, n, n, a);
-    auto each = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) a[e] = f(a[e]);
-    };
-    if (p.act == BITSTACK_ACT_RELU) each([](float v) { return v < 0.0f ? 0.0f : v; });
-    else if (p.act == BITSTACK_ACT_GELU) each([](float v) { return gelu(v); });
-    else if (p.act == BITSTACK_ACT_GELU_TANH) each([](float v) { return gelu_tanh(v); });
-    else if (p.act == BITSTACK_ACT_SILU) each([](float v) { return f8_gate(v, 1.0f); });
+    activate<N>(p.act, a);
     add_residual<N>(p, row, n, a);
 }
 template <int N>

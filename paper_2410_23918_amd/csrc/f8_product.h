@@ -473,6 +473,14 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
     constexpr bool kGated = EPI == kEpiGated;
     constexpr int kLd = S::kRows + 4, kWide = kGated ? S::kRows / 2 : S::kRows, kPieces = kWide / 8;   // floats from token to token; outputs of a token
     static_assert(FT % FTS == 0 && S::kToks / FT * FTS * kLd * 4 <= S::kLds, "a part of the tile in LDS");
+    // a thread's eight columns are the same for all its tokens
+    constexpr int kStep = 64 * S::kWaves / kPieces;   // tokens at a time
+    const int piece = tid % kPieces, n = n0 + piece * 8;
+    float bias[8] = {}, bias_u[8] = {};
+    if (n < p.cols) {
+        add_bias<8>(p, n, n, bias);
+        if constexpr (kGated) add_bias<8>(p, n, p.cols + n, bias_u);
+    }
     float* const sums = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int i0 = 0; i0 < FT; i0 += FTS) {
@@ -485,19 +493,37 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
                 *reinterpret_cast<v4f*>(sums + ((wt * FTS + i) * 16 + ln) * kLd + at) = acc[j][i0 + i];
             }
         __syncthreads();
-        for (int k = tid; k < S::kToks / FT * FTS * kPieces; k += 64 * S::kWaves) {
-            const int t = k / kPieces, n = n0 + k % kPieces * 8, tok = t / (16 * FTS) * 16 * FT + i0 * 16 + t % (16 * FTS);
-            if (tok >= rows || n >= p.cols) continue;
-            const v4f* const from = reinterpret_cast<const v4f*>(sums + t * kLd + k % kPieces * 8);
-            float a[8], u[8];
+        if (n >= p.cols) continue;
+        constexpr int kAll = S::kToks / FT * FTS / kStep, kTogether = kAll < 4 ? kAll : 4;   // tokens of a thread, those whose residuals are requested together
+        static_assert(kAll % kTogether == 0, "whole groups");
+#pragma unroll 1
+        for (int t0 = tid / kPieces; t0 < S::kToks / FT * FTS; t0 += kTogether * kStep) {
+            float r[kTogether][8];
+            int tok[kTogether];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a[e] = from[e >> 2][e & 3];
-                if constexpr (kGated) u[e] = from[kWide / 4 + (e >> 2)][e & 3];
+            for (int k = 0; k < kTogether; ++k) {
+                const int t = t0 + k * kStep;
+                tok[k] = t / (16 * FTS) * 16 * FT + i0 * 16 + t % (16 * FTS);
+                if (p.residual) load_as<8>(p.y_dtype, p.residual, size_t(row0 + min(tok[k], rows - 1)) * p.ld_r + n, p.cols - n, r[k]);
             }
-            if constexpr (kGated) epilogue_gated<8>(p, row0 + tok, n, a, u);
-            else epilogue<8>(p, row0 + tok, n, a);
-            store_as<8>(p.y_dtype, p.y, size_t(row0 + tok) * p.ldy + n, p.cols - n, a);
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+                const v4f* const from = reinterpret_cast<const v4f*>(sums + (t0 + k * kStep) * kLd + piece * 8);
+                float a[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = from[e >> 2][e & 3] + bias[e];
+                if constexpr (kGated) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) a[e] = f8_gate(a[e], from[kWide / 4 + (e >> 2)][e & 3] + bias_u[e]);
+                } else {
+                    activate<8>(p.act, a);
+                }
+                if (p.residual) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) a[e] += r[k][e];
+                }
+                if (tok[k] < rows) store_as<8>(p.y_dtype, p.y, size_t(row0 + tok[k]) * p.ldy + n, p.cols - n, a);
+            }
         }
     }
 }
