@@ -34,7 +34,10 @@ class ExpertLayer:
         return cls(router, all_of(stacks1), all_of(stacks2), top_k)
 
     def __call__(self, x):
-        r = B.route(x.float() @ self.router.T, self.top_k)
+        logits = x.float() @ self.router.T
+        if x.shape[0] <= 64:   # a few tokens: the whole layer in one call, activations as they are
+            return B.expert_layer_f8(x, logits, self.w1, self.w2, self.top_k)
+        r = B.route(logits, self.top_k)
         h = B.grouped_linear_f8(x, *self.w1, r.offsets, r.rows)              # a row for each (token, expert), sorted by expert
         y = B.grouped_linear_f8(h, *self.w2, r.offsets, gated=True)
         return B.combine(y, r.slots, r.weights)

@@ -102,7 +102,8 @@ int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* 
 /* The same with what follows a product in a decoder, on the fp32 sums a[t][o], rounded once:
  *     y = act(a + bias) + residual,                                      columns of y: out
  *     SILU_GATED: y = g / (1 + exp(-g)) u + residual, (g, u) = a + bias in halves, columns of y: out / 2   (w's rows are gates above values, out is even)
- * RELU: max(v, 0).  GELU: v (1 + erf(v / sqrt 2)) / 2.  GELU_TANH: v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2.  SILU: v / (1 + exp(-v)).
+ * RELU: max(v, 0).  GELU: v (1 + erf(v / sqrt 2)) / 2.  GELU_TANH: v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2, 0 where
+ * that is below 2^-122.  SILU: v / (1 + exp(-v)).
  *   bias: [out] of bias_dtype (not F8), or NULL.  residual: [rows][columns of y] of y_dtype, ld_residual elements from row to row, or NULL; it may be y, but
  *   must not overlap it otherwise.  All NULL and NONE: bitstack_f8_linear.
  * Gates and values are written half as wide and never as they are.  Where out / 2 is a multiple of 128 (a block's scale is then that of gates or of values alone; the

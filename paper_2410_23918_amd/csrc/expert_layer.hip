@@ -28,6 +28,10 @@ typedef unsigned v4u __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ v4f multiply8(const v8h& w, const v8h& x, const v4f& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x, c, 0, 0, 0); }
 __device__ __forceinline__ v4f multiply8(const v8bf& w, const v8bf& x, const v4f& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0); }
 
+// Between a product and what reads its result lie eight wait states, which the hardware does not keep.  The compiler does within a block of instructions; where it had moved the
+// reader past a branch there was one.  What has read the product is settled before any branch.
+__device__ __forceinline__ void settle(v4f& v) { asm volatile("" : "+v"(v)); }
+
 // eight e4m3 numbers as fp16 or bf16, exactly
 __device__ __forceinline__ void widen(int lo, int hi, v8h& to) {
     const v2h a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true),
@@ -388,9 +392,8 @@ __device__ __forceinline__ Active active_of(const LayerExpert* list, int a) {
 // most; its eight wavefronts take every eighth block of columns each and meet in LDS.  A workgroup has a run of units and requests the weight DEPTH blocks ahead, over
 // the ends of units.
 //   KEEP > 0: a wavefront has at most KEEP blocks of columns and keeps its tokens' share of them in registers for as long as the units are the same expert's; a
-// compute unit's registers hold 16 tokens of 6144 or 32 of 4096.  Read anew for every unit they come from beyond L2, which the stream of the weight has gone through since
-// the last unit, and take as much of what the memory gives as a weight of as many rows: 64 tokens through two of eight experts, 28672 x 4096, 328 us, without
-// the tokens' loads 183.  KEEP = 0: they are (FR = 4, so that there are more rows to each load).
+// compute unit's registers hold 16 tokens of 6144 or 32 of 4096.  KEEP = 0: they are read anew for every unit, FR = 4 so that there are more rows to each load (64
+// tokens through two of eight experts, 28672 x 4096: FR = 2 328 us, FR = 4 247, kept 187; 183 without the tokens' loads, timing only).
 //   ODD: width is no multiple of 4, so that a lane's four rows may have two scales.
 template <int T, int FR, int NF, int DEPTH, int KEEP, bool S_F32, bool ODD>
 __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
@@ -491,8 +494,10 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
     int nf;           // their fragments of tokens
     auto enter_late = [&]() __attribute__((always_inline)) {
         nf = (now.a.rows + 15) / 16;
+        if constexpr (KEEP == 0) {
 #pragma unroll
-        for (int f = kAhead; f < NF; ++f) x_late[f] = token_row(now.a, f);
+            for (int f = kAhead; f < NF; ++f) x_late[f] = token_row(now.a, f);
+        }
     };
     enter_late();
     enter();
@@ -508,14 +513,19 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
     clear();
     KeptX<T> kept[KEEP + 1][NF];
     auto keep = [&]() __attribute__((always_inline)) {   // the tokens of the unit that comes
+        const E* row[NF];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) row[f] = token_row(now.a, f);
+        int kg_here = kg;
+        asm volatile("" : "+v"(kg_here));   // nothing of this is made ahead and kept in registers
 #pragma unroll
         for (int k = 0; k < KEEP; ++k) {
             const int b = min(wave + 8 * k, kb - 1);
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 RawX<T> x;
-                x.load(x_late[f], b, kg, p.hidden);
-                if (ragged && b == kb - 1) x.end(b, kg, p.hidden);
+                x.load(row[f], b, kg_here, p.hidden);
+                if (ragged && b == kb - 1) x.end(b, kg_here, p.hidden);
                 kept[k][f].keep(x);
                 if constexpr (T == BITSTACK_T_F32) __builtin_amdgcn_sched_barrier(0);   // registers
             }
@@ -552,6 +562,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
                 for (int c = 0; c < 4; ++c) part = multiply8(w[c], x.part(q, c), part);
 #pragma unroll
             for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[v], scale[j][v], acc[j][f][v]);
+            if constexpr (NF > 1) settle(acc[j][f]);
         };
         if constexpr (KEEP > 0) {   // a fragment of rows at a time: registers
 #pragma unroll
@@ -804,6 +815,7 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
             auto add = [&](const v4f& part, int j, int f) __attribute__((always_inline)) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[j][f][v] = fmaf(part[v], scale, acc[j][f][v]);
+                if constexpr (NF > 1) settle(acc[j][f]);
             };
             constexpr v4f kNone = {0.0f, 0.0f, 0.0f, 0.0f};
             if constexpr (NF == 1) {
@@ -837,14 +849,15 @@ __global__ __launch_bounds__(512, 2) void k_layer_down(LayerParams p) {
                             for (int c = 0; c < 4; ++c)
 #pragma unroll
                                 for (int f = 0; f < 2; ++f) part[f] = multiply8(w[c], next[f].v[q][c], part[f]);
+                        add(part[0], j, 0);
                         add(part[1], j, 1);
                     } else {
 #pragma unroll
                         for (int q = 0; q < kLoads; ++q)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) part[0] = multiply8(w[c], next[0].v[q][c], part[0]);
+                        add(part[0], j, 0);
                     }
-                    add(part[0], j, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
@@ -1028,7 +1041,6 @@ static hipError_t down(const LayerParams& p, hipStream_t st) {
     return down_as<4, 2, PARTS, false, kMore, S_F32>(p, st);
 }
 
-static std::atomic<int> g_force[4];
 LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, bool f32) {
     LayerPlan plan;
     const int rows = tokens * top_k;
@@ -1038,10 +1050,8 @@ LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, 
     plan.most = std::min(experts, rows) + (tokens > cap ? rows / cap : 0);
     const double actives = experts * (1.0 - std::pow(1.0 - double(top_k) / experts, tokens));
     plan.down_rows = 64;
-    if (g_force[1]) plan.down_rows = g_force[1];
-    if (g_force[3]) plan.fragments = g_force[3], plan.most = std::min(experts, rows) + (tokens > 16 * g_force[3] ? rows / (16 * g_force[3]) : 0);
     if (down_lds_bytes(plan.down_rows, tokens, top_k, plan.most) > 163840) plan.down_rows = 32;   // 64 tokens with many choices of many experts
-    plan.pack = tokens <= 16 / (f32 ? 3 : 2);
+    plan.pack = tokens <= 16 / (f32 ? 3 : 2) && plan.down_rows == 64;
     plan.tiles_down = (hidden + plan.down_rows - 1) / plan.down_rows;
     // Parts of the columns: a workgroup of each compute unit takes a part of 2.5 us and the bytes at 25 a nanosecond (more than an equal share of what the memory gives)
     plan.splits = 1;
@@ -1054,7 +1064,6 @@ LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, 
             plan.splits = s;
         }
     }
-    if (g_force[2]) plan.splits = g_force[2];
     return plan;
 }
 
@@ -1069,4 +1078,3 @@ hipError_t launch_expert_layer(const LayerParams& p, hipStream_t st) {
 }
 
 }  // namespace bitstack
-extern "C" void bitstack_layer_force(int i, int v) { bitstack::g_force[i] = v; }

@@ -108,6 +108,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     };
     F8Plan plan = plan_in(~size_t(0));
     if (!f8_launchable(plan)) return BITSTACK_E_RANGE;   // with any kernel's tiles
+    if (parts_only(epi, w->out) && plan.part_bytes >> 37) return BITSTACK_E_RANGE;   // joining them is one launch, 32 bytes to a thread
     const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
     Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {

@@ -976,29 +976,36 @@ __global__ __launch_bounds__(256) void k_f8_join_with(F8Params p) {
     else store4_in(p, p.cols, tok, n, epilogue4(p, tok, n, sum));
 }
 
-// Gates and values of a weight whose halves do not begin with a block of 128 rows, so that a wavefront's rows of both have several scales: the sums of all rows,
-// as k_f8_tile leaves them without gates, are looked up one by one.
+// Gates and values of a weight whose halves do not begin with a block of 128 rows, so that a wavefront's rows of both have several scales: a wavefront takes 16
+// outputs of 16 tokens from the sums of all rows, as k_f8_tile leaves them without gates, four rows of a token to a load; values that do not begin with a multiple of
+// four take two.  Bound by memory: 2048 x 7000 from 115 MB of sums.
 template <int FR, int FT, int WR, int WT>
 __global__ __launch_bounds__(256) void k_f8_join_rows(F8Params p) {
-    const int nrt = (p.out + 16 * FR * WR - 1) / (16 * FR * WR), wide = (p.cols + 3) / 4;
-    const size_t step = size_t(nrt) * p.n_tiles * 8 * (FR * FT * 256);
-    for (size_t k = size_t(blockIdx.x) * 256 + threadIdx.x; k < size_t(p.rows) * wide; k += size_t(gridDim.x) * 256) {
-        const int tok = int(k / wide), n = int(k % wide) * 4;
-        auto sum_of = [&](int row) {
-            const int rt = row / (16 * FR * WR), wr = row / (16 * FR) % WR, kg = row / (4 * FR) % 4, j = row / 4 % FR;
-            const int tt = tok / (16 * FT * WT), wt = tok / (16 * FT) % WT, i = tok / 16 % FT;
-            const float* from = p.part + (((size_t(rt) * p.n_tiles + tt) * 8 + wt * WR + wr) * (FR * FT) + j * FT + i) * 256 + (kg * 16 + tok % 16) * 4 + row % 4;
-            float sum = from[0];
-            for (int s = 1; s < p.slices; ++s) sum += from[s * step];
-            return sum;
-        };
-        v4f gate = {}, value = {};
-        for (int e = 0; e < 4 && n + e < p.cols; ++e) {
-            gate[e] = sum_of(n + e);
-            value[e] = sum_of(p.cols + n + e);
-        }
-        store4_in(p, p.cols, tok, n, epilogue4_gated(p, tok, n, gate, value));
+    const int lane = threadIdx.x & 63, nrt = (p.out + 16 * FR * WR - 1) / (16 * FR * WR), wide = (p.cols + 15) / 16;
+    const size_t unit = size_t(blockIdx.x) * 4 + (threadIdx.x >> 6), step = size_t(nrt) * p.n_tiles * 8 * (FR * FT * 64);
+    const int tok = int(unit / wide) * 16 + (lane & 15), n = int(unit % wide) * 16 + (lane >> 4) * 4;
+    if (tok >= p.rows || n >= p.cols) return;
+    const int tt = tok / (16 * FT * WT), wt = tok / (16 * FT) % WT, i = tok / 16 % FT;
+    auto four = [&](int row) {   // of a multiple of four
+        if (row >= p.out) return v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        const int rt = row / (16 * FR * WR), wr = row / (16 * FR) % WR, kg = row / (4 * FR) % 4, j = row / 4 % FR;
+        const v4f* from = reinterpret_cast<const v4f*>(p.part) + (((size_t(rt) * p.n_tiles + tt) * 8 + wt * WR + wr) * (FR * FT) + j * FT + i) * 64 + kg * 16 + tok % 16;
+        v4f sum = from[0];
+#pragma unroll 4
+        for (int s = 1; s < p.slices; ++s) sum += from[s * step];
+        return sum;
+    };
+    const int first = p.cols + n, turn = first & 3;
+    const v4f gate = four(n), low = four(first - turn), high = turn ? four(first - turn + 4) : low;
+    v4f value;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        value[e] = low[e];
+#pragma unroll
+        for (int k = 1; k < 4; ++k)
+            if (turn == k) value[e] = e + k < 4 ? low[(e + k) & 3] : high[(e + k) & 3];
     }
+    store4_in(p, p.cols, tok, n, epilogue4_gated(p, tok, n, gate, value));
 }
 
 static hipError_t allow_lds(const void* kernel, std::atomic<bool>& done, int bytes) {   // (doing it twice is harmless)
@@ -1016,8 +1023,8 @@ static hipError_t join(const F8Params& p, hipStream_t st) {
     if constexpr (EPI == kEpiNone) {
         if (p.slices > 1) hipLaunchKernelGGL((k_f8_join<FR, FT, WR, WT>), dim3(unsigned((units + 3) / 4)), dim3(256), 0, st, p);
     } else if (p.parts_only) {
-        const size_t fours = size_t(p.rows) * ((p.cols + 3) / 4);
-        hipLaunchKernelGGL((k_f8_join_rows<FR, FT, WR, WT>), dim3(unsigned(std::min<size_t>((fours + 255) / 256, 1 << 16))), dim3(256), 0, st, p);
+        const size_t fragments = size_t((p.rows + 15) / 16) * ((p.cols + 15) / 16);
+        hipLaunchKernelGGL((k_f8_join_rows<FR, FT, WR, WT>), dim3(unsigned((fragments + 3) / 4)), dim3(256), 0, st, p);
     } else if (p.slices > 1) {
         const size_t fragments = units * (EPI == kEpiGated ? FR / 2 : FR);
         hipLaunchKernelGGL((k_f8_join_with<FR, FT, WR, WT, EPI>), dim3(unsigned((fragments + 3) / 4)), dim3(256), 0, st, p);

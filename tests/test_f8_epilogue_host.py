@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2410_23918_amd as B
-from test_asm_distances import CSRC, HIPCC, faults, functions
+from test_asm_distances import CSRC, HIPCC, faults, functions, registers, too_close, wrap
 
 OK, NULL, SHAPE, RANGE, ALIGN, SIZE, ARG = 0, -1, -2, -3, -4, -6, -8
 P = 1 << 20   # an aligned address
@@ -82,16 +82,44 @@ def test_without_a_gpu_tensor():
             B.linear_f8(**(dict(x=x, q=q, scales=s) | change))
 
 
+# wait states that the compiler leaves in one block between a product and an instruction of another kind that reads its result
+BEHIND = {"v_mfma_f32_16x16x32_f16": 8, "v_mfma_f32_16x16x32_bf16": 8, "v_mfma_scale_f32_16x16x128_f8f6f4": 12}
+
+
+def early_readers(assembly):
+    """instructions that read a product's result too early, along every path: the compiler has been seen to leave one wait state where a branch lies between"""
+    found = []
+    for name, code, before in functions(assembly):
+        for at, ins in enumerate(code):
+            if ins.product or not ins.name.startswith(("v_", "ds_", "buffer_store", "global_store")):
+                continue
+            operands = [registers(o) for o in ins.text.partition(" ")[2].split(",")]
+            reads = set().union(*(operands[1:] if ins.vector and not ins.name.startswith(("v_fmac", "v_dot", "v_mac")) else operands))
+            for product, states in BEHIND.items():
+                other = too_close(code, before, at, states, lambda o: o.name == product and o.writes & reads)
+                if other:
+                    found.append(f"{name}: {other.text}   ...   {ins.text}")
+    return found
+
+
+def test_early_readers_are_told_apart():
+    product = "\tv_mfma_f32_16x16x32_f16 v[0:3], v[16:19], v[20:23], v[0:3]"
+    assert early_readers(wrap(product, "\ts_nop 6", "\tv_fma_f32 v9, v3, v8, v9")) and not early_readers(wrap(product, "\ts_nop 7", "\tv_fma_f32 v9, v3, v8, v9"))
+    assert early_readers(wrap(product, "\ts_cbranch_scc1 .LBB0_1", "\ts_nop 15", ".LBB0_1:", "\tds_write_b128 v9, v[0:3]"))
+    assert not early_readers(wrap(product, "\tv_fma_f32 v9, v4, v8, v9"))
+
+
 @pytest.mark.skipif(shutil.which(HIPCC) is None, reason="no compiler")
-@pytest.mark.parametrize("source", ["f8_epilogue.hip", "f8_gated.hip"])
+@pytest.mark.parametrize("source", ["f8_epilogue.hip", "f8_gated.hip", "expert_layer.hip"])
 def test_assembly(source, tmp_path):
     from paper_2410_23918_amd import build
     out = tmp_path / "kernels.asm"
     subprocess.run([HIPCC, *[f for f in build.FLAGS if f != "-shared"], "--cuda-device-only", "-S", str(CSRC / source), "-o", str(out)], check=True, capture_output=True)
     assembly = out.read_text()
-    assert len([name for name, code, _ in functions(assembly) if any(i.product for i in code)]) == 32   # as many as without an epilogue
-    assert sum(i.in_asm and i.vector for _, code, _ in functions(assembly) for i in code) >= 10
-    found = faults(assembly)
+    if source != "expert_layer.hip":
+        assert len([name for name, code, _ in functions(assembly) if any(i.product for i in code)]) == 32   # as many as without an epilogue
+        assert sum(i.in_asm and i.vector for _, code, _ in functions(assembly) for i in code) >= 10
+    found = faults(assembly) + early_readers(assembly)
     assert not found, "\n".join(found[:10])
     assert "v_pk_fma_f32" not in assembly and "v_pk_mul_f32" not in assembly and "v_pk_add_f32" not in assembly
     assert "scratch_load" not in assembly   # no sum leaves the registers

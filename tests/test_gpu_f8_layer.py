@@ -102,3 +102,20 @@ def test_layer(tokens, experts, top_k, hidden, width, dtype, scales):
         y = B.expert_layer_f8(x, logits, w1, w2, top_k, renormalise=not masked, residual=residual)
         assert y.dtype is dtype and y.shape == x.shape
         check(y, *reference(x, logits, w1, w2, top_k, not masked, residual))
+
+
+LONG = [  # more columns, more units of work than workgroups, experts with more tokens than a unit takes
+    (9, 8, 2, 2300, 1056), (20, 4, 2, 2300, 260), (40, 3, 2, 4096, 640), (12, 6, 2, 5001, 520), (40, 3, 2, 5001, 520), (10, 4, 2, 8200, 264), (64, 2, 2, 8200, 264), (64, 4, 4, 1500, 640),
+    (50, 5, 2, 2300, 131), (64, 2, 1, 2300, 1001), (64, 64, 8, 2304, 1024), (1, 16, 8, 4096, 1536), (5, 4, 3, 6144, 2048),
+]
+
+
+@pytest.mark.parametrize("scales", ["e8m0", "f32"])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["f16", "bf16", "f32"])
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,width", LONG)
+def test_longer(tokens, experts, top_k, hidden, width, dtype, scales):
+    g = rng(tokens + 7 * hidden + width)
+    w1, w2 = weights(g, experts, 2 * width, hidden, scales), weights(g, experts, hidden, width, scales)
+    x, logits = inputs(tokens, experts, hidden, dtype, g, tokens % 2 == 0)
+    residual = torch.randn((tokens, hidden), generator=g, device=DEV).to(dtype)
+    check(B.expert_layer_f8(x, logits, w1, w2, top_k, residual=residual), *reference(x, logits, w1, w2, top_k, True, residual))
