@@ -14,6 +14,7 @@ struct LayerExpert {   // that has tokens
 struct LayerPlan {
     int fragments;   // of 16 tokens in a unit of work; an expert with more tokens has several
     int most;        // entries of the list of experts, at most
+    int up_few;      // k_layer_up: eight gates to a unit, not 16
     int pack;        // k_layer_down: the parts of h are columns of one fragment
     int down_rows, tiles_down, splits;   // k_layer_down: rows of W2 in a tile, tiles, parts of the columns
 };
@@ -31,7 +32,7 @@ struct LayerParams {
     size_t ld_x, ld_logits, ld_w1, ld_w2, ld_r, ld_y;   // elements, of the weights bytes
     int dtype, logits_dtype, s1_f32, s2_f32;
     int tokens, top_k, renormalise, experts, hidden, width;
-    int fragments, most, pack;   // LayerPlan
+    int fragments, most, up_few, pack;   // LayerPlan
     // workspace
     int* count;                // entries of list
     LayerExpert* list;         // [most]

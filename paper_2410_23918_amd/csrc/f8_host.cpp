@@ -400,6 +400,7 @@ int bitstack_f8_expert_layer(const void* x, int dtype, size_t ld_x, const void* 
     p.width = width;
     p.fragments = plan.fragments;
     p.most = plan.most;
+    p.up_few = plan.up_few;
     p.pack = plan.pack;
     p.count = reinterpret_cast<int*>(ws);
     p.list = reinterpret_cast<LayerExpert*>(ws + at.list);

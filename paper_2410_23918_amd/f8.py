@@ -269,24 +269,33 @@ def _linear_with(x, q, scales, gated, bias, activation, residual, y, out_dtype, 
     rows, dtype, held = _fill_rows(x, inn, gated)
     device = q.device
     _same_device(device, scales, bias, residual, y, workspace, *held)
+    args = _args
+    e = args.e
+    e.activation = act
+    if bias is None:
+        e.bias = None
+    else:
+        if bias.dim() != 1 or bias.shape[0] != out or not bias.is_contiguous():
+            raise ValueError("bias: one for each row of q, contiguous")
+        e.bias, e.bias_dtype = bias.data_ptr(), _type(bias, "bias")
     if act == 5:
         _need(out % 2 == 0, "silu_gated: gates above values are needed, an even number of rows")
         out //= 2
     dtype = out_dtype or (dtype if y is None else y.dtype)
-    args = _args
-    e = args.e
-    e.bias, e.bias_dtype, e.activation, e.residual, e.ld_residual = None, 0, act, None, 0
-    if bias is not None:
-        _need(bias.dim() == 1 and bias.shape[0] == q.shape[0] and bias.is_contiguous(), "bias: one for each row of q, contiguous")
-        e.bias, e.bias_dtype = bias.data_ptr(), _type(bias, "bias")
-    if residual is not None:
-        _need(residual.shape == (rows, out) and residual.dtype is dtype, f"residual: [{rows}, {out}] of y's type")
+    if residual is None:
+        e.residual = None
+    else:
+        if residual.shape != (rows, out) or residual.dtype is not dtype:
+            raise ValueError(f"residual: [{rows}, {out}] of y's type")
         e.residual, e.ld_residual = residual.data_ptr(), _matrix(residual, "residual")
     with _on(device, stream, (*held, q, scales, bias, residual, y, workspace)) as handle:
         if y is None:
             y = q.new_empty((rows, out), dtype=dtype)
+            ld_y = out
         else:
-            _need(y.shape == (rows, out) and y.dtype is dtype, f"y: [{rows}, {out}] is needed")
+            if y.shape != (rows, out) or y.dtype is not dtype:
+                raise ValueError(f"y: [{rows}, {out}] is needed")
+            ld_y = _matrix(y, "y")
         t = _type(y, "y")
         if workspace is None:
             nbytes = L.bitstack_f8_epilogue_call_workspace_bytes(args.xp, args.wp, args.ep, t)
@@ -295,8 +304,9 @@ def _linear_with(x, q, scales, gated, bias, activation, residual, y, out_dtype, 
         else:
             _need(workspace.is_contiguous(), "workspace: contiguous")
             nbytes = workspace.numel() * workspace.element_size()
-        _check(L.bitstack_f8_linear_epilogue(args.xp, args.wp, args.ep, y.data_ptr(), t, _matrix(y, "y"), None if workspace is None else workspace.data_ptr(), nbytes, handle),
-               "bitstack_f8_linear_epilogue")
+        rc = L.bitstack_f8_linear_epilogue(args.xp, args.wp, args.ep, y.data_ptr(), t, ld_y, None if workspace is None else workspace.data_ptr(), nbytes, handle)
+        if rc:
+            raise BitStackError(rc, "bitstack_f8_linear_epilogue")
     return y
 
 
