@@ -1,6 +1,7 @@
 /*
- * bitstack_f8.h -- products in 8-bit floating point with a scale for each block of 128, the same grouped by
- * expert, and the routing of tokens to experts, on MI355X (gfx950).
+ * bitstack_f8.h -- products in 8-bit floating point with a scale for each block of 128, the same with a bias, an
+ * activation and a residual, the same grouped by expert, the routing of tokens to experts, and a whole layer of experts
+ * for a few tokens, on MI355X (gfx950).
  *
  * Next to a stack of residual blocks a weight can be held in 8-bit floating point: what the materialising path
  * restores (bitstack_restore_weight) in half the bytes and at twice the rate of the matrix cores, or a weight that

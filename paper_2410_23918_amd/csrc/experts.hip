@@ -1,4 +1,4 @@
-// Around the products grouped by expert (f8_product.hip): which experts a token goes to and where its rows lie, and the
+// Around the products grouped by expert (f8_product.h): which experts a token goes to and where its rows lie, and the
 // weighted sums of a token's rows.
 #include <hip/hip_runtime.h>
 

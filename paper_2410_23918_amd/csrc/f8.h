@@ -1,4 +1,4 @@
-// Shared by the 8-bit kernels (f8_rows.hip, f8_product.hip), the routing (experts.hip) and their host code (f8_host.cpp).
+// Shared by the 8-bit kernels (f8_rows.hip, f8_product.h), the routing (experts.hip), the layer of experts (expert_layer.hip) and their host code (f8_host.cpp).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -73,6 +73,8 @@ __device__ __forceinline__ void add_residual(const F8Params& p, int row, int n, 
     for (int e = 0; e < N; ++e) a[e] += r[e];
 }
 
+// What an activation costs in the largest tiles, where nothing hides it: 2048 tokens, 28672 x 8192, fp16, in a graph: bias and residual 423 us (the bare product 408),
+// with relu 425, gelu_tanh 433, silu 447, gelu 495.
 // v Phi(v), Phi(v) = erfc(-v / sqrt 2) / 2: no digits are lost where Phi is small
 __device__ __forceinline__ float gelu(float v) { return v < -40.0f ? 0.0f : 0.5f * v * erfcf(v * -0.70710678118654752440f); }
 // v / (1 + exp(-2 sqrt(2 / pi) (v + 0.044715 v^3))): seven instructions, the exponent's rounding, 2^-22 of it, counts where the value is small

@@ -457,7 +457,9 @@ __device__ __forceinline__ void finish_tile(const F8Params& p, unsigned char* sm
     }
 }
 
-// The same with an epilogue: the sums meet in LDS as they are, FTS fragments of the tokens at a time, and a thread takes eight neighbouring outputs from there.
+// The same with an epilogue: the sums meet in LDS as they are, FTS fragments of the tokens at a time, and a thread takes eight neighbouring outputs from there
+// (the lanes' own four would be pieces of 8 bytes of y and of the residual).  2048 tokens, 28672 x 4096 gated in tiles of 256 x 256: 254 us beside other calls, 230 in a graph with the
+// rows' 8 bits, the bare product 223; its seven rounds of sums go through LDS in two halves each.
 template <class S, int FR, int FT, int WR, int EPI, int FTS>
 __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned char* smem, const v4f (&acc)[FR][FT], size_t tile, int n0, int row0, int rows) {
     const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, kg = lane >> 4;
@@ -947,7 +949,8 @@ __global__ __launch_bounds__(256) void k_f8_join(F8Params p) {
     for (int j = 0; j < FR; ++j) store4(p, t.row0 + tok, n + 4 * j, sum[j]);
 }
 
-// The same with an epilogue: a wavefront takes one fragment of the weight's rows (gated: a pair), so that there are enough of them for the memory.
+// The same with an epilogue: a wavefront takes one fragment of the weight's rows (gated: a pair), so that there are enough of them for the memory.  300 x 4096 from two
+// slices, with a residual, 6.4 us: 10 MB of sums, 5 MB in and out.
 template <int FR, int FT, int WR, int WT, int EPI>
 __global__ __launch_bounds__(256) void k_f8_join_with(F8Params p) {
     constexpr bool kGated = EPI == kEpiGated;
