@@ -107,8 +107,9 @@ int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* 
  * that is below 2^-122.  SILU: v / (1 + exp(-v)).
  *   bias: [out] of bias_dtype (not F8), or NULL.  residual: [rows][columns of y] of y_dtype, ld_residual elements from row to row, or NULL; it may be y, but
  *   must not overlap it otherwise.  All NULL and NONE: bitstack_f8_linear.
- * Gates and values are written half as wide and never as they are.  Where out / 2 is a multiple of 128 (a block's scale is then that of gates or of values alone; the
- * weight below 4 GiB) they meet inside the product; otherwise the sums of all rows go through the workspace, in more time. */
+ * Gates and values are written half as wide and never as they are.  Where out / 2 is a multiple of 128 (a block's scale is then that of gates or of values alone) and
+ * (out / 2 + 256) ld < 2^31 they meet inside the product; otherwise the sums of all rows go through the workspace, in more time.  Where out / 2 is a multiple of 128
+ * the first value lies less than 4 GiB behind the first gate (BITSTACK_E_RANGE). */
 typedef struct bitstack_f8_epilogue {
     const void* bias;
     int bias_dtype;
@@ -116,7 +117,8 @@ typedef struct bitstack_f8_epilogue {
     const void* residual;
     size_t ld_residual;
 } bitstack_f8_epilogue_t;
-/* As bitstack_f8_workspace_bytes (up to so many rows, any types), and as bitstack_f8_call_workspace_bytes (one call). */
+/* As bitstack_f8_workspace_bytes (up to so many rows, any types; a weight whose rows lie next to each other, rounded up to 128 bytes: others with (out / 2 + 256) ld >= 2^31 may
+ * need what the other function says), and as bitstack_f8_call_workspace_bytes (one call). */
 size_t bitstack_f8_epilogue_workspace_bytes(int rows, int in, int out, int activation);
 size_t bitstack_f8_epilogue_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, int y_dtype);
 int bitstack_f8_linear_epilogue(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, void* y, int y_dtype,

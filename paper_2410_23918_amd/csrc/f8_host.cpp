@@ -72,20 +72,23 @@ bool raw_rows(const bitstack_f8_rows_t& x, const bitstack_f8_weight_t& w, int y_
     return !misaligned(x.x, 16) && (x.rows == 1 || (x.ld % 8 == 0 && x.ld <= kMaxRowBytes / 2)) && (size_t(x.rows - 1) * x.ld + w.in) * 2 <= kMaxRowBytes;
 }
 
-// What follows the product.  Gates and values whose rows do not share their blocks of 128 are joined from partial sums of all rows.
+// What follows the product.  Gates and values meet inside it where their rows do not share blocks of 128 and one descriptor reaches both by 31-bit offsets;
+// otherwise they are joined from partial sums of all rows.
 bool is_gated(const bitstack_f8_epilogue_t* e) { return e && e->activation == BITSTACK_ACT_SILU_GATED; }
 bool any_epilogue(const bitstack_f8_epilogue_t* e) { return e && (e->bias || e->residual || e->activation != BITSTACK_ACT_NONE); }
-bool parts_only(const bitstack_f8_epilogue_t* e, int out) { return is_gated(e) && out / 2 % kF8Block != 0; }
-F8Plan plan_of(const bitstack_f8_epilogue_t* e, int rows, int out, int in, int experts, bool grouped, bool exact, bool ws_f32, size_t room = ~size_t(0)) {
-    return parts_only(e, out) ? f8_plan_parts(rows, out, in, exact, ws_f32, room) : f8_plan(rows, out, in, experts, grouped, exact, ws_f32, room);
+bool parts_only(const bitstack_f8_epilogue_t* e, int out, size_t ld) {
+    return is_gated(e) && (out / 2 % kF8Block != 0 || (size_t(out / 2) + 256) * ld > kMaxRowBytes);
+}
+F8Plan plan_of(const bitstack_f8_epilogue_t* e, int rows, const bitstack_f8_weight_t& w, bool grouped, bool exact, size_t room = ~size_t(0)) {
+    const bool ws_f32 = w.scale_type == BITSTACK_S_F32;
+    return parts_only(e, w.out, w.ld) ? f8_plan_parts(rows, w.out, w.in, exact, ws_f32, room) : f8_plan(rows, w.out, w.in, w.experts, grouped, exact, ws_f32, room);
 }
 int check_epilogue(const bitstack_f8_epilogue_t& e, const bitstack_f8_weight_t& w, int rows, int y_dtype) {
     if (e.activation < BITSTACK_ACT_NONE || e.activation > BITSTACK_ACT_SILU_GATED) return BITSTACK_E_ARG;
     if (e.bias && !real_type(e.bias_dtype)) return BITSTACK_E_ARG;
     const bool gated = is_gated(&e);
     if (gated && w.out % 2 != 0) return BITSTACK_E_SHAPE;
-    // gates and values are reached from one descriptor, by 31-bit offsets
-    if (gated && !parts_only(&e, w.out) && (size_t(w.out / 2) + 256) * w.ld > kMaxRowBytes) return BITSTACK_E_RANGE;
+    if (gated && w.out / 2 % kF8Block == 0 && w.ld <= kMaxLd && size_t(w.out / 2) * w.ld >> 32) return BITSTACK_E_RANGE;   // as documented
     if (e.bias && misaligned(e.bias, type_size(e.bias_dtype))) return BITSTACK_E_ALIGN;
     if (misaligned(e.residual, type_size(y_dtype))) return BITSTACK_E_ALIGN;
     if (e.residual && rows > 1 && e.ld_residual < size_t(gated ? w.out / 2 : w.out)) return BITSTACK_E_SHAPE;
@@ -104,11 +107,11 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     if (w->ld < size_t(w->in) || w->ld > kMaxLd || (y_rows > 1 && ld_y < size_t(cols))) return BITSTACK_E_SHAPE;
     if (misaligned(y, type_size(y_dtype))) return BITSTACK_E_ALIGN;
     auto plan_in = [&](size_t room) {
-        return plan_of(epi, y_rows, w->out, w->in, w->experts, offsets != nullptr, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32, room);
+        return plan_of(epi, y_rows, *w, offsets != nullptr, y_dtype == BITSTACK_T_F32, room);
     };
     F8Plan plan = plan_in(~size_t(0));
     if (!f8_launchable(plan)) return BITSTACK_E_RANGE;   // with any kernel's tiles
-    if (parts_only(epi, w->out) && plan.part_bytes >> 37) return BITSTACK_E_RANGE;   // joining them is one launch, 32 bytes to a thread
+    if (parts_only(epi, w->out, w->ld) && plan.part_bytes >> 37) return BITSTACK_E_RANGE;   // joining them is one launch, 32 bytes to a thread
     const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
     Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {
@@ -169,7 +172,7 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
         p.bias_dtype = epi->bias_dtype;
         p.residual = epi->residual;
         p.ld_r = epi->ld_residual;
-        p.parts_only = parts_only(epi, w->out);
+        p.parts_only = parts_only(epi, w->out, w->ld);
     }
     const hipError_t e = launch_f8_product(p, plan, st);
     return e == hipSuccess ? BITSTACK_OK : hip_error(e);
@@ -278,7 +281,7 @@ size_t bitstack_f8_epilogue_workspace_bytes(int rows, int in, int out, int activ
     if (activation < BITSTACK_ACT_NONE || activation > BITSTACK_ACT_SILU_GATED || (activation == BITSTACK_ACT_SILU_GATED && out % 2 != 0)) return 0;
     size_t most = bitstack_f8_workspace_bytes(rows, in, rows, out, 1);
     const bitstack_f8_epilogue_t e = {nullptr, 0, activation, nullptr, 0};
-    if (!most || !rows || !parts_only(&e, out)) return most;
+    if (!most || !rows || !parts_only(&e, out, bitstack_f8_row_bytes(in))) return most;
     for (int k = 0; k < 4; ++k) {
         const size_t n = workspace_of(rows, in, f8_plan_parts(rows, out, in, k & 1, k >> 1), false, false).total;
         most = n > most ? n : most;
@@ -288,7 +291,7 @@ size_t bitstack_f8_epilogue_workspace_bytes(int rows, int in, int out, int activ
 
 size_t bitstack_f8_epilogue_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const bitstack_f8_epilogue_t* epilogue, int y_dtype) {
     if (!x || !w || w->experts != 1 || check_call(x, w, x->rows, y_dtype) || (epilogue && check_epilogue(*epilogue, *w, x->rows, y_dtype)) || x->rows == 0) return 0;
-    const F8Plan plan = plan_of(epilogue, x->rows, w->out, w->in, 1, false, y_dtype == BITSTACK_T_F32, w->scale_type == BITSTACK_S_F32);
+    const F8Plan plan = plan_of(epilogue, x->rows, *w, false, y_dtype == BITSTACK_T_F32);
     return workspace_of(x->rows, w->in, plan, x->dtype == BITSTACK_T_F8 || raw_rows(*x, *w, x->rows, plan, false), false).total;
 }
 

@@ -321,7 +321,8 @@ def f8_workspace_bytes(x_rows: int, inn: int, y_rows: int, out: int, experts: in
 
 
 def f8_epilogue_workspace_bytes(rows: int, inn: int, out: int, activation=None) -> int:
-    """bitstack_f8_epilogue_workspace_bytes: of a `workspace` for linear_f8 with bias, activation or residual and up to so many rows (out: rows of q)."""
+    """bitstack_f8_epilogue_workspace_bytes: of a `workspace` for linear_f8 with bias, activation or residual and up to so many rows (out: rows of q, which
+    lie next to each other; gates and values some 2 GiB apart may need more, and a call without `workspace` allocates it)."""
     n = int(_f8_lib().bitstack_f8_epilogue_workspace_bytes(rows, inn, out, _ACTIVATIONS.get(activation, -1)))
     if n == 0:
         raise BitStackError(-2, "bitstack_f8_epilogue_workspace_bytes")
