@@ -96,7 +96,9 @@ size_t bitstack_f8_call_workspace_bytes(const bitstack_f8_rows_t* x, const bitst
                                         int grouped);
 
 /* y[t][o] = sum_j x8[t][j] w[o][j]: y [rows][out] of y_dtype (not F8), ld_y elements from row to row.  w and x are
- * host structs, read during the call.  rows may be 0. */
+ * host structs, read during the call.  rows may be 0.  y may lie over x, unless x is BITSTACK_T_F8: the call then needs the workspace of
+ * bitstack_f8_workspace_bytes also where bitstack_f8_call_workspace_bytes says 0.  This holds for the next two calls too; y must not lie over anything else
+ * that a call reads, but for the residual below. */
 int bitstack_f8_linear(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, void* y, int y_dtype, size_t ld_y,
                        void* workspace, size_t workspace_bytes, bitstack_stream_t stream);
 
@@ -166,7 +168,7 @@ int bitstack_combine(const void* h, int dtype, size_t ld_h, int h_rows, int widt
  * the residual).  Two kernels that read the weights of the experts which have tokens once: faster than the calls above for as long as that is what
  * takes the time.  x and h are not brought to 8 bits: x is taken as it is, h with 16 bits (outputs of 16 bits) or 24, sums are fp32, y is rounded once.  A
  * block of 128 columns is summed before its scale is applied; these sums have to be finite.
- *   x, y, residual: [tokens][hidden] of dtype (not F8), residual may be NULL, and may be y.  logits: of logits_dtype.  ld_*: elements from row to row.
+ *   x, y, residual: [tokens][hidden] of dtype (not F8), residual may be NULL; y may be x, residual or both, and must not lie over anything else that is read.  logits: of logits_dtype.  ld_*: elements from row to row.
  *   w1: [experts][2 width][hidden], gates above values; w2: [experts][hidden][width]; hidden at least 8, an expert's w1 below 4 GiB.
  *   workspace: 256-byte aligned, enough for up to so many tokens of any type; free for other use once the stream has passed the call.
  * The results do not depend on the order in which anything runs. */

@@ -95,6 +95,20 @@ int check_epilogue(const bitstack_f8_epilogue_t& e, const bitstack_f8_weight_t& 
     return BITSTACK_OK;
 }
 
+// Do rows of a and of b, so many bytes long and so far apart, share memory?
+struct Rows {
+    const void* p;
+    size_t ld, bytes;
+};
+bool share_memory(const Rows& a, const Rows& b, int rows) {
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+    if (a0 + (rows - 1) * a.ld + a.bytes <= b0 || b0 + (rows - 1) * b.ld + b.bytes <= a0) return false;
+    for (int i = 0; i < rows; ++i)   // they may lie between each other
+        for (int j = 0; j < rows; ++j)
+            if (a0 + i * a.ld < b0 + j * b.ld + b.bytes && b0 + j * b.ld < a0 + i * a.ld + a.bytes) return true;
+    return false;
+}
+
 int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const int32_t* offsets, const int32_t* index, int y_rows, const bitstack_f8_epilogue_t* epi,
             void* y, int y_dtype, size_t ld_y, void* workspace, size_t workspace_bytes, bitstack_stream_t stream) {
     int rc = check_call(x, w, y_rows, y_dtype);
@@ -112,7 +126,13 @@ int product(const bitstack_f8_rows_t* x, const bitstack_f8_weight_t* w, const in
     F8Plan plan = plan_in(~size_t(0));
     if (!f8_launchable(plan)) return BITSTACK_E_RANGE;   // with any kernel's tiles
     if (parts_only(epi, w->out, w->ld) && plan.part_bytes >> 37) return BITSTACK_E_RANGE;   // joining them is one launch, 32 bytes to a thread
-    const bool quantised = x->dtype == BITSTACK_T_F8, raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
+    const bool quantised = x->dtype == BITSTACK_T_F8;
+    // Where every workgroup reads x for itself, one may have written its outputs before another one reads: not over x
+    bool raw = raw_rows(*x, *w, y_rows, plan, offsets != nullptr);
+    if (raw && plan.tiles > 1) {
+        const size_t size = type_size(y_dtype);
+        raw = !share_memory({x->x, x->rows > 1 ? x->ld * 2 : 0, size_t(w->in) * 2}, {y, y_rows > 1 ? ld_y * size : 0, cols * size}, y_rows);
+    }
     Workspace at = workspace_of(x->rows, w->in, plan, quantised || raw, offsets != nullptr);
     if (at.total) {
         if (!workspace) return BITSTACK_E_NULL;

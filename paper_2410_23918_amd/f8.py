@@ -222,6 +222,14 @@ def _fill_rows(x, inn, gated):
     return rows, x.dtype, (x,)
 
 
+def _lies_over(y, x):
+    """do the extents of two matrices meet?  A call whose y lies over its x needs a workspace for x in 8 bits"""
+    if isinstance(x, F8Rows) or 0 in y.shape:
+        return False
+    a, b = x.data_ptr(), y.data_ptr()
+    return a < b + ((y.shape[0] - 1) * y.stride(0) + y.shape[1]) * y.element_size() and b < a + ((x.shape[0] - 1) * x.stride(0) + x.shape[1]) * x.element_size()
+
+
 def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, stream, grouped):
     L = _f8_lib()
     out, inn, experts = _fill_weight(q, scales, grouped)
@@ -233,7 +241,7 @@ def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, strea
         if index is not None:
             _need(index.dtype is torch.int32 and index.dim() == 1 and index.is_contiguous(), "rows: int32 [rows of y]")
             rows = index.shape[0]
-    args = _args
+    args, given = _args, y is not None
     with _on(device, stream, (*held, q, scales, offsets, index, y, workspace)) as handle:
         if y is None:
             y = q.new_empty((rows, out), dtype=out_dtype or dtype)
@@ -245,6 +253,8 @@ def _product(x, q, scales, offsets, index, gated, y, out_dtype, workspace, strea
         t = _type(y, "y")
         if workspace is None:
             nbytes = L.bitstack_f8_call_workspace_bytes(args.xp, args.wp, rows, t, grouped)
+            if nbytes == 0 and given and _lies_over(y, x):
+                nbytes = L.bitstack_f8_workspace_bytes(rows, inn, rows, out, 1)
             if nbytes:
                 workspace = q.new_empty(nbytes, dtype=torch.uint8)
         else:
@@ -270,7 +280,7 @@ def _linear_with(x, q, scales, gated, bias, activation, residual, y, out_dtype, 
     rows, dtype, held = _fill_rows(x, inn, gated)
     device = q.device
     _same_device(device, scales, bias, residual, y, workspace, *held)
-    args = _args
+    args, given = _args, y is not None
     e = args.e
     e.activation = act
     if bias is None:
@@ -300,6 +310,8 @@ def _linear_with(x, q, scales, gated, bias, activation, residual, y, out_dtype, 
         t = _type(y, "y")
         if workspace is None:
             nbytes = L.bitstack_f8_epilogue_call_workspace_bytes(args.xp, args.wp, args.ep, t)
+            if nbytes == 0 and given and _lies_over(y, x):
+                nbytes = L.bitstack_f8_workspace_bytes(rows, inn, rows, args.w.out, 1)
             if nbytes:
                 workspace = q.new_empty(nbytes, dtype=torch.uint8)
         else:
@@ -331,7 +343,7 @@ def f8_epilogue_workspace_bytes(rows: int, inn: int, out: int, activation=None) 
 
 def linear_f8(x, q, scales, *, gated: bool = False, bias=None, activation=None, residual=None, y=None, out_dtype=None, workspace=None, stream=None):
     """bitstack_f8_linear: y = x8 w^T.  x [tokens, in] (gated: [tokens, 2 in], gate and value side by side) or an F8Rows; q [out, in] and its
-    scales.  y has the type of x (fp16 for F8Rows) unless given.  workspace: a uint8 tensor of f8_workspace_bytes, else one is allocated.
+    scales.  y has the type of x (fp16 for F8Rows) unless given; it may be x, or lie over it.  workspace: a uint8 tensor of f8_workspace_bytes, else one is allocated.
     bitstack_f8_linear_epilogue, with any of these: y = act(x8 w^T + bias) + residual.  bias [out]; activation "relu", "gelu" (by erf), "gelu_tanh", "silu", or
     "silu_gated", where q's rows are gates above values and y is [tokens, out / 2]; residual of y's shape and type (y itself if it is given).  workspace:
     f8_epilogue_workspace_bytes."""
