@@ -15,7 +15,11 @@ import paper_2410_23918_amd as B  # noqa: E402
 class ExpertLayer:
     """y = sum over a token's experts e of p_e  W2_e (g / (1 + exp(-g)) u),  (g, u) = W1_e x.
 
-    router: [experts, hidden]; w1, w2: (q, scales) of all experts, [experts, 2 width, hidden] (gates above values) and [experts, hidden, width]."""
+    router: [experts, hidden]; w1, w2: (q, scales) of all experts, [experts, 2 width, hidden] (gates above values) and [experts, hidden, width].
+
+    A few tokens go through the layer in one call, which takes activations as they are (their products, of a block of 128 columns before its scale, have to be
+    finite: up to 1e33); others through four, which bring them to 8 bits, some 4 % of y's norm.  So y changes by as much where the number of tokens passes from one to
+    the other."""
 
     def __init__(self, router, w1, w2, top_k: int):
         self.router, self.w1, self.w2, self.top_k = router, w1, w2, top_k
@@ -33,9 +37,22 @@ class ExpertLayer:
             return q, scales
         return cls(router, all_of(stacks1), all_of(stacks2), top_k)
 
+    def in_one_call(self, x) -> bool:
+        """Does the layer's one call take these tokens, and in less time than the four?  On an MI355X, one call and four: 64 experts of 4096 x 1024, six chosen, bf16, 16 tokens
+        126 us and 152, 64 tokens 158 and 186; eight of 4096 x 14336, two chosen, bf16, 16 tokens (four to an expert) 254 and 257, 64 tokens 293 and 269, fp32, one token 89 and
+        89, 16 tokens 324 and 309; 384 of 7168 x 2048, eight chosen, bf16, 16 tokens 914 and 894.  Where the weights are small (four of 512 x 768, 64 tokens, bf16: 24 and 52)
+        four calls take the host longer than the GPU."""
+        (experts, rows, hidden), tokens = self.w1[0].shape, x.shape[0]
+        if tokens > 64 or hidden < 8 or rows > 2**16 or self.w1[0].stride(0) >= 2**32:   # (the call's limits; width: 2 GiB of h)
+            return False
+        wide = x.dtype is torch.float32 and hidden > 2048
+        to_an_expert = tokens * self.top_k / experts
+        small = 3 * rows // 2 * hidden * experts * x.element_size() <= 2**27
+        return small or (experts <= 256 and to_an_expert <= (0.5 if wide else 8))
+
     def __call__(self, x):
         logits = x.float() @ self.router.T
-        if x.shape[0] <= 64:   # a few tokens: the whole layer in one call, activations as they are
+        if self.in_one_call(x):
             return B.expert_layer_f8(x, logits, self.w1, self.w2, self.top_k)
         r = B.route(logits, self.top_k)
         h = B.grouped_linear_f8(x, *self.w1, r.offsets, r.rows)              # a row for each (token, expert), sorted by expert
