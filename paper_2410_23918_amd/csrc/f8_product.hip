@@ -90,17 +90,24 @@ F8Plan f8_plan(int rows, int out, int in, int experts, bool grouped, bool exact,
     return plan;
 }
 F8Plan f8_plan_parts(int rows, int out, int in, bool exact, bool ws_f32, size_t room) {
-    const int kb = (in + 127) / 128;
+    const int forced = g_forced.load(), kb = (in + 127) / 128;
+    auto plan_of = [&](const F8KernelShape& k, int slices) {
+        const int each = (kb + slices - 1) / slices, n_tiles = (rows + k.toks - 1) / k.toks;
+        const size_t tiles = size_t((out + k.rows - 1) / k.rows) * n_tiles;
+        return F8Plan{k.kernel, (kb + each - 1) / each, k.toks, n_tiles, int(std::min<size_t>(tiles, 0x7fffffff)), size_t((kb + each - 1) / each) * tiles * (k.rows * k.toks * 4)};
+    };
+    auto makes_parts = [&](const F8KernelShape& k) { return k.kernel > kSlices64 && makes(k, exact); };
+    for (const F8KernelShape& k : kShapes)
+        if (forced && k.kernel == forced % 1024 && makes_parts(k)) return plan_of(k, std::max(1, std::min(forced / 1024, kb)));
     F8Plan plan{};
     double best = 1e30;
     for (const F8KernelShape& k : kShapes) {
-        if (k.kernel <= kSlices64 || !makes(k, exact)) continue;
+        if (!makes_parts(k)) continue;
         for (int slices : {1, 2, 3, 4, 5, 6, 7, 8, 12, 16}) {
             if (slices > 1 && slices > kb / 4) continue;
-            const int each = (kb + slices - 1) / slices, n_tiles = (rows + k.toks - 1) / k.toks;
-            const size_t tiles = size_t((out + k.rows - 1) / k.rows) * n_tiles;
-            const F8Plan this_one{k.kernel, (kb + each - 1) / each, k.toks, n_tiles, int(std::min<size_t>(tiles, 0x7fffffff)), size_t((kb + each - 1) / each) * tiles * (k.rows * k.toks * 4)};
+            const F8Plan this_one = plan_of(k, slices);
             // the sums are written and read whatever the slices
+            const double tiles = double((out + k.rows - 1) / k.rows) * this_one.n_tiles;
             const double us = f8_time_us(k, slices, rows, out, kb, 1, false, exact, ws_f32) + (slices == 1 ? 4.0 + tiles * k.rows * k.toks * 8 / 6.3e6 : 0.0);
             if (plan.kernel && (us >= best || !f8_launchable(this_one) || this_one.part_bytes > room)) continue;   // the smallest tiles in one slice if nothing fits
             best = f8_launchable(this_one) && this_one.part_bytes <= room ? us : 1e30;
