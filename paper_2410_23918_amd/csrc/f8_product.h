@@ -221,7 +221,7 @@ __device__ __forceinline__ bool tile_of(const F8Params& p, int nrt, unsigned tog
 // lies in four lanes), by every workgroup anew: one launch instead of two.  One token through 1024 x 4096: 7.0 us, 5.5 and 2.4 + a launch for the rows
 // quantised before; 14336 x 4096 16.7, 16.2 and 2.4; 4096 x 14336, where 256 workgroups convert 112 blocks each, 20.4, 14.4 and 2.5.
 //   Gated: the upper half of the rows are gates, the lower half values (of one fragment its first eight rows and its last, of several those with even and with
-// odd numbers).
+// odd numbers).  Both halves are whole blocks of 128 rows, so that no tile of gates, 8 to 128 of them here and below, is in part empty.
 template <int FR, int FT, int DEPTH, int MODE, int T, int EPI>
 __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
     constexpr bool kRaw = T != kRowsF8, kGated = EPI == kEpiGated;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
         for (int i = 0; i < FT; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     if (expert >= 0) {
         const unsigned char* const wbase = p.w + (size_t(expert) * p.out + n0) * p.ldw;
-        const int w_rows = kGated ? min(8 * FR, p.cols - n0) : min(16 * FR, p.out - n0);
+        const int w_rows = kGated ? 8 * FR : min(16 * FR, p.out - n0);
         const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(wbase), 0,
                                                                             int((w_rows - 1 + (kGated ? p.cols : 0)) * p.ldw + (p.in + 15) / 16 * 16), 0x00020000);
         const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p.x), 0, int(unsigned(p.x_bytes)), 0x00020000);
@@ -264,8 +264,8 @@ __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
 #pragma unroll
         for (int j = 0; j < FR; ++j) {
             int r = min(16 * j + ln, w_rows - 1);
-            if constexpr (kGated && FR == 1) r = min(ln & 7, w_rows - 1) + (ln & 8 ? p.cols : 0);
-            if constexpr (kGated && FR > 1) r = min(8 * (j & ~1) + ln, w_rows - 1) + (j & 1 ? p.cols : 0);
+            if constexpr (kGated && FR == 1) r = (ln & 7) + (ln & 8 ? p.cols : 0);
+            if constexpr (kGated && FR > 1) r = 8 * (j & ~1) + ln + (j & 1 ? p.cols : 0);
             w_off[j] = unsigned(r) * unsigned(p.ldw) + kg * 16;
         }
 #pragma unroll
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_slices(F8Params p) {
         for (int k = tid; k < kEach * FT * kLanes; k += 512) {
             const int l = k % kLanes, i = k / kLanes % FT, j = k / kLanes / FT;
             const int tok = 16 * i + (l & 15), n = n0 + 16 * j + 4 * (l >> 4);
-            if (tok >= rows || n >= p.cols) continue;
+            if (tok >= rows) continue;
             const v4f gate = sum_of((2 * j * FT + i) * 64 + l), value = sum_of(FR == 1 ? i * 64 + l + 32 : ((2 * j + 1) * FT + i) * 64 + l);
             store4_in(p, p.cols, row0 + tok, n, epilogue4_gated(p, row0 + tok, n, gate, value));
         }
@@ -479,10 +479,11 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
     constexpr int kStep = 64 * S::kWaves / kPieces;   // tokens at a time
     const int piece = tid % kPieces, n = n0 + piece * 8;
     float bias[8] = {}, bias_u[8] = {};
-    if (n < p.cols) {
+    if (kGated || n < p.cols) {
         add_bias<8>(p, n, n, bias);
         if constexpr (kGated) add_bias<8>(p, n, p.cols + n, bias_u);
     }
+    const int n_left = kGated ? 8 : p.cols - n;
     float* const sums = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int i0 = 0; i0 < FT; i0 += FTS) {
@@ -495,7 +496,7 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
                 *reinterpret_cast<v4f*>(sums + ((wt * FTS + i) * 16 + ln) * kLd + at) = acc[j][i0 + i];
             }
         __syncthreads();
-        if (n >= p.cols) continue;
+        if (!kGated && n >= p.cols) continue;
         constexpr int kAll = S::kToks / FT * FTS / kStep, kTogether = kAll < 4 ? kAll : 4;   // tokens of a thread, those whose residuals are requested together
         static_assert(kAll % kTogether == 0, "whole groups");
 #pragma unroll 1
@@ -506,7 +507,7 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
             for (int k = 0; k < kTogether; ++k) {
                 const int t = t0 + k * kStep;
                 tok[k] = t / (16 * FTS) * 16 * FT + i0 * 16 + t % (16 * FTS);
-                if (p.residual) load_as<8>(p.y_dtype, p.residual, size_t(row0 + min(tok[k], rows - 1)) * p.ld_r + n, p.cols - n, r[k]);
+                if (p.residual) load_as<8>(p.y_dtype, p.residual, size_t(row0 + min(tok[k], rows - 1)) * p.ld_r + n, n_left, r[k]);
             }
 #pragma unroll
             for (int k = 0; k < kTogether; ++k) {
@@ -524,7 +525,7 @@ __device__ __forceinline__ void finish_tile_with(const F8Params& p, unsigned cha
 #pragma unroll
                     for (int e = 0; e < 8; ++e) a[e] += r[k][e];
                 }
-                if (tok[k] < rows) store_as<8>(p.y_dtype, p.y, size_t(row0 + tok[k]) * p.ldy + n, p.cols - n, a);
+                if (tok[k] < rows) store_as<8>(p.y_dtype, p.y, size_t(row0 + tok[k]) * p.ldy + n, n_left, a);
             }
         }
     }
@@ -562,7 +563,7 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
 
     if (expert >= 0) {
         const unsigned char* const wbase = p.w + (size_t(expert) * p.out + n0) * p.ldw;
-        const int w_rows = kGated ? p.cols + min(S::kRows / 2, p.cols - n0) : min(S::kRows, p.out - n0);   // that the descriptor reaches
+        const int w_rows = kGated ? p.cols + S::kRows / 2 : min(S::kRows, p.out - n0);   // that the descriptor reaches
         const v4i wrs = buffer_over(wbase, unsigned((w_rows - 1) * p.ldw + (p.in + 15) / 16 * 16));
         const v4i xrs = buffer_over(p.x, unsigned(p.x_rows) * unsigned(p.kp));
         const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
@@ -571,7 +572,7 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
         auto w_turn = [](int r) { return (r >> 1 & 1) | (r / (4 * FR) & 3) << 1; };
         unsigned x_off[kXLoads];
         // load i of the weight brings rows 8 (wave kWLoads + i) .. + 7 of the tile; past the last row the descriptor ends, and zeros arrive.  Gated: four
-        // gates and the four values next to them (past the last gate come values, of whose columns nothing is stored)
+        // gates and the four values next to them
         constexpr unsigned kLoadRows = kGated ? 4 : 8;
         const unsigned w_lane = kGated ? (unsigned(lane >> 3 & 3) + (lane & 32 ? unsigned(p.cols) : 0u)) * unsigned(p.ldw) : unsigned(lane >> 3) * unsigned(p.ldw);
         const unsigned w_load = unsigned(kLoadRows * wave * kWLoads) * unsigned(p.ldw), w_next = kLoadRows * unsigned(p.ldw);
@@ -628,7 +629,7 @@ __global__ __launch_bounds__(512, (F8TileShape<FR, FT, WR, WT, MODE>::kTwo ? 4 :
         auto read_s = [&](int i, int b) __attribute__((always_inline)) { return int(read_lds<unsigned char>(s_frag + r_src + i * 64 + (b & 3))); };
         // the weight's scales of 64 steps, one to a lane
         const bool s_f32 = MODE == kModeF32 || (MODE == kModeExact && p.ws_f32);
-        const size_t s_row = (size_t(expert) * ((p.out + 127) / 128) + (kGated ? min(n0 + wr * 8 * FR, p.cols - 1) : min(n0 + wr * 16 * FR, p.out - 1)) / 128) * p.kb;
+        const size_t s_row = (size_t(expert) * ((p.out + 127) / 128) + (kGated ? n0 + wr * 8 * FR : min(n0 + wr * 16 * FR, p.out - 1)) / 128) * p.kb;
         int scales[kScales] = {};
         auto load_scales = [&](int b0) {
             const int b = min(b0 + lane, p.kb - 1);
@@ -758,7 +759,7 @@ __global__ __launch_bounds__(512, 2) void k_f8_tile256(F8Params p) {
 
     if (expert >= 0) {
         const unsigned char* const wbase = p.w + (size_t(expert) * p.out + n0) * p.ldw;
-        const int w_rows = kGated ? p.cols + min(128, p.cols - n0) : min(256, p.out - n0);
+        const int w_rows = kGated ? p.cols + 128 : min(256, p.out - n0);
         const v4i wrs = buffer_over(wbase, unsigned((w_rows - 1) * p.ldw + (p.in + 15) / 16 * 16));
         const v4i xrs = buffer_over(p.x, p.x_bytes);
         const v4i xsrs = buffer_over(p.xs, unsigned(p.x_rows) * unsigned(p.ks));
@@ -965,7 +966,7 @@ __global__ __launch_bounds__(256) void k_f8_join_with(F8Params p) {
     const int rt = int(tile / p.n_tiles), tt = int(tile % p.n_tiles);
     constexpr int kToks = 16 * FT * WT, kRows = (kGated ? 8 : 16) * FR;   // outputs of a wavefront
     const int tok = tt * kToks + wave / WR * 16 * FT + 16 * i + ln, n = rt * kRows * WR + wave % WR * kRows + kg * (kRows / 4) + 4 * j;
-    if (tok >= p.rows || n >= p.cols) return;
+    if (tok >= p.rows || (!kGated && n >= p.cols)) return;
     const v4f* from = reinterpret_cast<const v4f*>(p.part) + (size_t(tile) * 8 + wave) * (FR * FT * 64) + ((kGated ? 2 * j : j) * FT + i) * 64 + lane;
     const size_t step = size_t(tiles) * 8 * (FR * FT * 64);
     v4f sum = from[0], value = kGated ? from[FT * 64] : sum;
