@@ -165,11 +165,13 @@ int bitstack_combine(const void* h, int dtype, size_t ld_h, int h_rows, int widt
 /* From the router's logits to the weighted sums, for up to 64 tokens:
  *     (g, u) = w1[e] x[t],   h = g / (1 + exp(-g)) u,   y[t] = sum_j p[t][j] w2[e] h   (+ residual[t]),   e = chosen[t][j],
  * chosen and p as bitstack_route makes them of logits [tokens][experts], top_k and renormalise (a token all of whose experts are masked has y = 0, or
- * the residual).  Two kernels that read the weights of the experts which have tokens once: faster than the calls above for as long as that is what
- * takes the time.  x and h are not brought to 8 bits: x is taken as it is, h with 16 bits (outputs of 16 bits) or 24, sums are fp32, y is rounded once.  A
- * block of 128 columns is summed before its scale is applied; these sums have to be finite.
- *   x, y, residual: [tokens][hidden] of dtype (not F8), residual may be NULL; y may be x, residual or both, and must not lie over anything else that is read.  logits: of logits_dtype.  ld_*: elements from row to row.
- *   w1: [experts][2 width][hidden], gates above values; w2: [experts][hidden][width]; hidden at least 8, an expert's w1 below 4 GiB.
+ * the residual).  Two kernels that read the weights of the experts which have tokens, once for each 16 (or 32) of an expert's tokens: faster than the calls
+ * above for as long as that is what takes the time (not where experts have many tokens, or with wide fp32 x).  x and h are not brought to 8 bits: x is taken
+ * as it is, h with 16 bits (outputs of 16 bits) or 24, sums are fp32, y is rounded once.  A block of 128 columns is summed before its scale is applied; these sums have to be finite.
+ *   x, y, residual: [tokens][hidden] of dtype (not F8), residual may be NULL; y may be x, residual or both, and must not lie over anything else that is read.
+ * logits: of logits_dtype.  ld_*: elements from row to row.
+ *   w1: [experts][2 width][hidden], gates above values; w2: [experts][hidden][width]; hidden at least 8, an expert's w1 below 4 GiB, h (16 or 32 rows for each
+ * entry of as many tokens of an expert, 4 bytes an element or 6 for fp32) below 2 GiB: BITSTACK_E_RANGE.
  *   workspace: 256-byte aligned, enough for up to so many tokens of any type; free for other use once the stream has passed the call.
  * The results do not depend on the order in which anything runs. */
 size_t bitstack_f8_expert_layer_workspace_bytes(int tokens, int hidden, int width, int experts, int top_k);

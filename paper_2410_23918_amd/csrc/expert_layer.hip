@@ -397,8 +397,8 @@ __device__ __forceinline__ Active active_of(const LayerExpert* list, int a) {
 //   ODD: width is no multiple of 4, so that a lane's four rows may have two scales.
 //   Bound by the stream of the weights where there is enough of it.  28672 x 4096 an expert: one token, two experts, 46 us (5.1 TB/s; 45.5 without the products,
 // timing only), 64 tokens, all eight, 185 (5.1); 57 tokens, six of 64 of 2048 x 4096, 101 (5.3).  Before the stream comes the routing, 2 us for one token: one token,
-// six of 64, 15.3 us (3.3).  fp32 activations are three products for one, and their parts, where they are not kept, are made anew for every 32 rows: 16 tokens, two of eight
-// of 2112 x 2001, 15.7 (2.2).
+// six of 64, 15.3 us (3.3).  16 tokens, two of eight of 2112 x 2001, fp32, 15.7 (2.2): some 522 units, three to a workgroup at most where the mean is two, and rows of an odd
+// length; fp32 activations are three products for one, 1.3 us there, and their parts, where they are not kept, are made anew for every 32 rows.
 template <int T, int FR, int NF, int DEPTH, int KEEP, bool S_F32, bool ODD>
 __global__ __launch_bounds__(512, 2) void k_layer_up(LayerParams p) {
     typedef typename Elem<T>::type E;
@@ -1053,12 +1053,16 @@ LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, 
     LayerPlan plan;
     const int rows = tokens * top_k;
     const double each = double(rows) / experts;   // tokens of an expert, in the mean
+    // Entries of 16 tokens, each of which takes the expert's weights anew, or of 32, which take twice the registers.  Eight experts of 4096 x 2048, two chosen, bf16: 32 tokens, 8 to an
+    // expert in the mean, 53.1 us and 56.4, 48 tokens 57.3 and 59.3, 64 tokens 68.5 and 61.0; fp32, 64 tokens 76.7 and 100.  In nine layers the other choice was faster by 8 % at
+    // most (profiles/expert_layer_choices.txt).
     plan.fragments = tokens <= 16 || each <= (f32 ? 16 : 8) ? 1 : 2;
     const int cap = 16 * plan.fragments;
     plan.most = std::min(experts, rows) + (tokens > cap ? rows / cap : 0);
     const double actives = experts * (1.0 - std::pow(1.0 - double(top_k) / experts, tokens));
     // Rounds of units, the last one in part empty: units of half as many rows where they fill theirs better.  One token, six experts of 2048 x 4096, 1.5 rounds or 3:
-    // the layer 30.5 us and 28.7; eight tokens, eight of 28672 x 4096, 28 or 56: 197.6 and 202.4.
+    // the layer 30.5 us and 28.7; eight tokens, eight of 28672 x 4096, 28 or 56: 197.6 and 202.4.  With hidden sizes of 2304 to 4096 (no other form looks at it) the other choice was
+    // faster by 6 % at most (profiles/expert_layer_choices.txt).
     const auto filled = [&](int n) {
         const double rounds = actives * ((width + n - 1) / n) / kLayerGroups;
         return rounds / std::ceil(rounds);
@@ -1068,7 +1072,8 @@ LayerPlan layer_plan(int tokens, int hidden, int width, int experts, int top_k, 
     if (down_lds_bytes(plan.down_rows, tokens, top_k, plan.most) > 163840) plan.down_rows = 32;   // 64 tokens with many choices of many experts
     plan.pack = tokens <= 16 / (f32 ? 3 : 2) && plan.down_rows == 64;
     plan.tiles_down = (hidden + plan.down_rows - 1) / plan.down_rows;
-    // Parts of the columns: a workgroup of each compute unit takes a part of 2.5 us and the bytes at 25 a nanosecond (more than an equal share of what the memory gives)
+    // Parts of the columns: a workgroup of each compute unit takes a part of 2.5 us and the bytes at 25 a nanosecond (more than an equal share of what the memory gives).  In 14 layers
+    // the fastest number was faster by 5 % at most (the same table).
     plan.splits = 1;
     double best = 1e30;
     const double tile_us = actives * plan.down_rows * width / 25e3;

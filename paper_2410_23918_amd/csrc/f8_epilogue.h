@@ -73,8 +73,8 @@ __device__ __forceinline__ void add_residual(const F8Params& p, int row, int n, 
     for (int e = 0; e < N; ++e) a[e] += r[e];
 }
 
-// What an activation costs in the largest tiles, where nothing hides it: 2048 tokens, 28672 x 8192, bf16, in a graph: the bare product 393 us, bias and residual 405,
-// and relu 407, gelu_tanh 416, silu 428, gelu 434 (by erfcf 477).
+// What an activation costs in the largest tiles, where nothing hides it: 2048 tokens, 28672 x 8192, bf16, in a graph: the bare product 398 us, with a bias 409, and
+// relu 411, gelu_tanh 419, silu 429, gelu 434 (by erfcf 477); with a residual, 117 MB, 447, 449, 454, 463 and 470.
 // v Phi(v).  Phi(-s) = exp(-s^2 / 2) t P(t), t = 1 / (1 + 0.305 s), for s >= 0, so that no digits are lost where it is small: P of degree 7 by least relative error over
 // 0 <= s <= 14: the polynomial's 1.26e-7, coefficients and 0.305 as fp32 numbers (fitted; all in fp32 14 half steps of a value, and the exponent's rounding, 2^-23 s^2 of it, where it is small).
 __device__ __forceinline__ float gelu(float v) {

@@ -470,7 +470,7 @@ def expert_layer_workspace_bytes(tokens: int, hidden: int, width: int, experts: 
 def expert_layer_f8(x, logits, w1, w2, top_k: int, *, renormalise: bool = True, residual=None, y=None, workspace=None, stream=None):
     """bitstack_f8_expert_layer: route, both products of every token's experts and the weighted sums (+ residual), for up to 64 tokens.  x [tokens, hidden];
     logits [tokens, experts]; w1 and w2 pairs (q, scales), q [experts, 2 width, hidden] (gates above values) and [experts, hidden, width].
-    y has the type of x.  Activations are not brought to 8 bits.  workspace: a uint8 tensor of expert_layer_workspace_bytes, else one is allocated."""
+    y has the type of x, and may be x.  Activations are not brought to 8 bits.  workspace: a uint8 tensor of expert_layer_workspace_bytes, else one is allocated."""
     L = _f8_lib()
     args = _args
     out1, hidden, experts = _fill_weight(*w1, True)
